@@ -64,12 +64,13 @@ typedef enum {
     SCAP_ERR_UNSUPPORTED_ARCH = 8
 } scap_status;
 
-typedef enum { SCAP_F16 = 0, SCAP_BF16 = 1 } scap_dtype;
+typedef enum { SCAP_F16 = 0, SCAP_BF16 = 1, SCAP_F32 = 2 /* y and r of scap_fc_act only */ } scap_dtype;
 
 /* A CUDA stream handle (cudaStream_t); NULL is the legacy default stream. */
 typedef struct CUstream_st *scap_stream_t;
 
 #define SCAP_MAX_BATCH 16
+#define SCAP_MAX_ROWS 1048576 /* of scap_fc_act */
 #define SCAP_MAX_EXPERTS 32
 #define SCAP_MAX_TOP_K 4
 
@@ -201,6 +202,23 @@ scap_status scap_sparse_fc(const void *x, const void *W, const float *m, const f
  * b is fp32 [N] or NULL.  Uses scap_fc_workspace(B, K, N).                                     */
 scap_status scap_dense_fc(const void *x, const void *W, const float *b, float *y, int B, int K, int N,
                           scap_dtype dt, void *ws, size_t ws_bytes, scap_stream_t stream);
+
+/* The FC on the rows of a prompt: y = act(x W + b) + r, any number of rows M = 0..SCAP_MAX_ROWS (0: nothing is done), on the tensor
+ * cores with fp32 accumulation and one rounding to the type of y.  It is the layer that scap_sparse_fc prunes when tokens come one
+ * by one, in the same weight layout; nothing is pruned here (the batch rule of the other calls does not apply).
+ *   x[M,K]  dtype dt, rows ldx >= K elements apart; a stride that is a multiple of 8 is read in place, another one is copied into the
+ *           workspace first
+ *   W[K,N]  dtype dt;  b[N] fp32 or NULL
+ *   r[M,N]  residual, NULL for none; y[M,N]; both of dtype ydt (dt or SCAP_F32), rows ldr / ldy >= N elements apart.  r may be
+ *           y itself (with the same stride); x may not overlap y
+ *   act     u: none; relu: max(u, 0); silu: u / (1 + e^-u); gelu: u/2 (1 + erf(u / sqrt 2)); gelu_tanh: u/2 (1 + tanh(sqrt(2/pi) (u +
+ *           0.044715 u^3)))
+ * A NaN or an infinity in x makes its row non-finite, one in W its column.  Rows and columns beyond M and N are left as they were.
+ * Workspace: scap_fc_act_workspace(M, K, N, ldx) bytes.                                                                         */
+typedef enum { SCAP_ACT_NONE = 0, SCAP_ACT_RELU = 1, SCAP_ACT_SILU = 2, SCAP_ACT_GELU = 3, SCAP_ACT_GELU_TANH = 4 } scap_act;
+size_t scap_fc_act_workspace(int M, int K, int N, int64_t ldx);
+scap_status scap_fc_act(const void *x, int64_t ldx, const void *W, const float *b, scap_act act, const void *r, int64_t ldr, void *y,
+                        int64_t ldy, int M, int K, int N, scap_dtype dt, scap_dtype ydt, void *ws, size_t ws_bytes, scap_stream_t stream);
 
 /* 8-bit weights (Table 4 applies SCAP to 8-bit models).  Storage: Wq[K,N] signed 8-bit, row-major like W, and
  * wscale[K] fp32, one scale per input channel: W[k,n] = wscale[k] * Wq[k,n] (symmetric, no zero point).  x has

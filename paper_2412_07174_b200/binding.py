@@ -11,7 +11,7 @@ import warnings
 import torch
 
 __all__ = [
-    "SCAP_F16", "SCAP_BF16", "ScapError", "lib", "lib_path", "status_string", "scap_version", "scap_tune", "scap_device_status",
+    "SCAP_F16", "SCAP_BF16", "SCAP_F32", "ScapError", "lib", "lib_path", "status_string", "scap_version", "scap_tune", "scap_device_status",
     "scap_calibrate_workspace", "scap_calibrate", "scap_calibrate_ex", "SCAP_MODE_HISTOGRAM", "SCAP_MODE_MEAN", "SCAP_MODE_MEDIAN", "SCAP_MODE_KDE",
     "SCAP_ETA_PER_CHANNEL", "SCAP_ETA_SCALAR", "scap_fold_bias_workspace", "scap_fold_bias",
     "scap_fc_workspace", "scap_sparse_fc", "scap_dense_fc", "scap_sparse_fc_q8", "scap_dense_fc_q8", "scap_fold_bias_q8",
@@ -19,9 +19,11 @@ __all__ = [
     "scap_fc_host_workspace", "scap_sparse_fc_host",
     "scap_glu_workspace", "scap_glu_ffn", "scap_gelu_ffn_workspace", "scap_gelu_ffn", "scap_glu_static_capacity", "scap_glu_ffn_static", "scap_moe_workspace",
     "scap_moe_ffn", "ScapExpert", "dtype_of", "EXPORTS",
+    "SCAP_ACT_NONE", "SCAP_ACT_RELU", "SCAP_ACT_SILU", "SCAP_ACT_GELU", "SCAP_ACT_GELU_TANH", "scap_fc_act_workspace", "scap_fc_act",
 ]
 
-SCAP_F16, SCAP_BF16 = 0, 1
+SCAP_F16, SCAP_BF16, SCAP_F32 = 0, 1, 2
+SCAP_ACT_NONE, SCAP_ACT_RELU, SCAP_ACT_SILU, SCAP_ACT_GELU, SCAP_ACT_GELU_TANH = range(5)
 _HERE = os.path.dirname(os.path.abspath(__file__))
 
 # every symbol include/scap.h declares
@@ -31,6 +33,7 @@ EXPORTS = [
     "scap_sparse_fc_q8", "scap_dense_fc_q8", "scap_fold_bias_q8", "scap_sparse_fc_q4", "scap_dense_fc_q4", "scap_fold_bias_q4",
     "scap_grouped_workspace", "scap_sparse_fc_grouped", "scap_fc_host_workspace", "scap_sparse_fc_host", "scap_glu_workspace", "scap_glu_ffn", "scap_gelu_ffn_workspace",
     "scap_gelu_ffn", "scap_glu_static_capacity", "scap_glu_ffn_static", "scap_moe_workspace", "scap_moe_ffn",
+    "scap_fc_act_workspace", "scap_fc_act",
 ]
 
 
@@ -124,6 +127,11 @@ def lib():
     L.scap_moe_workspace.restype = sz
     L.scap_moe_ffn.argtypes = [vp, vp, C.POINTER(ScapExpert), i, i, vp, i, i, i, i, vp, vp, vp, sz, vp]
     L.scap_moe_ffn.restype = i
+    i64 = C.c_int64
+    L.scap_fc_act_workspace.argtypes = [i, i, i, i64]
+    L.scap_fc_act_workspace.restype = sz
+    L.scap_fc_act.argtypes = [vp, i64, vp, vp, i, vp, i64, vp, i64, i, i, i, i, i, vp, sz, vp]
+    L.scap_fc_act.restype = i
     global _call
     try:
         from ._scap_call import call
@@ -380,3 +388,32 @@ def scap_moe_ffn(h, logits, experts, top_k: int, y, ws, expert_out=None, weight_
     p, n = _ws(ws)
     _check(lib().scap_moe_ffn(_ptr(h), _ptr(logits), arr, E, top_k, _ptr(y), B, D, F, dtype_of(h), _ptr(expert_out),
                               _ptr(weight_out), p, n, _stream(stream)), "scap_moe_ffn")
+
+
+def _rows(t, name: str) -> int:
+    """Row stride of a matrix whose rows are contiguous, in elements."""
+    if t.dim() != 2 or (t.stride(1) != 1 and t.shape[1] > 1):
+        raise ValueError("%s must be a matrix with contiguous rows" % name)
+    return max(t.stride(0), t.shape[1]) if t.shape[0] <= 1 else t.stride(0)
+
+
+def scap_fc_act_workspace(M: int, K: int, N: int, ldx: int | None = None) -> int:
+    return lib().scap_fc_act_workspace(M, K, N, K if ldx is None else ldx)
+
+
+def scap_fc_act(x, W, b, y, ws, act: int = SCAP_ACT_NONE, res=None, stream=None) -> None:
+    """y = act(x W + b) + res on any number of rows; rows of x, res and y may lie apart (views of wider matrices)."""
+    M, K = x.shape
+    N = W.shape[1]
+    ydt = SCAP_F32 if y.dtype is torch.float32 else dtype_of(y)
+    if x.dtype is not W.dtype or W.shape[0] != K or not W.is_contiguous() or y.shape != (M, N):
+        raise ValueError("x [M, K] and W [K, N] must have one dtype, W contiguous rows, y the shape [M, N]")
+    if b is not None and (b.dtype is not torch.float32 or b.numel() != N or not b.is_contiguous()):
+        raise ValueError("b must be float32 [N]")
+    ldr = 0
+    if res is not None:
+        if res.shape != y.shape or res.dtype is not y.dtype:
+            raise ValueError("res must have the shape and dtype of y")
+        ldr = _rows(res, "res")
+    p, n = _ws(ws)
+    _invoke("scap_fc_act", x, _rows(x, "x"), W, b, int(act), res, ldr, y, _rows(y, "y"), M, K, N, dtype_of(x), ydt, p, n, _stream(stream))

@@ -1,0 +1,518 @@
+// The FC on the rows of a prompt: y = act(x W + b) + r for any number of rows, on the 5th-generation tensor cores.
+//
+// The library's other FC kernels take up to 16 rows, where the weights are the only traffic that counts.  With the rows of a prompt
+// the product itself is the work, so this is a matrix product: x[M,K] and W[K,N] are both moved by TMA (128-byte swizzle), W exactly
+// as it lies in memory, and the accumulators live in TMEM.
+//
+// The weight tile is the M operand of the MMA (128 output channels, MN-major), the rows of x are its N operand (BN of them,
+// K-major).  So an accumulator lane is one output channel and its columns are rows of y: a warp of the epilogue holds 32 consecutive
+// channels of a row, which it can read (residual) and write in one contiguous piece without a turn through shared memory, and the bias of a
+// lane is one register.  It also makes BN, the rows per tile, a free number in steps of 16 from a single row up.
+//
+//   warps 0-7  epilogue: accumulators to registers, bias, activation, residual, rounding, store.  Two accumulators in TMEM, so
+//              the MMAs of the next tile run meanwhile
+//   warp 8     boxes: per block of 64 channels two of W (64 x 64) and one of x (BN rows)
+//   warp 9     MMAs
+//
+// Two forms, one source:
+//   CG = 2  two CTAs of a cluster share a tile of 256 channels x BN rows (tcgen05 cta_group::2): each loads its own 128 channels
+//           of W and half of the rows, the MMA of the pair reads both, so a row of x crosses from L2 once per pair.  For many rows.
+//   CG = 1  one CTA, 128 channels x BN rows; where the tiles are too few for the device, a cluster of S CTAs splits the
+//           channels (K) and adds its S partial tiles through distributed shared memory, in rank order.  For few rows.
+// Accumulation in fp32 (TMEM), one rounding at the end to the type of y.  No atomics: the same bits each time.
+//
+// Every wait is bounded: one that runs out sets the status word, the CTA stops issuing work, waits for the copies and MMAs
+// under way, and frees its TMEM.
+#include <string.h>
+
+#include <type_traits>
+
+#include "scap_tc.cuh"
+
+namespace scap {
+
+constexpr int FA_EPI_WARPS = 8;
+constexpr int FA_THREADS = (FA_EPI_WARPS + 2) * 32;
+constexpr int FA_BK = 64;                    // channels per stage
+constexpr int FA_TN = 128;                   // output channels per CTA
+constexpr int FA_ABYTES = FA_TN * FA_BK * 2; // 16 KB of W per stage
+constexpr int FA_MAX_STAGES = 12;
+constexpr int FA_SMEM = 226 * 1024;          // of the 227 KB that a CTA may have; the barriers are inside
+
+struct FaArgs {
+    const float *b;
+    const void *r;
+    void *y;
+    long long ldr, ldy;
+    int M, K, N;
+    int act, ydt;
+    int BN, stages, S;
+    int tiles_n, tiles_m, groups;  // groups: row tiles that are walked together, for reuse in L2
+    uint32_t tmem_cols;
+    uint32_t limit;
+    int *status;
+};
+
+struct FaShared {
+    unsigned long long full[FA_MAX_STAGES], empty[FA_MAX_STAGES], tfull[2], tempty[2], drain;
+    uint32_t tmem_base;
+    int abort_flag;
+};
+
+__device__ __forceinline__ bool fa_wait(uint32_t bar, uint32_t parity, const FaArgs &a, volatile int *abort_flag) {
+    for (uint32_t i = 0; i < a.limit; ++i) {
+        if (mbarrier_try_wait(bar, parity)) return true;
+        if (*abort_flag) return false;
+    }
+    if (a.status) atomicCAS(a.status, 0, 40);
+    *abort_flag = 1;
+    return false;
+}
+
+template <int CG>
+__device__ __forceinline__ void fa_box(uint32_t dst, const CUtensorMap *map, int x, int y, uint32_t bar) {
+    if constexpr (CG == 2)  // the barrier may be the other CTA's
+        asm volatile("cp.async.bulk.tensor.2d.cta_group::2.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3}], [%4];" ::"r"(dst),
+                     "l"(map), "r"(x), "r"(y), "r"(bar) : "memory");
+    else
+        asm volatile("cp.async.bulk.tensor.2d.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3}], [%4];" ::"r"(dst),
+                     "l"(map), "r"(x), "r"(y), "r"(bar) : "memory");
+}
+
+template <int CG>
+__device__ __forceinline__ void fa_mma(uint32_t d, uint64_t da, uint64_t db, uint32_t idesc, uint32_t acc) {
+    if constexpr (CG == 2)
+        asm volatile(
+            "{\n\t.reg .pred p;\n\tsetp.ne.b32 p, %4, 0;\n\t"
+            "tcgen05.mma.cta_group::2.kind::f16 [%0], %1, %2, %3, {%5, %5, %5, %5, %5, %5, %5, %5}, p;\n\t}\n" ::"r"(d), "l"(da), "l"(db), "r"(idesc),
+            "r"(acc), "r"(0u) : "memory");
+    else
+        tc_mma(d, da, db, idesc, acc);
+}
+
+// Arrival on a barrier when the MMAs issued so far are done; with CG = 2 on both CTAs' barriers at this offset.
+template <int CG>
+__device__ __forceinline__ void fa_commit(uint32_t bar) {
+    if constexpr (CG == 2)
+        asm volatile("tcgen05.commit.cta_group::2.mbarrier::arrive::one.shared::cluster.multicast::cluster.b64 [%0], %1;" ::"r"(bar), "h"((unsigned short)3) : "memory");
+    else
+        asm volatile("tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];" ::"r"(bar) : "memory");
+}
+
+__device__ __forceinline__ void fa_arrive_cluster(uint32_t addr) {
+    asm volatile("mbarrier.arrive.release.cluster.shared::cluster.b64 _, [%0];" ::"r"(addr) : "memory");
+}
+
+__device__ __forceinline__ void fa_ld16(uint32_t (&v)[16], uint32_t addr) {
+    asm volatile(
+        "tcgen05.ld.sync.aligned.32x32b.x16.b32 {%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15}, [%16];"
+        : "=r"(v[0]), "=r"(v[1]), "=r"(v[2]), "=r"(v[3]), "=r"(v[4]), "=r"(v[5]), "=r"(v[6]), "=r"(v[7]), "=r"(v[8]), "=r"(v[9]), "=r"(v[10]),
+          "=r"(v[11]), "=r"(v[12]), "=r"(v[13]), "=r"(v[14]), "=r"(v[15])
+        : "r"(addr));
+}
+
+__device__ __forceinline__ float fa_act(float u, int act) {
+    switch (act) {
+        case SCAP_ACT_RELU: return u > 0.0f || u != u ? u : 0.0f;
+        case SCAP_ACT_SILU: return u / (1.0f + expf(-u));
+        case SCAP_ACT_GELU: return 0.5f * u * erfcf(-0.70710678118654752f * u);  // 1 + erf(a) = erfc(-a), without its cancellation
+        case SCAP_ACT_GELU_TANH: return u / (1.0f + expf(-1.5957691216057308f * (u + 0.044715f * u * u * u)));  // (1 + tanh a) / 2 = 1 / (1 + e^(-2a))
+        default: return u;
+    }
+}
+
+// YT: 0 fp16, 1 bf16, 2 fp32
+__device__ __forceinline__ float fa_load(const void *p, long long i, int ydt) {
+    if (ydt == SCAP_F32) return ld_act(reinterpret_cast<const float *>(p) + i);
+    if (ydt == SCAP_BF16) return widen1(ld_act(reinterpret_cast<const __nv_bfloat16 *>(p) + i));
+    return widen1(ld_act(reinterpret_cast<const __half *>(p) + i));
+}
+__device__ __forceinline__ void fa_store(void *p, long long i, float v, int ydt) {
+    if (ydt == SCAP_F32) reinterpret_cast<float *>(p)[i] = v;
+    else if (ydt == SCAP_BF16) reinterpret_cast<__nv_bfloat16 *>(p)[i] = __float2bfloat16_rn(v);
+    else reinterpret_cast<__half *>(p)[i] = __float2half_rn(v);
+}
+
+// Tile number -> channel tile and row tile.  Row tiles are walked in groups: the tiles that run at the same time then share both
+// their rows of x and their columns of W in L2.
+__device__ __forceinline__ void fa_tile(const FaArgs &a, int t, int &tn, int &tm) {
+    const int per = a.groups * a.tiles_n, g = t / per, in = t - g * per;
+    const int rows = min(a.groups, a.tiles_m - g * a.groups);
+    tn = in / rows;
+    tm = g * a.groups + in - tn * rows;
+}
+
+template <bool BF16, int CG>
+__global__ void __launch_bounds__(FA_THREADS, 1) fc_act_kernel(const FaArgs a, const __grid_constant__ CUtensorMap wmap,
+                                                                const __grid_constant__ CUtensorMap xmap) {
+    extern __shared__ unsigned char fa_raw[];
+    unsigned char *ring = reinterpret_cast<unsigned char *>((reinterpret_cast<uintptr_t>(fa_raw) + 1023) & ~(uintptr_t)1023);
+    const int bn_cta = a.BN / CG;                                   // rows of x that this CTA loads
+    const uint32_t stage = FA_ABYTES + (uint32_t)bn_cta * FA_BK * 2;
+    FaShared *sh = reinterpret_cast<FaShared *>(ring + (size_t)a.stages * stage);
+    const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+    const int clusters = CG == 2 ? (int)gridDim.x / 2 : (int)gridDim.x;  // (CG = 1: one tile per CTA of x; y = K ranks)
+    const int rank = CG == 2 ? (int)(blockIdx.x & 1) : 0;
+    const int first = CG == 2 ? (int)blockIdx.x / 2 : (int)blockIdx.x;
+    const int S = CG == 2 ? 1 : a.S, srank = CG == 2 ? 0 : (int)blockIdx.y;
+    const int tiles = a.tiles_n * a.tiles_m;
+    const int nkb_all = (a.K + FA_BK - 1) / FA_BK;
+    const int kb0 = (int)((long long)nkb_all * srank / S), nkb = (int)((long long)nkb_all * (srank + 1) / S) - kb0;
+    volatile int *abort_flag = &sh->abort_flag;
+
+    if (tid == 0) {
+        for (int i = 0; i < a.stages; ++i) {
+            mbar_init(&sh->full[i], 1);
+            mbar_init(&sh->empty[i], 1);
+        }
+        for (int i = 0; i < 2; ++i) {
+            mbar_init(&sh->tfull[i], 1);
+            mbar_init(&sh->tempty[i], FA_EPI_WARPS * CG);
+        }
+        mbar_init(&sh->drain, 1);
+        sh->abort_flag = 0;
+        asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+    }
+    if (warp == FA_EPI_WARPS + 1) {
+        if constexpr (CG == 2) {
+            asm volatile("tcgen05.alloc.cta_group::2.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(&sh->tmem_base)), "r"(a.tmem_cols) : "memory");
+            asm volatile("tcgen05.relinquish_alloc_permit.cta_group::2.sync.aligned;" ::: "memory");
+        } else {
+            asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(&sh->tmem_base)), "r"(a.tmem_cols) : "memory");
+            asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
+        }
+    }
+    tc_fence_before();
+    __syncthreads();
+    if (CG == 2 || S > 1) { cluster_arrive(); cluster_wait(); }  // the partner's barriers are ready before anything can arrive on them
+    tc_fence_after();
+    const uint32_t tmem = sh->tmem_base;
+
+    if (warp == FA_EPI_WARPS) {
+        // ---- boxes.  W is a constant of the layer: its first stages are asked for before the work that this call follows has finished.
+        if (lane == 0) {
+            const uint32_t ring_at = smem_u32(ring);
+            const uint32_t bytes = (uint32_t)CG * stage;
+            const int mine = first < tiles ? (tiles - first + clusters - 1) / clusters : 0;
+            const int total = mine * nkb;
+            const int ahead = total < a.stages ? total : a.stages;
+            auto full_of = [&](int st) { return CG == 2 ? cluster_addr(smem_u32(&sh->full[st]), 0) : smem_u32(&sh->full[st]); };
+            auto place = [&](int i, int &n0, int &m0, int &k0) {
+                int tn, tm;
+                const int t = i / nkb;
+                fa_tile(a, first + t * clusters, tn, tm);
+                n0 = tn * FA_TN * CG + rank * FA_TN;
+                m0 = tm * a.BN + rank * bn_cta;
+                k0 = (kb0 + i - t * nkb) * FA_BK;
+            };
+            int n0, m0, k0;
+            for (int i = 0; i < ahead; ++i) {
+                place(i, n0, m0, k0);
+                if (rank == 0) mbar_arrive_expect_tx(&sh->full[i], bytes);
+                fa_box<CG>(ring_at + i * stage, &wmap, n0, k0, full_of(i));
+                fa_box<CG>(ring_at + i * stage + FA_ABYTES / 2, &wmap, n0 + 64, k0, full_of(i));
+            }
+            griddep_wait();
+            for (int i = 0; i < ahead; ++i) {
+                place(i, n0, m0, k0);
+                fa_box<CG>(ring_at + i * stage + FA_ABYTES, &xmap, k0, m0, full_of(i));
+            }
+            int st = a.stages, sent = ahead;
+            uint32_t par = 1;
+            for (int i = ahead; i < total; ++i) {
+                if (st == a.stages) { st = 0; par ^= 1u; }
+                if (!fa_wait(smem_u32(&sh->empty[st]), par, a, abort_flag)) break;
+                place(i, n0, m0, k0);
+                if (rank == 0) mbar_arrive_expect_tx(&sh->full[st], bytes);
+                fa_box<CG>(ring_at + st * stage, &wmap, n0, k0, full_of(st));
+                fa_box<CG>(ring_at + st * stage + FA_ABYTES / 2, &wmap, n0 + 64, k0, full_of(st));
+                fa_box<CG>(ring_at + st * stage + FA_ABYTES, &xmap, k0, m0, full_of(st));
+                sent = i + 1;
+                ++st;
+            }
+            griddep_launch_dependents();
+            // After a wait that ran out nobody consumes the stages, but the copies under way still write here: wait for them, with a limit.
+            if (*abort_flag && rank == 0) {
+                for (int i = sent > a.stages ? sent - a.stages : 0; i < sent; ++i)
+                    for (uint32_t n = 0; n < TRIES / 16 && !mbarrier_try_wait(smem_u32(&sh->full[i % a.stages]), (uint32_t)(i / a.stages) & 1u); ++n) {}
+            }
+        }
+        __syncwarp();
+    } else if (warp == FA_EPI_WARPS + 1) {
+        // ---- MMAs (the whole warp runs the loop, one lane issues; with CG = 2 only in the first CTA of the pair)
+        if (rank == 0) {
+            const uint32_t idesc = (1u << 4) | ((BF16 ? 1u : 0u) << 7) | ((BF16 ? 1u : 0u) << 10) | (1u << 15) | (0u << 16) |
+                                   ((uint32_t)(a.BN >> 3) << 17) | ((uint32_t)((FA_TN * CG) >> 4) << 24);
+            const uint64_t dw0 = tc_desc(smem_u32(ring), FA_ABYTES / 2, 1024, 2), dx0 = tc_desc(smem_u32(ring) + FA_ABYTES, 16, 1024, 2);
+            const bool leader = lane == 0;
+            int st = 0, n = 0;
+            uint32_t par = 0;
+            bool ok = true, issued = false;
+            for (int t = first; t < tiles && ok; t += clusters, ++n) {
+                const int acc = n & 1;
+                if (n >= 2) {
+                    ok = fa_wait(smem_u32(&sh->tempty[acc]), (uint32_t)((n >> 1) - 1) & 1u, a, abort_flag);
+                    ok = __all_sync(0xffffffffu, ok);
+                    if (!ok) break;
+                    tc_fence_after();
+                }
+                const uint32_t d = tmem + (uint32_t)acc * (uint32_t)a.BN;
+                for (int kb = 0; kb < nkb; ++kb) {
+                    ok = fa_wait(smem_u32(&sh->full[st]), par, a, abort_flag);
+                    ok = __all_sync(0xffffffffu, ok);
+                    if (!ok) break;
+                    tc_fence_after();
+                    const uint64_t dw = dw0 + (uint64_t)((uint32_t)st * (stage >> 4)), dx = dx0 + (uint64_t)((uint32_t)st * (stage >> 4));
+                    if (leader) {
+#pragma unroll
+                        for (uint32_t k = 0; k < FA_BK / 16; ++k) fa_mma<CG>(d, dw + k * (2048 >> 4), dx + k * (32 >> 4), idesc, (kb > 0 || k > 0) ? 1u : 0u);
+                        fa_commit<CG>(smem_u32(&sh->empty[st]));
+                    }
+                    issued = true;
+                    if (++st == a.stages) { st = 0; par ^= 1u; }
+                }
+                if (ok && leader) fa_commit<CG>(smem_u32(&sh->tfull[acc]));
+                __syncwarp();
+            }
+            if (!ok && issued && leader) {  // let the MMAs under way finish before shared memory and TMEM go
+                if constexpr (CG == 2)
+                    asm volatile("tcgen05.commit.cta_group::2.mbarrier::arrive::one.shared::cluster.b64 [%0];" ::"r"(smem_u32(&sh->drain)) : "memory");
+                else
+                    fa_commit<CG>(smem_u32(&sh->drain));
+                for (uint32_t i = 0; i < TRIES / 16 && !mbarrier_try_wait(smem_u32(&sh->drain), 0); ++i) {}
+            }
+            __syncwarp();
+        }
+    } else {
+        // ---- epilogue: warp w reads the 32 lanes of its quarter, and every other 16 columns
+        const int quarter = warp & 3, half = warp >> 2;
+        const uint32_t lane_at = tmem + ((uint32_t)(quarter * 32) << 16);
+        griddep_wait();  // b and r may come from the work just before; y may still be read by it
+        int n = 0;
+        for (int t = first; t < tiles; t += clusters, ++n) {
+            int tn, tm;
+            fa_tile(a, t, tn, tm);
+            const int col = tn * FA_TN * CG + rank * FA_TN + quarter * 32 + lane;  // output channel of this lane
+            const bool on = col < a.N;
+            const float bias = on && a.b ? ld_act(a.b + col) : 0.0f;
+            const int m0 = tm * a.BN, rows = min(a.BN, a.M - m0), acc = n & 1;
+            bool ok = fa_wait(smem_u32(&sh->tfull[acc]), (uint32_t)(n >> 1) & 1u, a, abort_flag);
+            ok = __all_sync(0xffffffffu, ok);
+            if (!ok) break;
+            tc_fence_after();
+            if (S == 1) {
+                for (int c = half * 16; c < rows; c += 32) {
+                    uint32_t v[16];
+                    fa_ld16(v, lane_at + (uint32_t)(acc * a.BN + c));
+                    float r[16];
+#pragma unroll
+                    for (int j = 0; j < 16; ++j) r[j] = a.r && on && c + j < rows ? fa_load(a.r, (long long)(m0 + c + j) * a.ldr + col, a.ydt) : 0.0f;
+                    asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory");
+#pragma unroll
+                    for (int j = 0; j < 16; ++j) {
+                        float u = fa_act(__uint_as_float(v[j]) + bias, a.act);
+                        if (a.r) u += r[j];
+                        if (on && c + j < rows) fa_store(a.y, (long long)(m0 + c + j) * a.ldy + col, u, a.ydt);
+                    }
+                }
+                tc_fence_before();
+                __syncwarp();
+                if (lane == 0) {
+                    if constexpr (CG == 2) fa_arrive_cluster(cluster_addr(smem_u32(&sh->tempty[acc]), 0));
+                    else mbar_arrive(&sh->tempty[acc]);
+                }
+            } else {
+                // partial tile of this rank into the ring, which nobody uses any more: [row of y][channel]
+                float *part = reinterpret_cast<float *>(ring);
+                for (int c = half * 16; c < rows; c += 32) {
+                    uint32_t v[16];
+                    fa_ld16(v, lane_at + (uint32_t)c);
+                    asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory");
+#pragma unroll
+                    for (int j = 0; j < 16; ++j)
+                        if (c + j < rows) part[(c + j) * FA_TN + quarter * 32 + lane] = __uint_as_float(v[j]);
+                }
+            }
+        }
+    }
+    if (CG == 1 && S > 1) {
+        __syncwarp();
+        cluster_arrive();
+        cluster_wait();
+        if (!*abort_flag && warp < FA_EPI_WARPS) {
+            int tn, tm;
+            fa_tile(a, first, tn, tm);
+            const int m0 = tm * a.BN, rows = min(a.BN, a.M - m0);
+            const int ch = (warp & 3) * 32 + lane, col = tn * FA_TN + ch;
+            const float bias = col < a.N && a.b ? ld_act(a.b + col) : 0.0f;
+            const uint32_t part = smem_u32(ring);
+            // rank s finishes rows s, s + S, ... of the tile
+            for (int c = srank + S * (warp >> 2); c < rows; c += 2 * S) {
+                float u = 0.0f;
+                for (int s = 0; s < S; ++s) {
+                    float v;
+                    asm volatile("ld.shared::cluster.f32 %0, [%1];" : "=f"(v) : "r"(cluster_addr(part + (uint32_t)(c * FA_TN + ch) * 4, s)) : "memory");
+                    u += v;
+                }
+                if (col < a.N) {
+                    u = fa_act(u + bias, a.act);
+                    if (a.r) u += fa_load(a.r, (long long)(m0 + c) * a.ldr + col, a.ydt);
+                    fa_store(a.y, (long long)(m0 + c) * a.ldy + col, u, a.ydt);
+                }
+            }
+        }
+    }
+    tc_fence_before();
+    __syncthreads();
+    if (CG == 2 || S > 1) { cluster_arrive(); cluster_wait(); }  // nobody leaves while the other may still use its shared memory
+    tc_fence_after();
+    if (warp == FA_EPI_WARPS + 1) {
+        if constexpr (CG == 2)
+            asm volatile("tcgen05.dealloc.cta_group::2.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(a.tmem_cols) : "memory");
+        else
+            asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(a.tmem_cols) : "memory");
+    }
+}
+
+// Rows of x whose stride TMA cannot take (not a multiple of 16 bytes), copied to rows that it can.
+__global__ void fc_act_repack_kernel(const unsigned short *x, long long ldx, unsigned short *out, int ldo, int M, int K) {
+    griddep_wait();
+    const long long n = (long long)M * ldo;
+    for (long long i = (long long)blockIdx.x * blockDim.x + threadIdx.x; i < n; i += (long long)gridDim.x * blockDim.x) {
+        const long long m = i / ldo;
+        const int k = (int)(i - m * ldo);
+        out[i] = k < K ? __ldcg(x + m * ldx + k) : (unsigned short)0;
+    }
+}
+
+struct FaPlan {
+    int cg, BN, S, stages;
+};
+
+static int fa_stages(int cg, int BN) {
+    const int stage = FA_ABYTES + BN / cg * FA_BK * 2;
+    const int n = (FA_SMEM - 1024 - (int)sizeof(FaShared)) / stage;
+    return n < FA_MAX_STAGES ? n : FA_MAX_STAGES;
+}
+
+// The form with the shortest estimate: waves of tiles x (blocks of 64 channels x the slower of their MMAs and their
+// loads + what a tile costs besides).
+static FaPlan fa_plan(int M, int K, int N) {
+    const int sms = sm_count(), nkb = (K + FA_BK - 1) / FA_BK;
+    FaPlan best = {1, 16, 1, 0};
+    double best_t = 1e300;
+    for (int cg = 1; cg <= 2; ++cg)
+        for (int BN = 16 * cg; BN <= 256; BN += 16 * cg) {
+            if (BN >= M + 16 * cg) break;
+            const long long tiles = (long long)((N + FA_TN * cg - 1) / (FA_TN * cg)) * ((M + BN - 1) / BN);
+            const int most = cg == 1 ? MAX_CLUSTER : 1;
+            for (int S = 1; S <= most; ++S) {
+                if (S > 1 && (S > nkb || tiles * S > sms)) break;
+                const double slots = cg == 2 ? sms / 2 : sms;
+                const double waves = (double)((long long)((tiles * S + slots - 1) / slots));
+                const double mma = 4.0 * (BN / 2 < 46 ? 46 : BN / 2), load = (FA_ABYTES + BN / cg * FA_BK * 2) / 50.0;
+                const double t = waves * (((nkb + S - 1) / S) * (mma > load ? mma : load) + 600.0) + 3.0 * BN + (S > 1 ? 1500.0 : 0.0);
+                if (t < best_t) { best_t = t; best = {cg, BN, S, 0}; }
+            }
+        }
+    best.stages = fa_stages(best.cg, best.BN);
+    return best;
+}
+
+static bool fa_map(CUtensorMap *map, const void *p, long long inner, long long outer, long long ld, int box_inner, int box_outer, bool bf16) {
+    EncodeTiledFn fn = encode_tiled_fn();
+    if (!fn) return false;
+    const cuuint64_t dims[2] = {(cuuint64_t)inner, (cuuint64_t)outer};
+    const cuuint64_t strides[1] = {(cuuint64_t)ld * 2};
+    const cuuint32_t box[2] = {(cuuint32_t)box_inner, (cuuint32_t)box_outer};
+    const cuuint32_t estr[2] = {1, 1};
+    return fn(map, bf16 ? CU_TENSOR_MAP_DATA_TYPE_BFLOAT16 : CU_TENSOR_MAP_DATA_TYPE_FLOAT16, 2, const_cast<void *>(p), dims, strides, box, estr,
+              CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
+template <bool BF16, int CG>
+static cudaError_t fa_launch(const FaArgs &a, const CUtensorMap &wmap, const CUtensorMap &xmap, cudaStream_t st) {
+    static SmemOptIn opt_in;
+    auto kern = fc_act_kernel<BF16, CG>;
+    cudaError_t e = ensure_dynamic_smem(kern, FA_SMEM, opt_in);
+    if (e != cudaSuccess) return e;
+    const int tiles = a.tiles_n * a.tiles_m;
+    cudaLaunchConfig_t cfg = {};
+    if (CG == 2) {
+        const int pairs = sm_count() / 2;
+        cfg.gridDim = dim3(2 * (tiles < pairs ? tiles : pairs));
+    } else {
+        cfg.gridDim = a.S > 1 ? dim3(tiles, a.S) : dim3(tiles < sm_count() ? tiles : sm_count());
+    }
+    cfg.blockDim = dim3(FA_THREADS);
+    cfg.dynamicSmemBytes = FA_SMEM;
+    cfg.stream = st;
+    cudaLaunchAttribute attr[2];
+    attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attr[0].val.programmaticStreamSerializationAllowed = g_tune.pdl ? 1 : 0;
+    attr[1].id = cudaLaunchAttributeClusterDimension;
+    attr[1].val.clusterDim.x = CG;
+    attr[1].val.clusterDim.y = CG == 1 ? a.S : 1;
+    attr[1].val.clusterDim.z = 1;
+    cfg.attrs = attr;
+    cfg.numAttrs = CG == 2 || a.S > 1 ? 2 : 1;
+    return cudaLaunchKernelEx(&cfg, kern, a, wmap, xmap);
+}
+
+}  // namespace scap
+
+using namespace scap;
+
+extern "C" size_t scap_fc_act_workspace(int M, int K, int N, int64_t ldx) {
+    if (M < 0 || M > SCAP_MAX_ROWS || K < 1 || K > SCAP_MAX_K || N < 1 || ldx < K) return 0;
+    return ldx % 8 == 0 ? 16 : (size_t)(M > 0 ? M : 1) * align_up((size_t)K, 8) * 2;
+}
+
+extern "C" scap_status scap_fc_act(const void *x, int64_t ldx, const void *W, const float *b, scap_act act, const void *r, int64_t ldr, void *y,
+                                   int64_t ldy, int M, int K, int N, scap_dtype dt, scap_dtype ydt, void *ws, size_t ws_bytes, scap_stream_t stream) {
+    if (M < 0 || M > SCAP_MAX_ROWS || K < 1 || K > SCAP_MAX_K || N < 1 || ldx < K || ldy < N || (r && ldr < N)) return SCAP_ERR_SHAPE;
+    if ((unsigned)act > (unsigned)SCAP_ACT_GELU_TANH) return SCAP_ERR_INVALID_ARG;
+    if ((dt != SCAP_F16 && dt != SCAP_BF16) || (ydt != SCAP_F32 && ydt != dt)) return SCAP_ERR_DTYPE;
+    if (M == 0) return SCAP_OK;
+    if (!x || !W || !y || !ws) return SCAP_ERR_INVALID_ARG;
+    if (N % 8 != 0 || !aligned16(x) || !aligned16(W) || !aligned16(y) || !aligned16(b) || !aligned16(r) || !aligned16(ws)) return SCAP_ERR_ALIGN;
+    // a tensor map takes strides below 2^40 bytes; offsets of y and r are 64-bit
+    if (ldx >= (1ll << 38) || ldy >= (1ll << 38) || (r && ldr >= (1ll << 38)) || N > (1 << 30)) return SCAP_ERR_SHAPE;
+    if (ws_bytes < scap_fc_act_workspace(M, K, N, ldx)) return SCAP_ERR_WORKSPACE;
+    scap_status dev = check_device();
+    if (dev != SCAP_OK) return dev;
+    cudaStream_t st = reinterpret_cast<cudaStream_t>(stream);
+
+    const FaPlan p = fa_plan(M, K, N);
+    FaArgs a = {};
+    a.b = b; a.r = r; a.y = y; a.ldr = ldr; a.ldy = ldy;
+    a.M = M; a.K = K; a.N = N; a.act = act; a.ydt = ydt;
+    a.BN = p.BN; a.S = p.S; a.stages = p.stages;
+    const long long tn = ((long long)N + FA_TN * p.cg - 1) / (FA_TN * p.cg), tm = ((long long)M + p.BN - 1) / p.BN;
+    if (tn * tm > (1ll << 30)) return SCAP_ERR_SHAPE;
+    a.tiles_n = (int)tn; a.tiles_m = (int)tm;
+    a.groups = a.tiles_m < 8 ? a.tiles_m : 8;
+    a.tmem_cols = 32;
+    while (a.tmem_cols < 2u * (uint32_t)p.BN) a.tmem_cols *= 2;
+    a.limit = g_tune.tc_spin ? (uint32_t)g_tune.tc_spin : TRIES;
+    a.status = tc_status_ptr();
+
+    const void *xs = x;
+    long long ldxs = ldx;
+    const bool repack = ldx % 8 != 0;
+    if (repack) { xs = ws; ldxs = (long long)align_up((size_t)K, 8); }
+    CUtensorMap wmap, xmap;
+    const bool bf16 = dt == SCAP_BF16;
+    if (!fa_map(&wmap, W, N, K, N, 64, FA_BK, bf16) || !fa_map(&xmap, xs, K, M, ldxs, FA_BK, p.BN / p.cg, bf16)) return SCAP_ERR_CUDA;
+    if (repack) {
+        const long long n = (long long)M * ldxs;
+        const long long blocks = (n + 255) / 256;
+        const cudaError_t e = launch(fc_act_repack_kernel, dim3((unsigned)(blocks < 8 * sm_count() ? blocks : 8 * sm_count())), dim3(256), 0, st, g_tune.pdl != 0,
+                                     reinterpret_cast<const unsigned short *>(x), (long long)ldx, reinterpret_cast<unsigned short *>(ws), (int)ldxs, M, K);
+        if (e != cudaSuccess) return cuda_status(e);
+    }
+    cudaError_t e;
+    if (bf16) e = p.cg == 2 ? fa_launch<true, 2>(a, wmap, xmap, st) : fa_launch<true, 1>(a, wmap, xmap, st);
+    else e = p.cg == 2 ? fa_launch<false, 2>(a, wmap, xmap, st) : fa_launch<false, 1>(a, wmap, xmap, st);
+    return cuda_status(e);
+}

@@ -1,0 +1,169 @@
+"""scap_fc_act (the FC on the rows of a prompt) against the same formula in 64 bits."""
+import numpy as np
+import pytest
+import torch
+
+from scap_testlib import Guarded
+
+ACTS = {"none": 0, "relu": 1, "silu": 2, "gelu": 3, "gelu_tanh": 4}
+
+
+def act64(u, act):
+    if act == "relu":
+        return u.clamp(min=0)
+    if act == "silu":
+        return u * torch.sigmoid(u)
+    if act == "gelu":
+        return 0.5 * u * torch.erfc(-u * 0.5 ** 0.5)
+    if act == "gelu_tanh":
+        return u * torch.sigmoid(2 * (2 / np.pi) ** 0.5 * (u + 0.044715 * u ** 3))
+    return u
+
+
+def run_case(M, K, N, dt, ydt, act="none", bias=True, res=False, ldx=None, ldy=None, in_place=False, seed=0):
+    import paper_2412_07174_b200 as scap
+    g = torch.Generator(device="cuda").manual_seed(1000 + seed)
+    ldx, ldy = ldx or K, ldy or N
+    xs = torch.randn(M, ldx, generator=g, device="cuda").to(dt)
+    x = xs[:, :K]
+    W = (0.05 * torch.randn(K, N, generator=g, device="cuda")).to(dt)
+    b = 0.3 * torch.randn(N, generator=g, device="cuda") if bias else None
+    buf = Guarded(M * ldy * ydt.itemsize)
+    full = buf.view(ydt, (M, ldy))
+    full.fill_(7.0)
+    y = full[:, :N]
+    r = None
+    if res or in_place:
+        r0 = torch.randn(M, N, generator=g, device="cuda").to(ydt)
+        if in_place:
+            y.copy_(r0)
+            r = y
+        else:
+            r = r0
+    ws = Guarded(scap.scap_fc_act_workspace(M, K, N, ldx))
+    scap.scap_fc_act(x, W, b, y, ws.payload, act=ACTS[act], res=r)
+    torch.cuda.synchronize()
+    assert buf.intact() and ws.intact()
+    if ldy > N:
+        assert bool((full[:, N:] == 7.0).all())  # the columns between the rows are left as they were
+    u = x.double() @ W.double()
+    mag = x.double().abs() @ W.double().abs()
+    if bias:
+        u = u + b.double()
+        mag = mag + b.double().abs()
+    ref = act64(u, act)
+    if r is not None:
+        ref = ref + r0.double()
+        mag = mag + r0.double().abs()
+    # Products are exact in fp32; the tensor core adds with truncation, fewer than K / 8 additions into one accumulator, each off by at
+    # most 2^-23 of the running sum of magnitudes; the activations have a slope below 1.2 and add a few units of 2^-23.  Then one
+    # rounding to the type of y: half a step, eps / 2 of the value.
+    bound = 1.2 * mag * (K / 8 + 16) * 2.0 ** -23 + ref.abs() * torch.finfo(ydt).eps / 2 * 1.001 + 1e-30
+    if ydt is torch.float16:
+        bound = bound + 2.0 ** -25  # half a step of the subnormal numbers
+    err = (y.double() - ref).abs()
+    assert bool((err <= bound).all()), float((err / bound).max())
+    return y
+
+
+BF, HF, F32 = torch.bfloat16, torch.float16, torch.float32
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("M", [1, 2, 15, 16, 17, 33, 64, 100, 129, 255, 256, 257, 500])
+def test_row_counts(M):
+    run_case(M, 512, 640, BF, F32, bias=True, seed=M)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("K,N", [(1, 8), (7, 8), (8, 8), (63, 72), (64, 128), (65, 136), (1000, 248), (4096, 264), (11008, 128), (129, 4104)])
+@pytest.mark.parametrize("dt", [BF, HF])
+def test_widths(K, N, dt):
+    run_case(37, K, N, dt, dt, act="silu", res=True, seed=K + N)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("act", list(ACTS))
+@pytest.mark.parametrize("ydt", [BF, HF, F32])
+def test_activations(act, ydt):
+    dt = BF if ydt is BF else HF
+    run_case(70, 192, 208, dt, ydt, act=act, res=True, seed=3)
+    run_case(70, 192, 208, dt, ydt, act=act, bias=False, seed=4)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("M,K,N", [(1024, 512, 4096), (2048, 448, 2056), (700, 2048, 9000), (1111, 1024, 1032), (3000, 640, 2048)])
+def test_many_tiles(M, K, N):
+    run_case(M, K, N, BF, BF, act="gelu", res=True, seed=M)
+    run_case(M, K, N, HF, F32, bias=False, seed=M + 1)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("M,K,N,ldx,ldy", [(5, 100, 64, 136, 64), (40, 100, 64, 101, 80), (300, 511, 520, 511, 521), (130, 256, 264, 300, 1000)])
+def test_strides(M, K, N, ldx, ldy):
+    run_case(M, K, N, BF, BF, act="relu", res=True, ldx=ldx, ldy=ldy, seed=ldx)
+    run_case(M, K, N, HF, F32, in_place=True, ldx=ldx, ldy=ldy, seed=ldx + 1)
+
+
+@pytest.mark.gpu
+def test_same_bits_in_a_graph_and_on_another_stream():
+    import paper_2412_07174_b200 as scap
+    x = torch.randn(200, 1000, device="cuda").to(BF)[:, :999]
+    x = x.contiguous()
+    W = (0.05 * torch.randn(999, 520, device="cuda")).to(BF)
+    b = torch.randn(520, device="cuda")
+    y, y2 = torch.empty(200, 520, device="cuda"), torch.empty(200, 520, device="cuda")
+    ws = torch.empty(scap.scap_fc_act_workspace(200, 999, 520), dtype=torch.uint8, device="cuda")
+    scap.scap_fc_act(x, W, b, y, ws, act=3)
+    torch.cuda.synchronize()
+    s = torch.cuda.Stream()
+    with torch.cuda.stream(s):
+        scap.scap_fc_act(x, W, b, y2, ws, act=3)
+    s.synchronize()
+    assert torch.equal(y, y2)
+    graph = torch.cuda.CUDAGraph()
+    x2 = x.clone()
+    with torch.cuda.graph(graph):
+        scap.scap_fc_act(x2, W, b, y2, ws, act=3)
+    x2.copy_(torch.randn_like(x2))
+    graph.replay()
+    scap.scap_fc_act(x2, W, b, y, ws, act=3)
+    torch.cuda.synchronize()
+    assert torch.equal(y, y2)
+    scap.scap_device_status()
+
+
+@pytest.mark.gpu
+def test_non_finite_rows_stay_in_their_row():
+    import paper_2412_07174_b200 as scap
+    x = torch.randn(40, 128, device="cuda").to(BF)
+    W = (0.05 * torch.randn(128, 64, device="cuda")).to(BF)
+    y0, y = torch.empty(40, 64, device="cuda"), torch.empty(40, 64, device="cuda")
+    ws = torch.empty(16, dtype=torch.uint8, device="cuda")
+    scap.scap_fc_act(x, W, None, y0, ws)
+    x[3, 5], x[17, 100] = float("nan"), float("inf")
+    scap.scap_fc_act(x, W, None, y, ws)
+    bad = ~torch.isfinite(y).all(1)
+    assert bad.nonzero().flatten().tolist() == [3, 17]
+    keep = [i for i in range(40) if i not in (3, 17)]
+    assert torch.equal(y[keep], y0[keep])
+
+
+def test_refusals():
+    from paper_2412_07174_b200 import binding, build
+    build.build()
+    L = binding.lib()
+    P = 0x10000  # a fake, 16-byte aligned, never dereferenced address
+    base = dict(x=P, ldx=64, W=P, b=P, act=0, r=None, ldr=0, y=P, ldy=64, M=4, K=64, N=64, dt=1, ydt=2, ws=P, wsb=1 << 20, st=None)
+    call = lambda **kw: L.scap_fc_act(*[kw.get(k, v) for k, v in base.items()])  # noqa: E731
+    assert call(x=None) == 1 and call(W=None) == 1 and call(y=None) == 1 and call(ws=None) == 1
+    assert call(act=5) == 1 and call(act=-1) == 1
+    assert call(M=-1) == 2 and call(M=(1 << 20) + 1) == 2 and call(K=0) == 2 and call(K=(1 << 20) + 1) == 2 and call(N=0) == 2
+    assert call(ldx=63) == 2 and call(ldy=63) == 2 and call(r=P, ldr=63) == 2
+    assert call(dt=2) == 3 and call(dt=7) == 3 and call(ydt=0) == 3 and call(ydt=3) == 3
+    assert call(N=60, ldy=64) == 4 and call(x=P + 2) == 4 and call(y=P + 4) == 4 and call(b=P + 4) == 4 and call(r=P + 2, ldr=64) == 4
+    assert call(ldx=65, wsb=4 * 64 * 2 - 1) == 5
+    assert call(M=0) == 0                                   # no rows: nothing to do
+    assert call(M=0, x=None) == 0
+    assert L.scap_fc_act_workspace(4, 64, 64, 63) == 0 and L.scap_fc_act_workspace(-1, 64, 64, 64) == 0
+    assert L.scap_fc_act_workspace(4, 61, 64, 61) == 4 * 64 * 2
