@@ -11,7 +11,7 @@
 //
 //   warps 0-7  epilogue: accumulators to registers, bias, activation, residual, rounding, store.  Two accumulators in TMEM, so
 //              the MMAs of the next tile run meanwhile
-//   warp 8     boxes: per block of 64 channels two of W (64 x 64) and one of x (BN rows)
+//   warp 8     boxes: per block of 128 channels two of W (64 columns x 128 channels) and two of x (64 channels x BN rows)
 //   warp 9     MMAs
 //
 // Two forms, one source:
@@ -23,6 +23,7 @@
 //
 // Every wait is bounded: one that runs out sets the status word, the CTA stops issuing work, waits for the copies and MMAs
 // under way, and frees its TMEM.
+#include <math.h>
 #include <string.h>
 
 #include <type_traits>
@@ -33,9 +34,9 @@ namespace scap {
 
 constexpr int FA_EPI_WARPS = 8;
 constexpr int FA_THREADS = (FA_EPI_WARPS + 2) * 32;
-constexpr int FA_BK = 64;                    // channels per stage
+constexpr int FA_BK = 128;                   // channels per stage: eight MMAs per round of waits (64: the issuing lanes fall behind the tensor core)
 constexpr int FA_TN = 128;                   // output channels per CTA
-constexpr int FA_ABYTES = FA_TN * FA_BK * 2; // 16 KB of W per stage
+constexpr int FA_ABYTES = FA_TN * FA_BK * 2; // 32 KB of W per stage
 constexpr int FA_MAX_STAGES = 12;
 constexpr int FA_SMEM = 226 * 1024;          // of the 227 KB that a CTA may have; the barriers are inside
 
@@ -45,7 +46,7 @@ struct FaArgs {
     void *y;
     long long ldr, ldy;
     int M, K, N;
-    int act, ydt;
+    int act;
     int BN, stages, S;
     int tiles_n, tiles_m, groups;  // groups: row tiles that are walked together, for reuse in L2
     uint32_t tmem_cols;
@@ -67,6 +68,12 @@ __device__ __forceinline__ bool fa_wait(uint32_t bar, uint32_t parity, const FaA
     if (a.status) atomicCAS(a.status, 0, 40);
     *abort_flag = 1;
     return false;
+}
+
+__device__ __forceinline__ bool fa_elect() {
+    uint32_t on;
+    asm volatile("{ .reg .pred p; elect.sync _|p, 0xffffffff; selp.u32 %0, 1, 0, p; }" : "=r"(on));
+    return on != 0;
 }
 
 template <int CG>
@@ -121,15 +128,22 @@ __device__ __forceinline__ float fa_act(float u, int act) {
     }
 }
 
-// YT: 0 fp16, 1 bf16, 2 fp32
-__device__ __forceinline__ float fa_load(const void *p, long long i, int ydt) {
-    if (ydt == SCAP_F32) return ld_act(reinterpret_cast<const float *>(p) + i);
-    if (ydt == SCAP_BF16) return widen1(ld_act(reinterpret_cast<const __nv_bfloat16 *>(p) + i));
-    return widen1(ld_act(reinterpret_cast<const __half *>(p) + i));
+// Elements of y and r: fp32, or 16 bits of the type of x.  A load gives the bits, 0 where it is off (no branch, and nothing that
+// waits for them, so that a batch of loads is under way together); fa_widen makes the number of them.
+template <bool F32>
+__device__ __forceinline__ uint32_t fa_load(const void *p, long long i, bool on) {
+    if constexpr (F32) return __float_as_uint(ld_act_if(reinterpret_cast<const float *>(p) + i, on));
+    else return ld_act_if_u16(reinterpret_cast<const unsigned short *>(p) + i, on);
 }
-__device__ __forceinline__ void fa_store(void *p, long long i, float v, int ydt) {
-    if (ydt == SCAP_F32) reinterpret_cast<float *>(p)[i] = v;
-    else if (ydt == SCAP_BF16) reinterpret_cast<__nv_bfloat16 *>(p)[i] = __float2bfloat16_rn(v);
+template <bool BF16, bool F32>
+__device__ __forceinline__ float fa_widen(uint32_t u) {
+    if constexpr (F32) return __uint_as_float(u);
+    else return widen_bits<BF16>((unsigned short)u);
+}
+template <bool BF16, bool F32>
+__device__ __forceinline__ void fa_store(void *p, long long i, float v) {
+    if constexpr (F32) reinterpret_cast<float *>(p)[i] = v;
+    else if constexpr (BF16) reinterpret_cast<__nv_bfloat16 *>(p)[i] = __float2bfloat16_rn(v);
     else reinterpret_cast<__half *>(p)[i] = __float2half_rn(v);
 }
 
@@ -142,7 +156,7 @@ __device__ __forceinline__ void fa_tile(const FaArgs &a, int t, int &tn, int &tm
     tm = g * a.groups + in - tn * rows;
 }
 
-template <bool BF16, int CG>
+template <bool BF16, int CG, bool F32>
 __global__ void __launch_bounds__(FA_THREADS, 1) fc_act_kernel(const FaArgs a, const __grid_constant__ CUtensorMap wmap,
                                                                 const __grid_constant__ CUtensorMap xmap) {
     extern __shared__ unsigned char fa_raw[];
@@ -150,7 +164,8 @@ __global__ void __launch_bounds__(FA_THREADS, 1) fc_act_kernel(const FaArgs a, c
     const int bn_cta = a.BN / CG;                                   // rows of x that this CTA loads
     const uint32_t stage = FA_ABYTES + (uint32_t)bn_cta * FA_BK * 2;
     FaShared *sh = reinterpret_cast<FaShared *>(ring + (size_t)a.stages * stage);
-    const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+    // (the shuffles tell the compiler that these are the same in the whole warp: addresses and descriptors then stay in uniform registers)
+    const int tid = threadIdx.x, warp = __shfl_sync(0xffffffffu, tid >> 5, 0), lane = tid & 31;
     const int clusters = CG == 2 ? (int)gridDim.x / 2 : (int)gridDim.x;  // (CG = 1: one tile per CTA of x; y = K ranks)
     const int rank = CG == 2 ? (int)(blockIdx.x & 1) : 0;
     const int first = CG == 2 ? (int)blockIdx.x / 2 : (int)blockIdx.x;
@@ -186,49 +201,49 @@ __global__ void __launch_bounds__(FA_THREADS, 1) fc_act_kernel(const FaArgs a, c
     __syncthreads();
     if (CG == 2 || S > 1) { cluster_arrive(); cluster_wait(); }  // the partner's barriers are ready before anything can arrive on them
     tc_fence_after();
-    const uint32_t tmem = sh->tmem_base;
+    const uint32_t tmem = __shfl_sync(0xffffffffu, sh->tmem_base, 0);
 
     if (warp == FA_EPI_WARPS) {
-        // ---- boxes.  W is a constant of the layer: its first stages are asked for before the work that this call follows has finished.
-        if (lane == 0) {
+        // ---- boxes, by one elected lane.  W is a constant of the layer: its first stages are asked for before the work that this call
+        // follows has finished.
+        if (fa_elect()) {
             const uint32_t ring_at = smem_u32(ring);
             const uint32_t bytes = (uint32_t)CG * stage;
-            const int mine = first < tiles ? (tiles - first + clusters - 1) / clusters : 0;
-            const int total = mine * nkb;
-            const int ahead = total < a.stages ? total : a.stages;
-            auto full_of = [&](int st) { return CG == 2 ? cluster_addr(smem_u32(&sh->full[st]), 0) : smem_u32(&sh->full[st]); };
-            auto place = [&](int i, int &n0, int &m0, int &k0) {
-                int tn, tm;
-                const int t = i / nkb;
-                fa_tile(a, first + t * clusters, tn, tm);
-                n0 = tn * FA_TN * CG + rank * FA_TN;
-                m0 = tm * a.BN + rank * bn_cta;
-                k0 = (kb0 + i - t * nkb) * FA_BK;
-            };
-            int n0, m0, k0;
-            for (int i = 0; i < ahead; ++i) {
-                place(i, n0, m0, k0);
-                if (rank == 0) mbar_arrive_expect_tx(&sh->full[i], bytes);
-                fa_box<CG>(ring_at + i * stage, &wmap, n0, k0, full_of(i));
-                fa_box<CG>(ring_at + i * stage + FA_ABYTES / 2, &wmap, n0 + 64, k0, full_of(i));
-            }
-            griddep_wait();
-            for (int i = 0; i < ahead; ++i) {
-                place(i, n0, m0, k0);
-                fa_box<CG>(ring_at + i * stage + FA_ABYTES, &xmap, k0, m0, full_of(i));
-            }
-            int st = a.stages, sent = ahead;
-            uint32_t par = 1;
-            for (int i = ahead; i < total; ++i) {
-                if (st == a.stages) { st = 0; par ^= 1u; }
-                if (!fa_wait(smem_u32(&sh->empty[st]), par, a, abort_flag)) break;
-                place(i, n0, m0, k0);
+            const uint32_t full0 = CG == 2 ? cluster_addr(smem_u32(&sh->full[0]), 0) : smem_u32(&sh->full[0]);
+            const uint32_t empty0 = smem_u32(&sh->empty[0]);
+            auto ask_w = [&](int st, int n0, int k0) {
                 if (rank == 0) mbar_arrive_expect_tx(&sh->full[st], bytes);
-                fa_box<CG>(ring_at + st * stage, &wmap, n0, k0, full_of(st));
-                fa_box<CG>(ring_at + st * stage + FA_ABYTES / 2, &wmap, n0 + 64, k0, full_of(st));
-                fa_box<CG>(ring_at + st * stage + FA_ABYTES, &xmap, k0, m0, full_of(st));
-                sent = i + 1;
-                ++st;
+                fa_box<CG>(ring_at + st * stage, &wmap, n0, k0, full0 + 8 * st);
+                fa_box<CG>(ring_at + st * stage + FA_ABYTES / 2, &wmap, n0 + 64, k0, full0 + 8 * st);
+            };
+            auto ask_x = [&](int st, int m0, int k0) {
+                fa_box<CG>(ring_at + st * stage + FA_ABYTES, &xmap, k0, m0, full0 + 8 * st);
+                fa_box<CG>(ring_at + st * stage + FA_ABYTES + bn_cta * 128, &xmap, k0 + 64, m0, full0 + 8 * st);
+            };
+            const int ahead = nkb < a.stages ? nkb : a.stages;  // stages of the first tile that go out at once
+            int sent = 0, st = 0, tn = 0, tm = 0;
+            uint32_t par = 1;  // of the round before: a fresh barrier passes
+            if (first < tiles) {
+                fa_tile(a, first, tn, tm);
+                const int n0 = tn * FA_TN * CG + rank * FA_TN, m0 = tm * a.BN + rank * bn_cta;
+                for (int i = 0; i < ahead; ++i) ask_w(i, n0, (kb0 + i) * FA_BK);
+                griddep_wait();
+                for (int i = 0; i < ahead; ++i) ask_x(i, m0, (kb0 + i) * FA_BK);
+                sent = st = ahead;
+                if (st == a.stages) { st = 0; par ^= 1u; }
+            }
+            bool ok = true;
+            for (int t = first; t < tiles && ok; t += clusters) {
+                fa_tile(a, t, tn, tm);
+                const int n0 = tn * FA_TN * CG + rank * FA_TN, m0 = tm * a.BN + rank * bn_cta;
+                for (int kb = t == first ? ahead : 0; kb < nkb; ++kb) {
+                    ok = fa_wait(empty0 + 8 * st, par, a, abort_flag);
+                    if (!ok) break;
+                    ask_w(st, n0, (kb0 + kb) * FA_BK);
+                    ask_x(st, m0, (kb0 + kb) * FA_BK);
+                    ++sent;
+                    if (++st == a.stages) { st = 0; par ^= 1u; }
+                }
             }
             griddep_launch_dependents();
             // After a wait that ran out nobody consumes the stages, but the copies under way still write here: wait for them, with a limit.
@@ -239,12 +254,13 @@ __global__ void __launch_bounds__(FA_THREADS, 1) fc_act_kernel(const FaArgs a, c
         }
         __syncwarp();
     } else if (warp == FA_EPI_WARPS + 1) {
-        // ---- MMAs (the whole warp runs the loop, one lane issues; with CG = 2 only in the first CTA of the pair)
-        if (rank == 0) {
+        // ---- MMAs, by one elected lane; with CG = 2 only in the first CTA of the pair.  The elected form matters: with `lane == 0` the four
+        // MMAs and the commit of a stage took 345 cycles to issue, with elect.sync 180, and a box 85 and 25.
+        if (rank == 0 && fa_elect()) {
             const uint32_t idesc = (1u << 4) | ((BF16 ? 1u : 0u) << 7) | ((BF16 ? 1u : 0u) << 10) | (1u << 15) | (0u << 16) |
                                    ((uint32_t)(a.BN >> 3) << 17) | ((uint32_t)((FA_TN * CG) >> 4) << 24);
             const uint64_t dw0 = tc_desc(smem_u32(ring), FA_ABYTES / 2, 1024, 2), dx0 = tc_desc(smem_u32(ring) + FA_ABYTES, 16, 1024, 2);
-            const bool leader = lane == 0;
+            const uint32_t full0 = smem_u32(&sh->full[0]), empty0 = smem_u32(&sh->empty[0]);
             int st = 0, n = 0;
             uint32_t par = 0;
             bool ok = true, issued = false;
@@ -252,37 +268,34 @@ __global__ void __launch_bounds__(FA_THREADS, 1) fc_act_kernel(const FaArgs a, c
                 const int acc = n & 1;
                 if (n >= 2) {
                     ok = fa_wait(smem_u32(&sh->tempty[acc]), (uint32_t)((n >> 1) - 1) & 1u, a, abort_flag);
-                    ok = __all_sync(0xffffffffu, ok);
                     if (!ok) break;
                     tc_fence_after();
                 }
                 const uint32_t d = tmem + (uint32_t)acc * (uint32_t)a.BN;
                 for (int kb = 0; kb < nkb; ++kb) {
-                    ok = fa_wait(smem_u32(&sh->full[st]), par, a, abort_flag);
-                    ok = __all_sync(0xffffffffu, ok);
+                    ok = fa_wait(full0 + 8 * st, par, a, abort_flag);
                     if (!ok) break;
                     tc_fence_after();
                     const uint64_t dw = dw0 + (uint64_t)((uint32_t)st * (stage >> 4)), dx = dx0 + (uint64_t)((uint32_t)st * (stage >> 4));
-                    if (leader) {
+                    // (the channels beyond K of the last block are zeros in both operands)
 #pragma unroll
-                        for (uint32_t k = 0; k < FA_BK / 16; ++k) fa_mma<CG>(d, dw + k * (2048 >> 4), dx + k * (32 >> 4), idesc, (kb > 0 || k > 0) ? 1u : 0u);
-                        fa_commit<CG>(smem_u32(&sh->empty[st]));
-                    }
+                    for (uint32_t k = 0; k < FA_BK / 16; ++k)
+                        fa_mma<CG>(d, dw + k * (2048 >> 4), dx + (k >> 2) * ((uint32_t)bn_cta * 128 >> 4) + (k & 3) * (32 >> 4), idesc, (kb > 0 || k > 0) ? 1u : 0u);
+                    fa_commit<CG>(empty0 + 8 * st);
                     issued = true;
                     if (++st == a.stages) { st = 0; par ^= 1u; }
                 }
-                if (ok && leader) fa_commit<CG>(smem_u32(&sh->tfull[acc]));
-                __syncwarp();
+                if (ok) fa_commit<CG>(smem_u32(&sh->tfull[acc]));
             }
-            if (!ok && issued && leader) {  // let the MMAs under way finish before shared memory and TMEM go
+            if (!ok && issued) {  // let the MMAs under way finish before shared memory and TMEM go
                 if constexpr (CG == 2)
                     asm volatile("tcgen05.commit.cta_group::2.mbarrier::arrive::one.shared::cluster.b64 [%0];" ::"r"(smem_u32(&sh->drain)) : "memory");
                 else
                     fa_commit<CG>(smem_u32(&sh->drain));
                 for (uint32_t i = 0; i < TRIES / 16 && !mbarrier_try_wait(smem_u32(&sh->drain), 0); ++i) {}
             }
-            __syncwarp();
         }
+        __syncwarp();
     } else {
         // ---- epilogue: warp w reads the 32 lanes of its quarter, and every other 16 columns
         const int quarter = warp & 3, half = warp >> 2;
@@ -296,6 +309,13 @@ __global__ void __launch_bounds__(FA_THREADS, 1) fc_act_kernel(const FaArgs a, c
             const bool on = col < a.N;
             const float bias = on && a.b ? ld_act(a.b + col) : 0.0f;
             const int m0 = tm * a.BN, rows = min(a.BN, a.M - m0), acc = n & 1;
+            // The residual of 16 rows is asked for ahead of their accumulators: while the MMAs run, and while the 16 rows before are worked on.
+            uint32_t r[16];
+            auto ask_r = [&](int c) {
+#pragma unroll
+                for (int j = 0; j < 16; ++j) r[j] = fa_load<F32>(a.r, (long long)(m0 + c + j) * a.ldr + col, on && c + j < rows);
+            };
+            if (S == 1 && a.r) ask_r(half * 16);
             bool ok = fa_wait(smem_u32(&sh->tfull[acc]), (uint32_t)(n >> 1) & 1u, a, abort_flag);
             ok = __all_sync(0xffffffffu, ok);
             if (!ok) break;
@@ -304,16 +324,18 @@ __global__ void __launch_bounds__(FA_THREADS, 1) fc_act_kernel(const FaArgs a, c
                 for (int c = half * 16; c < rows; c += 32) {
                     uint32_t v[16];
                     fa_ld16(v, lane_at + (uint32_t)(acc * a.BN + c));
-                    float r[16];
-#pragma unroll
-                    for (int j = 0; j < 16; ++j) r[j] = a.r && on && c + j < rows ? fa_load(a.r, (long long)(m0 + c + j) * a.ldr + col, a.ydt) : 0.0f;
                     asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory");
+                    float u[16];
 #pragma unroll
-                    for (int j = 0; j < 16; ++j) {
-                        float u = fa_act(__uint_as_float(v[j]) + bias, a.act);
-                        if (a.r) u += r[j];
-                        if (on && c + j < rows) fa_store(a.y, (long long)(m0 + c + j) * a.ldy + col, u, a.ydt);
+                    for (int j = 0; j < 16; ++j) u[j] = fa_act(__uint_as_float(v[j]) + bias, a.act);
+                    if (a.r) {
+#pragma unroll
+                        for (int j = 0; j < 16; ++j) u[j] += fa_widen<BF16, F32>(r[j]);
+                        ask_r(c + 32);
                     }
+#pragma unroll
+                    for (int j = 0; j < 16; ++j)
+                        if (on && c + j < rows) fa_store<BF16, F32>(a.y, (long long)(m0 + c + j) * a.ldy + col, u[j]);
                 }
                 tc_fence_before();
                 __syncwarp();
@@ -346,18 +368,41 @@ __global__ void __launch_bounds__(FA_THREADS, 1) fc_act_kernel(const FaArgs a, c
             const int ch = (warp & 3) * 32 + lane, col = tn * FA_TN + ch;
             const float bias = col < a.N && a.b ? ld_act(a.b + col) : 0.0f;
             const uint32_t part = smem_u32(ring);
-            // rank s finishes rows s, s + S, ... of the tile
-            for (int c = srank + S * (warp >> 2); c < rows; c += 2 * S) {
-                float u = 0.0f;
-                for (int s = 0; s < S; ++s) {
-                    float v;
-                    asm volatile("ld.shared::cluster.f32 %0, [%1];" : "=f"(v) : "r"(cluster_addr(part + (uint32_t)(c * FA_TN + ch) * 4, s)) : "memory");
-                    u += v;
+            // rank s finishes rows s, s + S, ... of the tile, a warp four of them at a time: a remote load takes several hundred cycles
+            for (int c0 = srank + S * (warp >> 2); c0 < rows; c0 += 8 * S) {
+                float u[4] = {0.0f, 0.0f, 0.0f, 0.0f};
+                uint32_t r[4];
+                if (a.r) {
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) {
+                        const int c = c0 + 2 * S * i;
+                        r[i] = fa_load<F32>(a.r, (long long)(m0 + c) * a.ldr + col, c < rows && col < a.N);
+                    }
                 }
-                if (col < a.N) {
-                    u = fa_act(u + bias, a.act);
-                    if (a.r) u += fa_load(a.r, (long long)(m0 + c) * a.ldr + col, a.ydt);
-                    fa_store(a.y, (long long)(m0 + c) * a.ldy + col, u, a.ydt);
+                for (int s0 = 0; s0 < S; s0 += 4) {
+                    float v[4][4];
+#pragma unroll
+                    for (int s = 0; s < 4; ++s) {  // (a rank or a row that there is not reads the first one, and is not used)
+                        const uint32_t at = cluster_addr(part + (uint32_t)ch * 4, s0 + s < S ? s0 + s : s0);
+#pragma unroll
+                        for (int i = 0; i < 4; ++i) {
+                            const int c = c0 + 2 * S * i;
+                            asm volatile("ld.shared::cluster.f32 %0, [%1];" : "=f"(v[s][i]) : "r"(at + (uint32_t)(c < rows ? c : c0) * (FA_TN * 4)) : "memory");
+                        }
+                    }
+#pragma unroll
+                    for (int s = 0; s < 4; ++s)
+#pragma unroll
+                        for (int i = 0; i < 4; ++i) u[i] += s0 + s < S ? v[s][i] : 0.0f;
+                }
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    const int c = c0 + 2 * S * i;
+                    if (c < rows && col < a.N) {
+                        float w = fa_act(u[i] + bias, a.act);
+                        if (a.r) w += fa_widen<BF16, F32>(r[i]);
+                        fa_store<BF16, F32>(a.y, (long long)(m0 + c) * a.ldy + col, w);
+                    }
                 }
             }
         }
@@ -395,11 +440,12 @@ static int fa_stages(int cg, int BN) {
     return n < FA_MAX_STAGES ? n : FA_MAX_STAGES;
 }
 
-// The form with the shortest estimate: waves of tiles x (blocks of 64 channels x the slower of their MMAs and their
-// loads + what a tile costs besides).
+// The form with the shortest estimate, in cycles: waves of tiles x blocks of 128 channels x the slower of a block's MMAs and its loads (60
+// bytes per cycle and SM, from L2), W at the rate of the memory, and what the epilogue and the sum over ranks cost.
 static FaPlan fa_plan(int M, int K, int N) {
     const int sms = sm_count(), nkb = (K + FA_BK - 1) / FA_BK;
     FaPlan best = {1, 16, 1, 0};
+    const double floor = 0.3 * K * (double)N * 2 / 1000.0;  // W at the rate of the memory, in cycles
     double best_t = 1e300;
     for (int cg = 1; cg <= 2; ++cg)
         for (int BN = 16 * cg; BN <= 256; BN += 16 * cg) {
@@ -410,8 +456,10 @@ static FaPlan fa_plan(int M, int K, int N) {
                 if (S > 1 && (S > nkb || tiles * S > sms)) break;
                 const double slots = cg == 2 ? sms / 2 : sms;
                 const double waves = (double)((long long)((tiles * S + slots - 1) / slots));
-                const double mma = 4.0 * (BN / 2 < 46 ? 46 : BN / 2), load = (FA_ABYTES + BN / cg * FA_BK * 2) / 50.0;
-                const double t = waves * (((nkb + S - 1) / S) * (mma > load ? mma : load) + 600.0) + 3.0 * BN + (S > 1 ? 1500.0 : 0.0);
+                const double mma = 8.0 * (BN / 2 < 46 ? 46 : BN / 2), load = (FA_ABYTES + BN / cg * FA_BK * 2) / 60.0;
+                double t = waves * ((nkb + S - 1) / S) * (mma > load ? mma : load);
+                t = sqrt(t * t + floor * floor);  // the closer to the memory's rate, the slower each SM's share
+                t += 3.0 * BN + (S > 1 ? 4000.0 + 40.0 * BN : 0.0);
                 if (t < best_t) { best_t = t; best = {cg, BN, S, 0}; }
             }
         }
@@ -430,10 +478,10 @@ static bool fa_map(CUtensorMap *map, const void *p, long long inner, long long o
               CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
-template <bool BF16, int CG>
-static cudaError_t fa_launch(const FaArgs &a, const CUtensorMap &wmap, const CUtensorMap &xmap, cudaStream_t st) {
+template <bool BF16, int CG, bool F32>
+static cudaError_t fa_launch_y(const FaArgs &a, const CUtensorMap &wmap, const CUtensorMap &xmap, cudaStream_t st) {
     static SmemOptIn opt_in;
-    auto kern = fc_act_kernel<BF16, CG>;
+    auto kern = fc_act_kernel<BF16, CG, F32>;
     cudaError_t e = ensure_dynamic_smem(kern, FA_SMEM, opt_in);
     if (e != cudaSuccess) return e;
     const int tiles = a.tiles_n * a.tiles_m;
@@ -457,6 +505,11 @@ static cudaError_t fa_launch(const FaArgs &a, const CUtensorMap &wmap, const CUt
     cfg.attrs = attr;
     cfg.numAttrs = CG == 2 || a.S > 1 ? 2 : 1;
     return cudaLaunchKernelEx(&cfg, kern, a, wmap, xmap);
+}
+
+template <bool BF16, int CG>
+static cudaError_t fa_launch(const FaArgs &a, bool f32, const CUtensorMap &wmap, const CUtensorMap &xmap, cudaStream_t st) {
+    return f32 ? fa_launch_y<BF16, CG, true>(a, wmap, xmap, st) : fa_launch_y<BF16, CG, false>(a, wmap, xmap, st);
 }
 
 }  // namespace scap
@@ -486,7 +539,7 @@ extern "C" scap_status scap_fc_act(const void *x, int64_t ldx, const void *W, co
     const FaPlan p = fa_plan(M, K, N);
     FaArgs a = {};
     a.b = b; a.r = r; a.y = y; a.ldr = ldr; a.ldy = ldy;
-    a.M = M; a.K = K; a.N = N; a.act = act; a.ydt = ydt;
+    a.M = M; a.K = K; a.N = N; a.act = act;
     a.BN = p.BN; a.S = p.S; a.stages = p.stages;
     const long long tn = ((long long)N + FA_TN * p.cg - 1) / (FA_TN * p.cg), tm = ((long long)M + p.BN - 1) / p.BN;
     if (tn * tm > (1ll << 30)) return SCAP_ERR_SHAPE;
@@ -503,7 +556,7 @@ extern "C" scap_status scap_fc_act(const void *x, int64_t ldx, const void *W, co
     if (repack) { xs = ws; ldxs = (long long)align_up((size_t)K, 8); }
     CUtensorMap wmap, xmap;
     const bool bf16 = dt == SCAP_BF16;
-    if (!fa_map(&wmap, W, N, K, N, 64, FA_BK, bf16) || !fa_map(&xmap, xs, K, M, ldxs, FA_BK, p.BN / p.cg, bf16)) return SCAP_ERR_CUDA;
+    if (!fa_map(&wmap, W, N, K, N, 64, FA_BK, bf16) || !fa_map(&xmap, xs, K, M, ldxs, 64, p.BN / p.cg, bf16)) return SCAP_ERR_CUDA;
     if (repack) {
         const long long n = (long long)M * ldxs;
         const long long blocks = (n + 255) / 256;
@@ -511,8 +564,9 @@ extern "C" scap_status scap_fc_act(const void *x, int64_t ldx, const void *W, co
                                      reinterpret_cast<const unsigned short *>(x), (long long)ldx, reinterpret_cast<unsigned short *>(ws), (int)ldxs, M, K);
         if (e != cudaSuccess) return cuda_status(e);
     }
+    const bool f32 = ydt == SCAP_F32;
     cudaError_t e;
-    if (bf16) e = p.cg == 2 ? fa_launch<true, 2>(a, wmap, xmap, st) : fa_launch<true, 1>(a, wmap, xmap, st);
-    else e = p.cg == 2 ? fa_launch<false, 2>(a, wmap, xmap, st) : fa_launch<false, 1>(a, wmap, xmap, st);
+    if (bf16) e = p.cg == 2 ? fa_launch<true, 2>(a, f32, wmap, xmap, st) : fa_launch<true, 1>(a, f32, wmap, xmap, st);
+    else e = p.cg == 2 ? fa_launch<false, 2>(a, f32, wmap, xmap, st) : fa_launch<false, 1>(a, f32, wmap, xmap, st);
     return cuda_status(e);
 }
