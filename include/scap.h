@@ -71,6 +71,7 @@ typedef struct CUstream_st *scap_stream_t;
 
 #define SCAP_MAX_BATCH 16
 #define SCAP_MAX_ROWS 1048576 /* of scap_fc_act */
+#define SCAP_MAX_SEQS 4096   /* of a 4-bit cache */
 #define SCAP_MAX_EXPERTS 32
 #define SCAP_MAX_TOP_K 4
 
@@ -369,6 +370,49 @@ size_t scap_moe_workspace(int B, int D, int F, int E, int top_k);
 scap_status scap_moe_ffn(const void *h, const float *logits, const scap_expert *experts_host, int E, int top_k,
                          float *y, int B, int D, int F, scap_dtype dt, int *expert_out, float *weight_out,
                          void *ws, size_t ws_bytes, scap_stream_t stream);
+
+/* ------------------------------------------------------------------------------------------
+ * A key / value cache in 4 bits, in pages
+ *
+ * What a decoding program needs beside the pruned projections: keys and values of the tokens so far, in the library's 4-bit
+ * convention (codes 0..15, value s (q - zero)).  A group of `group` channels of one token and key head, values x, is stored as
+ *   lo = min(0, min x), hi = max(0, max x);  s = (hi - lo) / 15, rounded to 20 significant bits;  zero = round(-lo / s);
+ *   q = min(15, max(0, round(x / s) + zero))                                              (ties to even; s = 0: all zeros)
+ * decided exactly as in real numbers.  A group with an infinity or a NaN reads back as NaN.
+ *
+ * scap_kv4 describes the cache of one layer; it is read on the host during a call.  `pages` is a pool of n_pages pages, page_stride
+ * bytes apart (a multiple of 16, at least scap_kv4_page_bytes() bytes; larger where a page holds several layers side by side:
+ * layer l then has pages + l * scap_kv4_page_bytes()).  The layout inside a page is the library's.  Any bytes are a valid empty pool.
+ *   page_tokens  tokens of a page, a multiple of 32 up to 4096;  heads 1..1024 key heads of head_dim 64, 128 or 256 channels
+ *   group        32, 64 or 128 channels, at most head_dim, at least a quarter of it
+ *   table        [n_seqs, table_stride] int32: the pages of each sequence in order, -1 behind them;  n_seqs up to SCAP_MAX_SEQS
+ *   lens         [n_seqs] int32: tokens of each sequence, the new ones of a call included
+ *   refs         [n_pages] int32: how many sequences hold a page, 0 = free.  Used by the calls on pages only
+ * table, lens, refs and row_start are DEVICE arrays and may be outputs of work placed before the call.  Where the table has no valid
+ * page for a token (beyond its row, or an entry outside 0..n_pages-1) nothing is stored or read, and attention does not see it.
+ * ------------------------------------------------------------------------------------------ */
+typedef struct {
+    void *pages;
+    size_t page_stride;
+    int n_pages, page_tokens, heads, head_dim, group;
+    int table_stride, n_seqs;
+    int *table;
+    int *lens;
+    int *refs;
+} scap_kv4;
+
+/* Bytes of one page of one layer; 0 for values that a cache cannot have. */
+size_t scap_kv4_page_bytes(int page_tokens, int heads, int head_dim, int group);
+
+/* Stores the keys and values of new tokens.  k and v hold `rows` tokens, [heads, head_dim] each (dtype dt), ldk / ldv elements
+ * apart (a multiple of 8: slices of a fused QKV result will do).  Sequence b has the rows row_start[b] .. row_start[b+1] - 1
+ * (row_start[n_seqs + 1], ascending; rows before the first and behind the last are not touched), which become its last tokens: the
+ * positions lens[b] - n .. lens[b] - 1.  row_start NULL: row b is the last token of sequence b, for the first `rows` sequences.
+ * scap_kv4_read is the way back: the same rows, their values as the cache holds them (rounded to dt).  0 <= rows <= SCAP_MAX_ROWS. */
+scap_status scap_kv4_append(const scap_kv4 *cache, const void *k, int64_t ldk, const void *v, int64_t ldv, const int *row_start, int rows,
+                            scap_dtype dt, scap_stream_t stream);
+scap_status scap_kv4_read(const scap_kv4 *cache, void *k, int64_t ldk, void *v, int64_t ldv, const int *row_start, int rows, scap_dtype dt,
+                          scap_stream_t stream);
 
 #ifdef __cplusplus
 }

@@ -20,6 +20,7 @@ __all__ = [
     "scap_glu_workspace", "scap_glu_ffn", "scap_gelu_ffn_workspace", "scap_gelu_ffn", "scap_glu_static_capacity", "scap_glu_ffn_static", "scap_moe_workspace",
     "scap_moe_ffn", "ScapExpert", "dtype_of", "EXPORTS",
     "SCAP_ACT_NONE", "SCAP_ACT_RELU", "SCAP_ACT_SILU", "SCAP_ACT_GELU", "SCAP_ACT_GELU_TANH", "scap_fc_act_workspace", "scap_fc_act",
+    "ScapKv4", "scap_kv4_page_bytes", "scap_kv4_append", "scap_kv4_read",
 ]
 
 SCAP_F16, SCAP_BF16, SCAP_F32 = 0, 1, 2
@@ -33,7 +34,7 @@ EXPORTS = [
     "scap_sparse_fc_q8", "scap_dense_fc_q8", "scap_fold_bias_q8", "scap_sparse_fc_q4", "scap_dense_fc_q4", "scap_fold_bias_q4",
     "scap_grouped_workspace", "scap_sparse_fc_grouped", "scap_fc_host_workspace", "scap_sparse_fc_host", "scap_glu_workspace", "scap_glu_ffn", "scap_gelu_ffn_workspace",
     "scap_gelu_ffn", "scap_glu_static_capacity", "scap_glu_ffn_static", "scap_moe_workspace", "scap_moe_ffn",
-    "scap_fc_act_workspace", "scap_fc_act",
+    "scap_fc_act_workspace", "scap_fc_act", "scap_kv4_page_bytes", "scap_kv4_append", "scap_kv4_read",
 ]
 
 
@@ -132,6 +133,11 @@ def lib():
     L.scap_fc_act_workspace.restype = sz
     L.scap_fc_act.argtypes = [vp, i64, vp, vp, i, vp, i64, vp, i64, i, i, i, i, i, vp, sz, vp]
     L.scap_fc_act.restype = i
+    L.scap_kv4_page_bytes.argtypes = [i, i, i, i]
+    L.scap_kv4_page_bytes.restype = sz
+    for n in ("scap_kv4_append", "scap_kv4_read"):
+        getattr(L, n).argtypes = [vp, vp, i64, vp, i64, vp, i, i, vp]
+        getattr(L, n).restype = i
     global _call
     try:
         from ._scap_call import call
@@ -417,3 +423,55 @@ def scap_fc_act(x, W, b, y, ws, act: int = SCAP_ACT_NONE, res=None, stream=None)
         ldr = _rows(res, "res")
     p, n = _ws(ws)
     _invoke("scap_fc_act", x, _rows(x, "x"), W, b, int(act), res, ldr, y, _rows(y, "y"), M, K, N, dtype_of(x), ydt, p, n, _stream(stream))
+
+
+class ScapKv4(C.Structure):
+    """The 4-bit cache of one layer (``scap_kv4``), made of the tensors that hold it.  ``pages`` [n_pages, bytes] uint8 may be a
+    view of wider pages (several layers side by side); ``table`` [n_seqs, pages of a sequence], ``lens`` [n_seqs] and ``refs`` [n_pages] are int32."""
+    _fields_ = [("pages", C.c_void_p), ("page_stride", C.c_size_t), ("n_pages", C.c_int), ("page_tokens", C.c_int), ("heads", C.c_int),
+                ("head_dim", C.c_int), ("group", C.c_int), ("table_stride", C.c_int), ("n_seqs", C.c_int), ("table", C.c_void_p),
+                ("lens", C.c_void_p), ("refs", C.c_void_p)]
+
+    def __init__(self, pages, page_tokens: int, heads: int, head_dim: int, group: int, table, lens, refs=None):
+        if pages.dtype is not torch.uint8 or pages.dim() != 2 or pages.stride(1) != 1:
+            raise ValueError("pages must be uint8 [n_pages, bytes] with contiguous rows")
+        for t, shape, name in ((table, (lens.shape[0], table.shape[-1]), "table"), (lens, (lens.shape[0],), "lens"), (refs, (pages.shape[0],), "refs")):
+            if t is not None and (t.dtype is not torch.int32 or tuple(t.shape) != shape or not t.is_contiguous()):
+                raise ValueError("%s must be a contiguous int32 tensor of shape %s" % (name, shape))
+        need = scap_kv4_page_bytes(page_tokens, heads, head_dim, group)
+        if pages.shape[1] < need:
+            raise ValueError("a page needs %d bytes, has %d" % (need, pages.shape[1]))
+        super().__init__(pages.data_ptr(), max(pages.stride(0), pages.shape[1]), pages.shape[0], int(page_tokens), int(heads), int(head_dim), int(group), table.shape[1],
+                         table.shape[0], table.data_ptr(), lens.data_ptr(), None if refs is None else refs.data_ptr())
+        self.tensors = (pages, table, lens, refs)  # kept alive with the description
+        self.address = C.addressof(self)
+
+
+def scap_kv4_page_bytes(page_tokens: int, heads: int, head_dim: int, group: int) -> int:
+    return lib().scap_kv4_page_bytes(int(page_tokens), int(heads), int(head_dim), int(group))
+
+
+def _tokens(t, heads: int, D: int, name: str) -> int:
+    """Elements between the tokens of [tokens, heads, D], which may be a slice of a wider row."""
+    if t.dim() != 3 or t.shape[1] != heads or t.shape[2] != D or t.stride(2) != 1 or (heads > 1 and t.stride(1) != D):
+        raise ValueError("%s must be [tokens, %d, %d] with contiguous heads" % (name, heads, D))
+    return t.stride(0) if t.shape[0] > 1 else max(t.stride(0), heads * D)
+
+
+def _kv4_rows(name: str, cache, k, v, row_start, stream) -> None:
+    if k.dtype is not v.dtype or k.shape != v.shape:
+        raise ValueError("k and v must have one dtype and shape")
+    if row_start is not None and (row_start.dtype is not torch.int32 or row_start.numel() != cache.n_seqs + 1 or not row_start.is_contiguous()):
+        raise ValueError("row_start must be int32 [n_seqs + 1]")
+    _invoke(name, cache.address, k, _tokens(k, cache.heads, cache.head_dim, "k"), v, _tokens(v, cache.heads, cache.head_dim, "v"), row_start, k.shape[0],
+            dtype_of(k), _stream(stream))
+
+
+def scap_kv4_append(cache, k, v, row_start=None, stream=None) -> None:
+    """Stores new tokens k, v [rows, heads, head_dim] as the last tokens of their sequences (``cache.lens`` includes them)."""
+    _kv4_rows("scap_kv4_append", cache, k, v, row_start, stream)
+
+
+def scap_kv4_read(cache, k_out, v_out, row_start=None, stream=None) -> None:
+    """The values that the cache holds for the last tokens of its sequences, addressed as in scap_kv4_append."""
+    _kv4_rows("scap_kv4_read", cache, k_out, v_out, row_start, stream)
