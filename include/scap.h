@@ -414,6 +414,20 @@ scap_status scap_kv4_append(const scap_kv4 *cache, const void *k, int64_t ldk, c
 scap_status scap_kv4_read(const scap_kv4 *cache, void *k, int64_t ldk, void *v, int64_t ldv, const int *row_start, int rows, scap_dtype dt,
                           scap_stream_t stream);
 
+/* Attention over the cache: for each sequence the last nq (1..16) of its lens[b] tokens are queries,
+ *   out[b,i,h] = sum_t p_t v_t / sum_t p_t,  p_t = exp(scale q[b,i,h] . k_t)  over the tokens t <= lens[b] - nq + i, and with window > 0
+ *   only the last `window` of these.
+ * q[n_seqs, nq, q_heads, head_dim] (dtype dt), tokens ldq elements apart (a multiple of 8); out likewise with ldo, rounded to dt;
+ * q_heads a multiple of cache->heads up to 1024, query head h reads key head h / (q_heads / heads).  lse[n_seqs, nq, q_heads] fp32 or
+ * NULL: log of the sum of the exp(...), for joining with attention over tokens that are not in the cache.  A row that sees nothing (an
+ * empty sequence, or nq > lens[b]) gives 0 and -inf.  A NaN or an infinity in a query, or in a key or value that it sees, makes
+ * its row non-finite, no other one.  Scores, sums and accumulators are fp32; a weight times the scale of its value is rounded to
+ * fp16 once, relative to the largest scale seen so far, so values below 2^-20 of the largest ones seen lose precision.
+ * Bitwise reproducible on one device.  Workspace: scap_kv4_attend_workspace() bytes.                                             */
+size_t scap_kv4_attend_workspace(int n_seqs, int nq, int q_heads, int heads, int head_dim);
+scap_status scap_kv4_attend(const scap_kv4 *cache, const void *q, int64_t ldq, void *out, int64_t ldo, float *lse, int nq, int q_heads,
+                            double scale, int window, scap_dtype dt, void *ws, size_t ws_bytes, scap_stream_t stream);
+
 #ifdef __cplusplus
 }
 #endif

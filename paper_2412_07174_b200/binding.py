@@ -20,7 +20,7 @@ __all__ = [
     "scap_glu_workspace", "scap_glu_ffn", "scap_gelu_ffn_workspace", "scap_gelu_ffn", "scap_glu_static_capacity", "scap_glu_ffn_static", "scap_moe_workspace",
     "scap_moe_ffn", "ScapExpert", "dtype_of", "EXPORTS",
     "SCAP_ACT_NONE", "SCAP_ACT_RELU", "SCAP_ACT_SILU", "SCAP_ACT_GELU", "SCAP_ACT_GELU_TANH", "scap_fc_act_workspace", "scap_fc_act",
-    "ScapKv4", "scap_kv4_page_bytes", "scap_kv4_append", "scap_kv4_read",
+    "ScapKv4", "scap_kv4_page_bytes", "scap_kv4_append", "scap_kv4_read", "scap_kv4_attend_workspace", "scap_kv4_attend",
 ]
 
 SCAP_F16, SCAP_BF16, SCAP_F32 = 0, 1, 2
@@ -34,7 +34,7 @@ EXPORTS = [
     "scap_sparse_fc_q8", "scap_dense_fc_q8", "scap_fold_bias_q8", "scap_sparse_fc_q4", "scap_dense_fc_q4", "scap_fold_bias_q4",
     "scap_grouped_workspace", "scap_sparse_fc_grouped", "scap_fc_host_workspace", "scap_sparse_fc_host", "scap_glu_workspace", "scap_glu_ffn", "scap_gelu_ffn_workspace",
     "scap_gelu_ffn", "scap_glu_static_capacity", "scap_glu_ffn_static", "scap_moe_workspace", "scap_moe_ffn",
-    "scap_fc_act_workspace", "scap_fc_act", "scap_kv4_page_bytes", "scap_kv4_append", "scap_kv4_read",
+    "scap_fc_act_workspace", "scap_fc_act", "scap_kv4_page_bytes", "scap_kv4_append", "scap_kv4_read", "scap_kv4_attend_workspace", "scap_kv4_attend",
 ]
 
 
@@ -55,6 +55,7 @@ def lib_path() -> str:
 
 _lib = None
 _call = None    # call(entry, arg, ...) -> status: the native helper, or ctypes where it is not built
+_call_real = None  # call_real(entry, x, arg, ...) -> status, for an entry point with one double: the native helper only
 _entry = {}     # name -> what `_call` takes as the entry point: its address, or the ctypes function
 
 
@@ -138,22 +139,26 @@ def lib():
     for n in ("scap_kv4_append", "scap_kv4_read"):
         getattr(L, n).argtypes = [vp, vp, i64, vp, i64, vp, i, i, vp]
         getattr(L, n).restype = i
-    global _call
+    L.scap_kv4_attend_workspace.argtypes = [i, i, i, i, i]
+    L.scap_kv4_attend_workspace.restype = sz
+    L.scap_kv4_attend.argtypes = [vp, vp, i64, vp, i64, vp, i, i, d, i, i, vp, sz, vp]
+    L.scap_kv4_attend.restype = i
+    global _call, _call_real
     try:
-        from ._scap_call import call
+        from ._scap_call import call, call_real
         _entry.update({n: C.cast(getattr(L, n), C.c_void_p).value for n in EXPORTS})
     except ImportError as e:
         warnings.warn("%s: calls go through ctypes, about 5 us slower each; `python -m paper_2412_07174_b200.build` builds the helper" % e)
-        call = _ctypes_call
+        call, call_real = _ctypes_call, None
         _entry.update({n: getattr(L, n) for n in EXPORTS})
-    _call = call
+    _call, _call_real = call, call_real
     _lib = L
     return L
 
 
 def _ctypes_call(entry, *args) -> int:
     """What the native helper does, by ctypes."""
-    return entry(*[_ptr(a) for a in args])
+    return entry(*[a if isinstance(a, C.c_double) else _ptr(a) for a in args])
 
 
 def _invoke(name: str, *args) -> None:
@@ -161,6 +166,15 @@ def _invoke(name: str, *args) -> None:
     if _lib is None:
         lib()
     code = _call(_entry[name], *args)
+    if code != 0:
+        raise ScapError(code, name)
+
+
+def _invoke_real(name: str, x: float, at: int, *args) -> None:
+    """The same for an entry point that has one double, `x`, before its argument number `at`."""
+    if _lib is None:
+        lib()
+    code = _call_real(_entry[name], x, *args) if _call is not _ctypes_call else _call(_entry[name], *args[:at], C.c_double(x), *args[at:])
     if code != 0:
         raise ScapError(code, name)
 
@@ -475,3 +489,26 @@ def scap_kv4_append(cache, k, v, row_start=None, stream=None) -> None:
 def scap_kv4_read(cache, k_out, v_out, row_start=None, stream=None) -> None:
     """The values that the cache holds for the last tokens of its sequences, addressed as in scap_kv4_append."""
     _kv4_rows("scap_kv4_read", cache, k_out, v_out, row_start, stream)
+
+
+def scap_kv4_attend_workspace(n_seqs: int, nq: int, q_heads: int, heads: int, head_dim: int) -> int:
+    return lib().scap_kv4_attend_workspace(int(n_seqs), int(nq), int(q_heads), int(heads), int(head_dim))
+
+
+def _queries(t, D: int, name: str) -> int:
+    """Elements between the tokens of [n_seqs, nq, heads, D], which may be a slice of a wider row."""
+    B, nq, heads, _ = t.shape
+    if t.stride(3) != 1 or (heads > 1 and t.stride(2) != D) or (B > 1 and nq > 1 and t.stride(0) != nq * t.stride(1)):
+        raise ValueError("%s must have contiguous heads, and evenly spaced tokens" % name)
+    return t.stride(1) if nq > 1 else (t.stride(0) if B > 1 else heads * D)
+
+
+def scap_kv4_attend(cache, q, out, scale: float, ws, window: int = 0, lse=None, stream=None) -> None:
+    """out[b, i, h]: attention of the last nq tokens of every sequence, q [n_seqs, nq, q_heads, head_dim], over its tokens in the cache."""
+    if q.dim() != 4 or q.shape[0] != cache.n_seqs or q.shape[3] != cache.head_dim or out.shape != q.shape or out.dtype is not q.dtype:
+        raise ValueError("q and out must be [%d, nq, q_heads, %d] of one dtype" % (cache.n_seqs, cache.head_dim))
+    if lse is not None and (lse.dtype is not torch.float32 or lse.shape != q.shape[:3] or not lse.is_contiguous()):
+        raise ValueError("lse must be contiguous float32 [n_seqs, nq, q_heads]")
+    p, n = _ws(ws)
+    _invoke_real("scap_kv4_attend", float(scale), 8, cache.address, q, _queries(q, cache.head_dim, "q"), out, _queries(out, cache.head_dim, "out"), lse, q.shape[1],
+                 q.shape[2], int(window), dtype_of(q), p, n, _stream(stream))
