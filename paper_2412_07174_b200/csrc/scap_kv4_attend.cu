@@ -1,17 +1,19 @@
 // Attention of new tokens over the 4-bit cache: out = softmax(scale q k^T + mask) v, one to sixteen new tokens per sequence.
 //
-// The rows of a key head (its query heads x the new tokens) are the M rows of mma.m16n8k16, up to 16 at a time; the cache is
-// dequantised by nothing but a mask: a code is an fp16 subnormal (see scap_kv4.cuh), and what belongs to a group of channels is
-// applied once per token:
-//   scores  s_t = ks_t (sum_c q_c code_tc - zero_t sum_c q_c)
-//   output  o_c = sum_t (p_t vs_t) code_tc - sum_t (p_t vs_t) zero_t, the second sum by one more MMA whose columns are the zero points.
+// The rows of a key head (its query heads x the new tokens) are the N columns of mma.m16n8k16, eight at a time (RN = 1 or 2 such groups), and
+// the codes its A operand: tokens are the M rows of the scores, channels those of the output.  The cache is dequantised by nothing but a
+// mask: a code is an fp16 subnormal (see scap_kv4.cuh), and what belongs to a group of channels is applied once per token:
+//   scores  s_t = ks_t (sum_c q_c code_tc - zero_t sum_c q_c), the second sum by one more MMA with the zero points as codes
+//   output  o_c = sum_t (p_t vs_t) code_tc - sum_t (p_t vs_t) zero_t, likewise.
 // p vs is rounded to fp16 (11 bits) once and used in both sums, so the rounding acts on the value v, not on its code part; the queries
 // are scaled by a power of two per row and are exact.  Scores, maxima, sums and accumulators are fp32.
+// (With the rows as the M rows of the MMA a head with eight or fewer of them pays for sixteen: twice the MMAs, accumulators and
+// exponentials; 131001 tokens, 8 key heads, 8 rows: 56 us.)
 //
 // What bounds it: the bytes of the cache, D/2 + 4 groups per token, head and side - if the instructions keep up: per tile of 32 tokens a
-// warp issues 64 MMAs (D = 128), 160 mask and shift instructions and about 150 for the softmax.
+// warp issues 36 MMAs (D = 128, RN = 1), 160 mask and shift instructions and about 100 for the softmax.
 //
-// Work is cut into equal parts, whatever the lengths: a unit is one tile of 32 tokens of one (sequence, 16 rows, head), all units are
+// Work is cut into equal parts, whatever the lengths: a unit is one tile of 32 tokens of one (sequence, 8 RN rows, head), all units are
 // numbered, and CTA i of C takes the units [U i / C, U (i + 1) / C).  Inside a CTA the tiles of an item go round the four warps, each
 // of which has its own ring of tiles, filled by cp.async.bulk (one copy per tile, 4.3 KB at D = 128), its own running maximum and sum, and no barrier with
 // the others until the item ends.  An item that lies in one CTA is finished there; the parts of one that is cut go to the
@@ -24,13 +26,16 @@ namespace scap {
 
 constexpr int AT_WARPS = 4;
 constexpr int AT_THREADS = AT_WARPS * 32;
-constexpr int AT_ROWS = 16;
 constexpr int AT_MIN_UNITS = 4;  // tiles per CTA at least
+constexpr int AT_UP = 133;       // a scale of exponent field e is below 2^(e - 126), a weight at most 2^8: their product below 2^15 as held
 
-template <int D>
-__host__ __device__ constexpr int at_resident() { return D == 256 ? 2 : 3; }
-template <int D, int G>
-__host__ __device__ constexpr int at_stages() { return D == 64 ? 6 : (D == 128 ? (G == 4 ? 3 : 4) : 3); }
+// CTAs per SM and tiles in a warp's ring, as registers and shared memory allow (RN groups of eight rows, G groups of channels).
+__host__ __device__ constexpr int at_resident(int D, int G, int RN) {
+    return D == 64 ? (RN == 1 ? 5 : 4) : (D == 128 ? (RN == 1 && G < 4 ? 4 : 3) : (RN == 1 ? 3 : 2));
+}
+__host__ __device__ constexpr int at_stages(int D, int G, int RN) {
+    return D == 64 ? 4 : (D == 128 ? (RN == 2 && G < 4 ? 4 : 3) : (RN == 1 ? 2 : 3));
+}
 
 struct AtArgs {
     KvCache c;
@@ -38,7 +43,7 @@ struct AtArgs {
     unsigned short *out;
     float *lse;
     long long ldq, ldo;   // elements between tokens
-    float *part;          // [2 C][16][D] weighted sums, then [2 C][16][2] maximum and sum
+    float *part;          // [2 C][8 RN][D] weighted sums, then [2 C][8 RN][2] reference and sum
     int nq, g, row_tiles, window;
     float scale;          // times log2 e
     int ctas;
@@ -59,23 +64,53 @@ __device__ __forceinline__ int at_tiles(const AtArgs &a, int b, int &first) {
     return (int)(((long long)len + KV_TILE - 1) / KV_TILE) - first;
 }
 
-// Sum over the block; every thread gets it.
-__device__ __forceinline__ long long at_block_sum(long long v, long long *s) {
-#pragma unroll
-    for (int o = 16; o > 0; o /= 2) v += __shfl_xor_sync(0xffffffffu, v, o);
-    __syncthreads();
-    if ((threadIdx.x & 31) == 0) s[threadIdx.x >> 5] = v;
-    __syncthreads();
-    v = 0;
-#pragma unroll
-    for (int w = 0; w < AT_WARPS; ++w) v += s[w];
-    return v;
+__device__ __forceinline__ long long at_cut(long long units, int i, int ctas) { return units * i / ctas; }
+__device__ __forceinline__ int at_cta_of(long long units, long long u, int ctas) { return (int)(((u + 1) * ctas - 1) / units); }
+__device__ __forceinline__ int at_ctas(long long units, int ctas) {
+    const long long n = (units + AT_MIN_UNITS - 1) / AT_MIN_UNITS;
+    return n < ctas ? (int)n : ctas;
 }
 
-// The sequence that unit u belongs to and the first unit of that sequence (the whole block takes part); per = items per sequence.
-__device__ __forceinline__ void at_find(const AtArgs &a, long long u, int per, long long *s, int &seq, long long &base) {
+// Number of tiles of all sequences and of those before `seq` (the whole block takes part).
+__device__ __forceinline__ void at_count(const AtArgs &a, int seq, long long *s, long long &all, long long &before) {
+    all = before = 0;
+    for (int b = threadIdx.x; b < a.c.n_seqs; b += AT_THREADS) {
+        int first;
+        const int n = at_tiles(a, b, first);
+        all += n;
+        if (b < seq) before += n;
+    }
+#pragma unroll
+    for (int o = 16; o > 0; o /= 2) {
+        all += __shfl_xor_sync(0xffffffffu, all, o);
+        before += __shfl_xor_sync(0xffffffffu, before, o);
+    }
+    __syncthreads();
+    if ((threadIdx.x & 31) == 0) {
+        s[threadIdx.x >> 5] = all;
+        s[AT_WARPS + (threadIdx.x >> 5)] = before;
+    }
+    __syncthreads();
+    all = before = 0;
+#pragma unroll
+    for (int w = 0; w < AT_WARPS; ++w) {
+        all += s[w];
+        before += s[AT_WARPS + w];
+    }
+}
+
+// This CTA's units [u, u1), the sequence that u belongs to and the first unit of that sequence (the whole block takes part); per = items
+// per sequence.  False: there is nothing for this CTA.
+__device__ __forceinline__ bool at_begin(const AtArgs &a, int per, long long *s, long long &u, long long &u1, int &seq, long long &base) {
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-    long long before = 0;
+    long long units = 0, before = 0;
+    const bool one = a.c.n_seqs <= AT_THREADS;  // one look at the lengths gives the sum and the place
+    if (!one) {
+        long long all;
+        at_count(a, 0, s, all, before);
+        units = all * per;
+        __syncthreads();
+    }
     for (int b0 = 0; b0 < a.c.n_seqs; b0 += AT_THREADS) {
         const int b = b0 + (int)threadIdx.x;
         int first;
@@ -86,14 +121,19 @@ __device__ __forceinline__ void at_find(const AtArgs &a, long long u, int per, l
             const long long up = __shfl_up_sync(0xffffffffu, incl, o);
             if (lane >= o) incl += up;
         }
-        __syncthreads();
         if (lane == 31) s[warp] = incl;
         __syncthreads();
         long long off = before, all = before;
+#pragma unroll
         for (int w = 0; w < AT_WARPS; ++w) {
             if (w < warp) off += s[w];
             all += s[w];
         }
+        if (one) units = all;
+        const int ctas = at_ctas(units, a.ctas);
+        if ((int)blockIdx.x >= ctas) return false;
+        u = at_cut(units, blockIdx.x, ctas);
+        u1 = at_cut(units, blockIdx.x + 1, ctas);
         if (n > 0 && off + incl - n <= u && u < off + incl) {
             s[AT_WARPS] = b;
             s[AT_WARPS + 1] = off + incl - n;
@@ -104,19 +144,18 @@ __device__ __forceinline__ void at_find(const AtArgs &a, long long u, int per, l
     }
     seq = (int)s[AT_WARPS];
     base = s[AT_WARPS + 1];
-    __syncthreads();
+    return true;
 }
 
-__device__ __forceinline__ long long at_cut(long long units, int i, int ctas) { return units * i / ctas; }
-__device__ __forceinline__ int at_cta_of(long long units, long long u, int ctas) { return (int)(((u + 1) * ctas - 1) / units); }
-__device__ __forceinline__ int at_ctas(long long units, int ctas) {
-    const long long n = (units + AT_MIN_UNITS - 1) / AT_MIN_UNITS;
-    return n < ctas ? (int)n : ctas;
+__device__ __forceinline__ void at_mma(float (&c)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1) {
+    asm("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
+        : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3]) : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
 }
-
-__device__ __forceinline__ void at_mma(float (&c)[4], const uint32_t (&a)[4], uint32_t b0, uint32_t b1) {
-    asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
-                 : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3]) : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
+// Transposes an 8 x 8 matrix of 16-bit elements, two neighbours of a row per lane.
+__device__ __forceinline__ uint32_t at_trans(uint32_t v) {
+    uint32_t r;
+    asm("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;" : "=r"(r) : "r"(v));
+    return r;
 }
 __device__ __forceinline__ uint32_t at_pack(float lo, float hi) {
     uint32_t r;
@@ -135,18 +174,20 @@ __device__ __forceinline__ void at_store(unsigned short *p, float v, bool bf16) 
 // 2^e for -126 <= e <= 127
 __device__ __forceinline__ float at_pow2(int e) { return __int_as_float((e + 127) << 23); }
 
-template <int D, int G>
-__global__ void __launch_bounds__(AT_THREADS, at_resident<D>()) kv4_attend_kernel(const AtArgs a) {
+template <int D, int G, int RN>
+__global__ void __launch_bounds__(AT_THREADS, at_resident(D, G, RN)) kv4_attend_kernel(const AtArgs a) {
     constexpr int W = D / 32;            // words of a K row per lane
     constexpr int TILE = kv_tile_bytes(D, G);
-    constexpr int ST = at_stages<D, G>();
-    constexpr int NT = D / 8;            // blocks of eight channels
+    constexpr int ST = at_stages(D, G, RN);
+    constexpr int MT = D / 16;           // blocks of sixteen channels
+    constexpr int ROWS = 8 * RN;
+    constexpr int PITCH = D + 4;         // of a row of the join
     constexpr float LN2 = 0.69314718055994531f;
-    static_assert(ST * TILE >= AT_ROWS * D * 4, "a warp's part of the join goes where its ring was");
+    static_assert(ST * TILE >= ROWS * PITCH * 4, "a warp's part of the join goes where its ring was");
     extern __shared__ __align__(128) unsigned char at_raw[];
     __shared__ unsigned long long s_full[AT_WARPS][ST];
-    __shared__ long long s_sum[AT_WARPS + 2];
-    __shared__ float s_m[AT_WARPS][AT_ROWS], s_l[AT_WARPS][AT_ROWS];
+    __shared__ long long s_sum[2 * AT_WARPS];
+    __shared__ float s_m[AT_WARPS][ROWS], s_l[AT_WARPS][ROWS];
 
     const int tid = threadIdx.x, warp = __shfl_sync(0xffffffffu, tid >> 5, 0), lane = tid & 31, qg = lane >> 2, qt = lane & 3;
     unsigned char *ring = at_raw + warp * ST * TILE;
@@ -154,408 +195,437 @@ __global__ void __launch_bounds__(AT_THREADS, at_resident<D>()) kv4_attend_kerne
         for (int i = 0; i < ST; ++i) mbarrier_init(smem_addr(&s_full[warp][i]), 1);
     __syncthreads();
     griddep_wait();
-    griddep_launch_dependents();
+    griddep_launch_dependents();  // (after the wait: the second kernel may rely on all work before this one)
 
     const int per = a.c.heads * a.row_tiles;
-    long long mine = 0;
-    for (int b = tid; b < a.c.n_seqs; b += AT_THREADS) {
-        int first;
-        mine += at_tiles(a, b, first);
-    }
-    const long long units = at_block_sum(mine, s_sum) * per;
-    const int ctas = at_ctas(units, a.ctas);
-    if ((int)blockIdx.x < ctas) {
-        long long u = at_cut(units, blockIdx.x, ctas);
-        const long long u1 = at_cut(units, blockIdx.x + 1, ctas);
-        int seq;
-        long long base;
-        at_find(a, u, per, s_sum, seq, base);
-        int slot = 0, phase = 0;  // of this warp's ring, over all items
-        bool dead = false;        // a wait of this warp ran out
+    long long u, u1, base;
+    int seq;
+    if (!at_begin(a, per, s_sum, u, u1, seq, base)) return;
+    int slot = 0, phase = 0;  // of this warp's ring, over all items
+    bool dead = false;        // a wait of this warp ran out
 
-        while (u < u1) {
-            int first_tile;
-            const int tiles = at_tiles(a, seq, first_tile);
-            if (tiles == 0) { ++seq; continue; }  // (an empty sequence has no units; its rows are the second kernel's)
-            const int item = (int)((u - base) / tiles), t0 = (int)(u - base - (long long)item * tiles);
-            const int t1 = (int)min((long long)tiles, t0 + (u1 - u));
-            const int rt = item / a.c.heads, h = item - rt * a.c.heads;
-            const int len = __ldcg(a.c.lens + seq), rows = min(AT_ROWS, a.nq * a.g - rt * AT_ROWS);
-            const int count = !dead && t1 - t0 - warp > 0 ? (t1 - t0 - warp + AT_WARPS - 1) / AT_WARPS : 0;  // tiles t0 + warp, + 4, ... are this warp's
+    while (u < u1) {
+        int first_tile;
+        const int tiles = at_tiles(a, seq, first_tile);
+        if (tiles == 0) { ++seq; continue; }  // (an empty sequence has no units; its rows are the second kernel's)
+        const int item = (int)((u - base) / tiles), t0 = (int)(u - base - (long long)item * tiles);
+        const int t1 = (int)min((long long)tiles, t0 + (u1 - u));
+        const int rt = item / a.c.heads, h = item - rt * a.c.heads;
+        const int len = __ldcg(a.c.lens + seq), rows = min(ROWS, a.nq * a.g - rt * ROWS);
+        const int count = !dead && t1 - t0 - warp > 0 ? (t1 - t0 - warp + AT_WARPS - 1) / AT_WARPS : 0;  // tiles t0 + warp, + 4, ... are this warp's
 
-            // ---- pages of the next 32 tiles of this warp, one per lane, and the first copies
-            auto pos_of = [&](int i) { return (first_tile + t0 + warp + AT_WARPS * i) * KV_TILE; };
-            int pages = lane < count ? kv_page(a.c, seq, pos_of(lane)) : -1;
-            int next_pages = 32 + lane < count ? kv_page(a.c, seq, pos_of(32 + lane)) : -1;
-            auto ask = [&](int i, int page, int st) {
-                if (page >= 0 && lane == 0) {
-                    const uint32_t bar = smem_addr(&s_full[warp][st]);
-                    const unsigned char *src = kv_tile(a.c, page, h, pos_of(i), TILE);
+        // ---- addresses of the next 32 tiles of this warp, one per lane (0: no page), and the first copies
+        auto pos_of = [&](int i) { return (first_tile + t0 + warp + AT_WARPS * i) * KV_TILE; };
+        auto where = [&](int i) -> unsigned long long {
+            const int page = i < count ? kv_page(a.c, seq, pos_of(i)) : -1;
+            return page < 0 ? 0ull : (unsigned long long)kv_tile(a.c, page, h, pos_of(i), TILE);
+        };
+        unsigned long long at_now = where(lane), at_next = where(32 + lane);
+        auto ask = [&](unsigned long long src, int st) {
+            if (lane == 0) {
+                const uint32_t bar = smem_addr(&s_full[warp][st]);
+                if (src) {
                     mbarrier_arrive_expect(bar, TILE);
                     asm volatile("cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];" ::"r"(smem_addr(ring + st * TILE)), "l"(src), "r"(TILE), "r"(bar)
                                  : "memory");
-                } else if (lane == 0) {
-                    asm volatile("mbarrier.arrive.shared::cta.b64 _, [%0];" ::"r"(smem_addr(&s_full[warp][st])) : "memory");  // no page: the tile is empty
-                }
-            };
-            {
-                int st = slot;
-                for (int i = 0; i < ST && i < count; ++i) {
-                    ask(i, __shfl_sync(0xffffffffu, pages, i), st);
-                    if (++st == ST) st = 0;
+                } else {
+                    asm volatile("mbarrier.arrive.shared::cta.b64 _, [%0];" ::"r"(bar) : "memory");  // the tile is empty
                 }
             }
+        };
+        {
+            int st = slot;
+            for (int i = 0; i < ST && i < count; ++i) {
+                ask(__shfl_sync(0xffffffffu, at_now, i), st);
+                if (++st == ST) st = 0;
+            }
+        }
 
-            // ---- queries: rows qg and qg + 8 as A operands, scaled to just below 2^15 by a power of two; channels 32 j + 8 qt + i, the
-            // even and odd nibbles of a code word in the two k halves of an MMA, the odd ones 16 times smaller as their codes are larger
-            uint32_t qa[2 * W][4];
-            float f[2], qz[2][G];
+        // ---- queries: rows 8 rn + qg as B operands, scaled to just below 2^12 by a power of two; channels 32 j + 8 qt + i, the
+        // even and odd nibbles of a code word in the two k halves of an MMA, the odd ones 16 times smaller as their codes are larger.
+        // zq: minus the sum of a group, in two fp16 parts, against the zero points (times 2^6, as zero 2^-18 is the subnormal used)
+        uint32_t qb[RN][2 * W][2], zq[RN][G];
+        float f[RN][2];  // what turns an accumulator of row 8 rn + 2 qt + k into a score in units of log 2
 #pragma unroll
-            for (int r = 0; r < 2; ++r) {
-                const int row = qg + 8 * r;
-                uint4 raw[W];
-                const int in = rt * AT_ROWS + row, tok = in / a.g, hd = in - tok * a.g;
-                const unsigned short *src = a.q + ((long long)seq * a.nq + tok) * a.ldq + (long long)(h * a.g + hd) * D + 8 * qt;
+        for (int rn = 0; rn < RN; ++rn) {
+            const int row = 8 * rn + qg;
+            uint4 raw[W];
+            const int in = rt * ROWS + row, tok = in / a.g, hd = in - tok * a.g;
+            const unsigned short *src = a.q + ((long long)seq * a.nq + tok) * a.ldq + (long long)(h * a.g + hd) * D + 8 * qt;
 #pragma unroll
-                for (int j = 0; j < W; ++j) raw[j] = ld_act16_if(src + 32 * j, row < rows);
-                float v[W][8], top = 0.0f;
+            for (int j = 0; j < W; ++j) raw[j] = ld_act16_if(src + 32 * j, row < rows);
+            float v[W][8], top = 0.0f;
 #pragma unroll
-                for (int j = 0; j < W; ++j)
+            for (int j = 0; j < W; ++j)
 #pragma unroll
-                    for (int i = 0; i < 8; ++i) {
-                        const uint32_t w = (&raw[j].x)[i >> 1];
-                        v[j][i] = at_widen((unsigned short)(i & 1 ? w >> 16 : w), a.bf16);
-                        top = fmaxf(top, fabsf(v[j][i]));
-                    }
-                top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 1));
-                top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 2));
-                int e = top > 0.0f ? 14 - ((__float_as_int(top) >> 23) - 127) : 0;
-                e = e > 100 ? 100 : (e < -100 ? -100 : e);
-                const float up = at_pow2(e);
-                float sum[G];
-#pragma unroll
-                for (int n = 0; n < G; ++n) sum[n] = 0.0f;
-#pragma unroll
-                for (int j = 0; j < W; ++j) {
-#pragma unroll
-                    for (int i = 0; i < 8; ++i) sum[j * G / W] += v[j][i];
-#pragma unroll
-                    for (int hi = 0; hi < 2; ++hi) {
-                        qa[2 * j + hi][r] = at_pack(v[j][2 * hi] * up, v[j][2 * hi + 4] * up);
-                        qa[2 * j + hi][2 + r] = at_pack(v[j][2 * hi + 1] * (up * 0.0625f), v[j][2 * hi + 5] * (up * 0.0625f));
-                    }
+                for (int i = 0; i < 8; ++i) {
+                    const uint32_t w = (&raw[j].x)[i >> 1];
+                    v[j][i] = at_widen((unsigned short)(i & 1 ? w >> 16 : w), a.bf16);
+                    top = fmaxf(top, fabsf(v[j][i]));
                 }
-                f[r] = at_pow2(24 - e) * a.scale;
+            top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 1));
+            top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 2));
+            int e = top > 0.0f ? 11 - ((__float_as_int(top) >> 23) - 127) : 0;
+            e = e > 100 ? 100 : (e < -100 ? -100 : e);
+            const float up = at_pow2(e);
+            float sum[G];
 #pragma unroll
-                for (int n = 0; n < G; ++n) {
-                    sum[n] += __shfl_xor_sync(0xffffffffu, sum[n], 1);
-                    sum[n] += __shfl_xor_sync(0xffffffffu, sum[n], 2);
-                    qz[r][n] = sum[n] * a.scale;
+            for (int n = 0; n < G; ++n) sum[n] = 0.0f;
+#pragma unroll
+            for (int j = 0; j < W; ++j) {
+#pragma unroll
+                for (int i = 0; i < 8; ++i) sum[j * G / W] += v[j][i];
+#pragma unroll
+                for (int hi = 0; hi < 2; ++hi) {
+                    qb[rn][2 * j + hi][0] = at_pack(v[j][2 * hi] * up, v[j][2 * hi + 4] * up);
+                    qb[rn][2 * j + hi][1] = at_pack(v[j][2 * hi + 1] * (up * 0.0625f), v[j][2 * hi + 5] * (up * 0.0625f));
                 }
             }
-            // keys that a row sees: lo[r] .. hi[r]
-            int hi[2], lo[2];
 #pragma unroll
-            for (int r = 0; r < 2; ++r) {
-                const int in = min(rt * AT_ROWS + qg + 8 * r, a.nq * a.g - 1), at = len - a.nq + in / a.g;
-                hi[r] = at;
-                lo[r] = a.window > 0 && at >= a.window ? at - a.window + 1 : 0;
+            for (int n = 0; n < G; ++n) {
+                sum[n] += __shfl_xor_sync(0xffffffffu, sum[n], 1);
+                sum[n] += __shfl_xor_sync(0xffffffffu, sum[n], 2);
+                const float x = -sum[n] * up * 0.015625f, x_hi = __half2float(__float2half_rn(x));
+                zq[rn][n] = at_pack(x_hi, x - x_hi);
             }
-            const int hi_all = len - a.nq, lo_all = a.window > 0 && len > a.window ? len - a.window : 0;  // what every row sees
+            const float mine = at_pow2(24 - e) * a.scale;
+#pragma unroll
+            for (int k = 0; k < 2; ++k) f[rn][k] = __shfl_sync(0xffffffffu, mine, (2 * qt + k) * 4);
+        }
+        // keys that a row sees: lo .. hi
+        int hi[RN][2], lo[RN][2];
+#pragma unroll
+        for (int rn = 0; rn < RN; ++rn)
+#pragma unroll
+            for (int k = 0; k < 2; ++k) {
+                const int in = min(rt * ROWS + 8 * rn + 2 * qt + k, a.nq * a.g - 1), at = len - a.nq + in / a.g;
+                hi[rn][k] = at;
+                lo[rn][k] = a.window > 0 && at >= a.window ? at - a.window + 1 : 0;
+            }
+        const int hi_all = len - a.nq, lo_all = a.window > 0 && len > a.window ? len - a.window : 0;  // what every row sees
 
-            float o[NT][4], z[G][4], m[2] = {-INFINITY, -INFINITY}, l[2] = {0.0f, 0.0f};
-            int top_e = 1;  // exponent field of the largest scale of values so far: p vs is held as p vs 2^(14 + 127 - top_e)
+        float o[RN][MT][4], z[RN][G][4], m[RN][2], l[RN][2];
+        int top_e = AT_UP - 126;  // exponent field of the largest scale of values so far (at least this): p vs is held as p vs 2^(AT_UP - top_e)
 #pragma unroll
-            for (int n = 0; n < NT; ++n)
+        for (int rn = 0; rn < RN; ++rn) {
 #pragma unroll
-                for (int i = 0; i < 4; ++i) o[n][i] = 0.0f;
+            for (int n = 0; n < MT; ++n)
+#pragma unroll
+                for (int i = 0; i < 4; ++i) o[rn][n][i] = 0.0f;
 #pragma unroll
             for (int n = 0; n < G; ++n)
 #pragma unroll
-                for (int i = 0; i < 4; ++i) z[n][i] = 0.0f;
+                for (int i = 0; i < 4; ++i) z[rn][n][i] = 0.0f;
+            m[rn][0] = m[rn][1] = -INFINITY;
+            l[rn][0] = l[rn][1] = 0.0f;
+        }
 
-            for (int i = 0; i < count; ++i) {
-                const uint32_t bar = smem_addr(&s_full[warp][slot]);
-                const int page = __shfl_sync(0xffffffffu, pages, i & 31);
-                bool landed = false;
-                for (uint32_t n = 0; n < a.limit && !landed; ++n) landed = mbarrier_try_wait(bar, phase);
-                if (!__all_sync(0xffffffffu, landed)) {
-                    // It ran out: no further work for this warp, but the copies under way still write here - wait for them, with a limit.
-                    if (lane == 0 && a.status) atomicCAS(a.status, 0, 41);
-                    dead = true;
-                    int st = slot, ph = phase;
-                    for (int k = i; k < i + ST && k < count; ++k) {
-                        for (uint32_t n = 0; n < TRIES / 16 && !mbarrier_try_wait(smem_addr(&s_full[warp][st]), ph); ++n) {}
-                        if (++st == ST) { st = 0; ph ^= 1; }
-                    }
-                    __syncwarp();
-                    break;
+        const uint32_t zmask = qt == 0 ? 15u : 0u;
+        for (int i = 0; i < count; ++i) {
+            const uint32_t bar = smem_addr(&s_full[warp][slot]);
+            bool landed = false;
+            for (uint32_t n = 0; n < a.limit && !landed; ++n) landed = mbarrier_try_wait(bar, phase);
+            if (!__all_sync(0xffffffffu, landed)) {
+                // It ran out: no further work for this warp, but the copies under way still write here - wait for them, with a limit.
+                if (lane == 0 && a.status) atomicCAS(a.status, 0, 41);
+                dead = true;
+                int st = slot, ph = phase;
+                for (int k = i; k < i + ST && k < count; ++k) {
+                    for (uint32_t n = 0; n < TRIES / 16 && !mbarrier_try_wait(smem_addr(&s_full[warp][st]), ph); ++n) {}
+                    if (++st == ST) { st = 0; ph ^= 1; }
                 }
-                const unsigned char *tile = ring + slot * TILE;
-                const int pos = pos_of(i);
-                if (page >= 0) {
-                    // ---- scores
-                    float s[4][4];
+                __syncwarp();
+                break;
+            }
+            const unsigned char *tile = ring + slot * TILE;
+            const int pos = pos_of(i);
+            if (__shfl_sync(0xffffffffu, at_now, i & 31) != 0) {
+                // keys that not every row sees: tokens behind the last, before a window, or newer than the row's own
+                const bool edge = pos + KV_TILE - 1 > hi_all || pos < lo_all;
+                // ---- scores: s[rn][j][k] is row 8 rn + 2 qt + k at token 8 j + qg.  The four blocks of eight tokens are two A operands.
+                float s[RN][4][2];
+                uint32_t kw[G][4];
+#pragma unroll
+                for (int n = 0; n < G; ++n)
+#pragma unroll
+                    for (int j = 0; j < 4; ++j) kw[n][j] = *reinterpret_cast<const uint32_t *>(tile + kv_k_words(D) + (n * KV_TILE + 8 * j + qg) * 4);
+                {
+                    float acc[2][RN][G][4];
+                    uint32_t w[4][W];
 #pragma unroll
                     for (int j = 0; j < 4; ++j) {
-                        float acc[G][4];
-#pragma unroll
-                        for (int n = 0; n < G; ++n)
-#pragma unroll
-                            for (int k = 0; k < 4; ++k) acc[n][k] = 0.0f;
                         const unsigned char *krow = tile + (8 * j + qg) * (D / 2) + qt * (D / 8);
-                        uint32_t w[W];
-                        if constexpr (W == 2) *reinterpret_cast<uint2 *>(w) = *reinterpret_cast<const uint2 *>(krow);
+                        if constexpr (W == 2) *reinterpret_cast<uint2 *>(w[j]) = *reinterpret_cast<const uint2 *>(krow);
                         else
 #pragma unroll
-                            for (int k = 0; k < W / 4; ++k) *reinterpret_cast<uint4 *>(w + 4 * k) = *reinterpret_cast<const uint4 *>(krow + 16 * k);
+                            for (int k = 0; k < W / 4; ++k) *reinterpret_cast<uint4 *>(w[j] + 4 * k) = *reinterpret_cast<const uint4 *>(krow + 16 * k);
+                    }
 #pragma unroll
-                        for (int k = 0; k < W; ++k) {
-                            at_mma(acc[k * G / W], qa[2 * k], w[k] & 0x000f000fu, w[k] & 0x00f000f0u);
-                            at_mma(acc[k * G / W], qa[2 * k + 1], (w[k] >> 8) & 0x000f000fu, (w[k] >> 8) & 0x00f000f0u);
-                        }
+                    for (int n = 0; n < G; ++n)
 #pragma unroll
-                        for (int k = 0; k < 4; ++k) s[j][k] = 0.0f;
+                        for (int mt = 0; mt < 2; ++mt) {
+                            const uint32_t z0 = (kw[n][2 * mt] & zmask) * 0x00400040u, z1 = (kw[n][2 * mt + 1] & zmask) * 0x00400040u;
 #pragma unroll
-                        for (int n = 0; n < G; ++n) {
-                            const uint2 kw = *reinterpret_cast<const uint2 *>(tile + kv_k_words(D) + (n * KV_TILE + 8 * j + 2 * qt) * 4);
-                            const float k0 = __uint_as_float(kw.x & ~15u), k1 = __uint_as_float(kw.y & ~15u);
-                            const float z0 = (float)(kw.x & 15u), z1 = (float)(kw.y & 15u);
+                            for (int rn = 0; rn < RN; ++rn) {
 #pragma unroll
-                            for (int r = 0; r < 2; ++r) {
-                                s[j][2 * r] += k0 * (acc[n][2 * r] * f[r] - z0 * qz[r][n]);
-                                s[j][2 * r + 1] += k1 * (acc[n][2 * r + 1] * f[r] - z1 * qz[r][n]);
+                                for (int k = 0; k < 4; ++k) acc[mt][rn][n][k] = 0.0f;
+                                at_mma(acc[mt][rn][n], z0, z1, 0u, 0u, zq[rn][n], 0u);
                             }
                         }
-                    }
-                    // ---- keys that not every row sees: tokens behind the last, before a window, or newer than the row's own
-                    const bool edge = pos + KV_TILE - 1 > hi_all || pos < lo_all;
-                    if (edge) {
 #pragma unroll
-                        for (int j = 0; j < 4; ++j)
+                    for (int k = 0; k < W; ++k)
 #pragma unroll
-                            for (int k = 0; k < 4; ++k) {
-                                const int at = pos + 8 * j + 2 * qt + (k & 1), r = k >> 1;
-                                if (at > hi[r] || at < lo[r]) s[j][k] = -INFINITY;
+                        for (int hi8 = 0; hi8 < 2; ++hi8)
+#pragma unroll
+                            for (int mt = 0; mt < 2; ++mt) {
+                                const uint32_t x = w[2 * mt][k] >> (8 * hi8), y = w[2 * mt + 1][k] >> (8 * hi8);
+                                const uint32_t a0 = x & 0x000f000fu, a1 = y & 0x000f000fu, a2 = x & 0x00f000f0u, a3 = y & 0x00f000f0u;
+#pragma unroll
+                                for (int rn = 0; rn < RN; ++rn) at_mma(acc[mt][rn][k * G / W], a0, a1, a2, a3, qb[rn][2 * k + hi8][0], qb[rn][2 * k + hi8][1]);
                             }
-                    }
-                    // ---- running maximum and sum
-                    float scale_o[2];
-                    bool same = true;
-#pragma unroll
-                    for (int r = 0; r < 2; ++r) {
-                        float t = m[r];
-#pragma unroll
-                        for (int j = 0; j < 4; ++j) t = fmaxf(t, fmaxf(s[j][2 * r], s[j][2 * r + 1]));
-                        t = fmaxf(t, __shfl_xor_sync(0xffffffffu, t, 1));
-                        t = fmaxf(t, __shfl_xor_sync(0xffffffffu, t, 2));
-                        const float ref = t == -INFINITY ? 0.0f : t;  // nothing seen so far: all weights are 0
-                        scale_o[r] = at_ex2(m[r] - ref);
-                        same = same && t == m[r];
-                        m[r] = t;
-                        l[r] *= scale_o[r];
-#pragma unroll
-                        for (int j = 0; j < 4; ++j)
-#pragma unroll
-                            for (int k = 0; k < 2; ++k) {
-                                s[j][2 * r + k] = at_ex2(s[j][2 * r + k] - ref);
-                                l[r] += s[j][2 * r + k];
-                            }
-                    }
-                    // ---- scales of the values; tokens behind the last one have none, whatever lies there
-                    uint2 vw[4][G];
-                    uint32_t big = 0;
 #pragma unroll
                     for (int j = 0; j < 4; ++j)
 #pragma unroll
                         for (int n = 0; n < G; ++n) {
-                            vw[j][n] = *reinterpret_cast<const uint2 *>(tile + kv_v_words(D, G) + (n * KV_TILE + 8 * j + 2 * qt) * 4);
-                            if (edge) {
-                                const int at = pos + 8 * j + 2 * qt;
-                                if (at >= len || at <= lo_all - a.nq) vw[j][n].x = 0;
-                                if (at + 1 >= len || at + 1 <= lo_all - a.nq) vw[j][n].y = 0;
-                            }
-                            big = max(big, vw[j][n].x < 0x7f800000u ? vw[j][n].x : 0u);
-                            big = max(big, vw[j][n].y < 0x7f800000u ? vw[j][n].y : 0u);
+                            const float ks = __uint_as_float(kw[n][j] & ~15u);
+#pragma unroll
+                            for (int rn = 0; rn < RN; ++rn)
+#pragma unroll
+                                for (int k = 0; k < 2; ++k) {
+                                    const float t = (ks * f[rn][k]) * acc[j >> 1][rn][n][2 * (j & 1) + k];
+                                    s[rn][j][k] = n == 0 ? t : s[rn][j][k] + t;
+                                }
                         }
-                    const int e = (int)(__reduce_max_sync(0xffffffffu, big) >> 23);
-                    if (e > top_e) {
-                        const int d = top_e - e < -126 ? -126 : top_e - e;
-                        const float down = at_pow2(d);
-                        scale_o[0] *= down;
-                        scale_o[1] *= down;
-                        same = false;
-                        top_e = e;
+                }
+                if (edge) {
+#pragma unroll
+                    for (int j = 0; j < 4; ++j)
+#pragma unroll
+                        for (int rn = 0; rn < RN; ++rn)
+#pragma unroll
+                            for (int k = 0; k < 2; ++k) {
+                                const int at = pos + 8 * j + qg;
+                                if (at > hi[rn][k] || at < lo[rn][k]) s[rn][j][k] = -INFINITY;
+                            }
+                }
+                // ---- largest scale of the values, a token per lane; tokens that no row sees have none, whatever lies there
+                uint32_t big = 0;
+#pragma unroll
+                for (int n = 0; n < G; ++n) {
+                    uint32_t w = *reinterpret_cast<const uint32_t *>(tile + kv_v_words(D, G) + (n * KV_TILE + lane) * 4);
+                    if (edge && (pos + lane >= len || pos + lane <= lo_all - a.nq)) w = 0;
+                    big = max(big, w < 0x7f800000u ? w : 0u);
+                }
+                const int e = (int)(__reduce_max_sync(0xffffffffu, big) >> 23);
+                // ---- reference of the weights: the largest score, but left as it is while weights stay below 2^8, so that the
+                // accumulators are rarely rescaled
+                float t[RN][2];
+                bool keep = e <= top_e;
+#pragma unroll
+                for (int rn = 0; rn < RN; ++rn)
+#pragma unroll
+                    for (int k = 0; k < 2; ++k) {
+                        float x = fmaxf(fmaxf(s[rn][0][k], s[rn][1][k]), fmaxf(s[rn][2][k], s[rn][3][k]));
+                        x = fmaxf(x, __shfl_xor_sync(0xffffffffu, x, 4));
+                        x = fmaxf(x, __shfl_xor_sync(0xffffffffu, x, 8));
+                        x = fmaxf(x, __shfl_xor_sync(0xffffffffu, x, 16));
+                        t[rn][k] = x;
+                        keep = keep && !(x > m[rn][k] + 8.0f);
                     }
-                    if (!__all_sync(0xffffffffu, same)) {
+                if (!__all_sync(0xffffffffu, keep)) {
+                    const float by = e > top_e ? at_pow2(top_e - e < -126 ? -126 : top_e - e) : 1.0f;
+                    top_e = max(top_e, e);
 #pragma unroll
-                        for (int n = 0; n < NT; ++n)
+                    for (int rn = 0; rn < RN; ++rn) {
+                        float down[2];
 #pragma unroll
-                            for (int k = 0; k < 4; ++k) o[n][k] *= scale_o[k >> 1];
+                        for (int k = 0; k < 2; ++k) {
+                            const float ref = fmaxf(m[rn][k], t[rn][k]);
+                            down[k] = ref == -INFINITY ? 1.0f : at_ex2(m[rn][k] - ref);
+                            l[rn][k] *= down[k];
+                            m[rn][k] = ref;
+                            down[k] *= by;
+                        }
+#pragma unroll
+                        for (int n = 0; n < MT; ++n)
+#pragma unroll
+                            for (int k = 0; k < 4; ++k) o[rn][n][k] *= down[k & 1];
 #pragma unroll
                         for (int n = 0; n < G; ++n)
 #pragma unroll
-                            for (int k = 0; k < 4; ++k) z[n][k] *= scale_o[k >> 1];
+                            for (int k = 0; k < 4; ++k) z[rn][n][k] *= down[k & 1];
                     }
-                    // ---- weighted values.  2^(14 + 127 - top_e) in two factors: the exponent may lie anywhere
-                    const int es = 141 - top_e, e1 = es / 2, e2 = es - e1;
-                    const float up1 = at_pow2(e1), up2 = at_pow2(e2);
+                }
 #pragma unroll
-                    for (int n = 0; n < G; ++n) {
-                        uint32_t pa[2][4];
+                for (int rn = 0; rn < RN; ++rn)
+#pragma unroll
+                    for (int k = 0; k < 2; ++k) {
+                        const float ref = m[rn][k] == -INFINITY ? 0.0f : m[rn][k];  // nothing seen so far: all weights are 0
+#pragma unroll
+                        for (int j = 0; j < 4; ++j) {
+                            s[rn][j][k] = at_ex2(s[rn][j][k] - ref);
+                            l[rn][k] += s[rn][j][k];
+                        }
+                    }
+                // ---- weighted values: p vs as B operands (a block of eight tokens x eight rows is transposed in registers)
+                const float up = at_pow2(AT_UP - top_e), up16 = up * 0.0625f;
+#pragma unroll
+                for (int n = 0; n < G; ++n) {
+                    uint32_t pb[RN][4];
+#pragma unroll
+                    for (int j = 0; j < 4; ++j) {
+                        const float vs = __uint_as_float(*reinterpret_cast<const uint32_t *>(tile + kv_v_words(D, G) + (n * KV_TILE + 8 * j + qg) * 4) & ~15u) * (j & 1 ? up16 : up);
+#pragma unroll
+                        for (int rn = 0; rn < RN; ++rn) {
+                            float x0 = s[rn][j][0] * vs, x1 = s[rn][j][1] * vs;
+                            if (edge) {  // a row does not see what another one does: not even a NaN
+                                const int at = pos + 8 * j + qg;
+                                if (at > hi[rn][0] || at < lo[rn][0]) x0 = 0.0f;
+                                if (at > hi[rn][1] || at < lo[rn][1]) x1 = 0.0f;
+                            }
+                            pb[rn][j] = at_trans(at_pack(x0, x1));
+                        }
+                    }
+#pragma unroll
+                    for (int ks = 0; ks < 2; ++ks) {
+                        const uint2 w0 = *reinterpret_cast<const uint2 *>(tile + kv_v_words(D, G) + (n * KV_TILE + 16 * ks + 2 * qt) * 4);
+                        const uint2 w1 = *reinterpret_cast<const uint2 *>(tile + kv_v_words(D, G) + (n * KV_TILE + 16 * ks + 8 + 2 * qt) * 4);
+                        const uint32_t z0 = __byte_perm(w0.x, w0.y, 0x5410) & 0x000f000fu, z1 = (__byte_perm(w1.x, w1.y, 0x5410) & 0x000f000fu) << 4;
+#pragma unroll
+                        for (int rn = 0; rn < RN; ++rn) at_mma(z[rn][n], z0, z0, z1, z1, pb[rn][2 * ks], pb[rn][2 * ks + 1]);
+                    }
+#pragma unroll
+                    for (int b4 = n * W / G; b4 < (n + 1) * W / G; ++b4) {
+                        const uint4 w4 = *reinterpret_cast<const uint4 *>(tile + kv_v_codes(D) + (b4 * 32 + lane) * 16);
+                        const uint32_t w[4] = {w4.x, w4.y, w4.z, w4.w};
 #pragma unroll
                         for (int ks = 0; ks < 2; ++ks)
 #pragma unroll
                             for (int half = 0; half < 2; ++half) {
-                                const int j = 2 * ks + half;
-                                const float down = half ? 0.0625f : 1.0f;
-                                const float v0 = __uint_as_float(vw[j][n].x & ~15u) * up1 * (up2 * down), v1 = __uint_as_float(vw[j][n].y & ~15u) * up1 * (up2 * down);
+                                const uint32_t x = w[2 * half] >> (8 * ks), y = w[2 * half + 1] >> (8 * ks);
+                                const uint32_t a0 = x & 0x000f000fu, a1 = y & 0x000f000fu, a2 = x & 0x00f000f0u, a3 = y & 0x00f000f0u;
 #pragma unroll
-                                for (int r = 0; r < 2; ++r) {
-                                    float x0 = s[j][2 * r] * v0, x1 = s[j][2 * r + 1] * v1;
-                                    if (edge) {  // a row does not see what another one does: not even a NaN
-                                        const int at = pos + 8 * j + 2 * qt;
-                                        if (at > hi[r] || at < lo[r]) x0 = 0.0f;
-                                        if (at + 1 > hi[r] || at + 1 < lo[r]) x1 = 0.0f;
-                                    }
-                                    pa[ks][2 * half + r] = at_pack(x0, x1);
-                                }
+                                for (int rn = 0; rn < RN; ++rn) at_mma(o[rn][2 * b4 + half], a0, a1, a2, a3, pb[rn][2 * ks], pb[rn][2 * ks + 1]);
                             }
-#pragma unroll
-                        for (int ks = 0; ks < 2; ++ks) {
-                            const uint2 w0 = vw[2 * ks][n], w1 = vw[2 * ks + 1][n];
-                            at_mma(z[n], pa[ks], (w0.x & 15u) | ((w0.y & 15u) << 16), ((w1.x & 15u) << 4) | ((w1.y & 15u) << 20));
-                        }
-#pragma unroll
-                        for (int b4 = n * (NT / 4) / G; b4 < (n + 1) * (NT / 4) / G; ++b4) {
-                            const uint4 w4 = *reinterpret_cast<const uint4 *>(tile + kv_v_codes(D) + (b4 * 32 + lane) * 16);
-                            const uint32_t w[4] = {w4.x, w4.y, w4.z, w4.w};
-#pragma unroll
-                            for (int k = 0; k < 4; ++k) {
-                                at_mma(o[4 * b4 + k], pa[0], w[k] & 0x000f000fu, w[k] & 0x00f000f0u);
-                                at_mma(o[4 * b4 + k], pa[1], (w[k] >> 8) & 0x000f000fu, (w[k] >> 8) & 0x00f000f0u);
-                            }
-                        }
                     }
                 }
-                // ---- the slot is free: the tile ST further on
-                __syncwarp();
-                if (i + ST < count) {
-                    const int ni = i + ST;
-                    // (pages holds those of the block of 32 that tile i lies in, next_pages the following block)
-                    const int from = (ni >> 5) == (i >> 5) ? pages : next_pages;
-                    ask(ni, __shfl_sync(0xffffffffu, from, ni & 31), slot);
-                }
-                if ((i & 31) == 31) {
-                    pages = next_pages;
-                    const int n = i + 33 + lane;
-                    next_pages = n < count ? kv_page(a.c, seq, pos_of(n)) : -1;
-                }
-                if (++slot == ST) { slot = 0; phase ^= 1; }
             }
+            // ---- the slot is free: the tile ST further on
+            __syncwarp();
+            if (i + ST < count) {
+                const int ni = i + ST;
+                // (at_now has those of the block of 32 that tile i lies in, at_next the block behind it)
+                ask(__shfl_sync(0xffffffffu, (ni >> 5) == (i >> 5) ? at_now : at_next, ni & 31), slot);
+            }
+            if ((i & 31) == 31) {
+                at_now = at_next;
+                at_next = where(i + 33 + lane);
+            }
+            if (++slot == ST) { slot = 0; phase ^= 1; }
+        }
 
-            // ---- join of the four warps: each puts its sums where its ring was (all of its copies have landed)
-            const int es = top_e - 141 + 24, e1 = es / 2, e2 = es - e1;
-            const float back1 = at_pow2(e1), back2 = at_pow2(e2);
-            float *part = reinterpret_cast<float *>(ring);
+        // ---- join of the four warps: each puts its sums where its ring was (all of its copies have landed)
+        const int es = top_e - AT_UP + 24, e1 = es / 2, e2 = es - e1;
+        const float back1 = at_pow2(e1), back2 = at_pow2(e2);
+        float *part = reinterpret_cast<float *>(ring);
 #pragma unroll
-            for (int r = 0; r < 2; ++r) {
-                l[r] += __shfl_xor_sync(0xffffffffu, l[r], 1);
-                l[r] += __shfl_xor_sync(0xffffffffu, l[r], 2);
-                if (qt == 0) {
-                    s_m[warp][qg + 8 * r] = m[r];
-                    s_l[warp][qg + 8 * r] = l[r];
+        for (int rn = 0; rn < RN; ++rn)
+#pragma unroll
+            for (int k = 0; k < 2; ++k) {
+                const int row = 8 * rn + 2 * qt + k;
+                float x = l[rn][k];
+                x += __shfl_xor_sync(0xffffffffu, x, 4);
+                x += __shfl_xor_sync(0xffffffffu, x, 8);
+                x += __shfl_xor_sync(0xffffffffu, x, 16);
+                if (qg == 0) {
+                    s_m[warp][row] = m[rn][k];
+                    s_l[warp][row] = x;
                 }
 #pragma unroll
-                for (int n = 0; n < NT; ++n) {
-                    const float zz = z[n * G / NT][2 * r];
-                    *reinterpret_cast<float2 *>(part + (qg + 8 * r) * D + 8 * n + 2 * qt) =
-                        make_float2((o[n][2 * r] - zz) * back1 * back2, (o[n][2 * r + 1] - zz) * back1 * back2);
+                for (int n = 0; n < MT; ++n) {
+                    const float zz = z[rn][n * G / MT][k];
+                    part[row * PITCH + 16 * n + qg] = (o[rn][n][k] - zz) * back1 * back2;
+                    part[row * PITCH + 16 * n + 8 + qg] = (o[rn][n][2 + k] - zz) * back1 * back2;
                 }
             }
-            __syncthreads();
-            const bool whole = t0 == 0 && t1 == tiles;
-            const int slot_out = 2 * (int)blockIdx.x + (t0 == 0 ? 1 : 0);
-            float *sums = a.part + (size_t)slot_out * AT_ROWS * D, *ml = a.part + (size_t)2 * a.ctas * AT_ROWS * D + (size_t)slot_out * AT_ROWS * 2;
-            for (int row = warp; row < rows; row += AT_WARPS) {
-                float top = -INFINITY, wt[AT_WARPS], sum = 0.0f;
+        __syncthreads();
+        const bool whole = t0 == 0 && t1 == tiles;
+        const int slot_out = 2 * (int)blockIdx.x + (t0 == 0 ? 1 : 0);
+        float *sums = a.part + (size_t)slot_out * ROWS * D, *ml = a.part + (size_t)2 * a.ctas * ROWS * D + (size_t)slot_out * ROWS * 2;
+        for (int row = warp; row < rows; row += AT_WARPS) {
+            float top = -INFINITY, wt[AT_WARPS], sum = 0.0f;
 #pragma unroll
-                for (int w = 0; w < AT_WARPS; ++w) top = fmaxf(top, s_m[w][row]);
-                const float ref = top == -INFINITY ? 0.0f : top;
+            for (int w = 0; w < AT_WARPS; ++w) top = fmaxf(top, s_m[w][row]);
+            const float ref = top == -INFINITY ? 0.0f : top;
+#pragma unroll
+            for (int w = 0; w < AT_WARPS; ++w) {
+                wt[w] = at_ex2(s_m[w][row] - ref);
+                sum += wt[w] * s_l[w][row];
+            }
+            const float by = whole ? (sum > 0.0f || sum != sum ? 1.0f / sum : 0.0f) : 1.0f;
+            const int in = rt * ROWS + row, tok = in / a.g, hd = in - tok * a.g;
+            const long long tokrow = (long long)seq * a.nq + tok;
+#pragma unroll
+            for (int c = 0; c < D; c += 32) {
+                float v = 0.0f;
 #pragma unroll
                 for (int w = 0; w < AT_WARPS; ++w) {
-                    wt[w] = at_ex2(s_m[w][row] - ref);
-                    sum += wt[w] * s_l[w][row];
+                    const float x = reinterpret_cast<const float *>(at_raw + w * ST * TILE)[row * PITCH + c + lane];
+                    v += wt[w] > 0.0f || x != x ? wt[w] * x : 0.0f;
                 }
-                const float by = whole ? (sum > 0.0f || sum != sum ? 1.0f / sum : 0.0f) : 1.0f;
-                const int in = rt * AT_ROWS + row, tok = in / a.g, hd = in - tok * a.g;
-                const long long tokrow = (long long)seq * a.nq + tok;
-#pragma unroll
-                for (int c = 0; c < D; c += 32) {
-                    float v = 0.0f;
-#pragma unroll
-                    for (int w = 0; w < AT_WARPS; ++w) {
-                        const float x = reinterpret_cast<const float *>(at_raw + w * ST * TILE)[row * D + c + lane];
-                        v += wt[w] > 0.0f || x != x ? wt[w] * x : 0.0f;
-                    }
-                    if (whole) at_store(a.out + tokrow * a.ldo + (long long)(h * a.g + hd) * D + c + lane, v * by, a.bf16);
-                    else sums[row * D + c + lane] = v;
-                }
-                if (lane == 0) {
-                    if (!whole) {
-                        ml[2 * row] = top;
-                        ml[2 * row + 1] = sum;
-                    } else if (a.lse) {
-                        a.lse[tokrow * (a.c.heads * a.g) + h * a.g + hd] = sum > 0.0f || sum != sum ? top * LN2 + logf(sum) : -INFINITY;
-                    }
+                if (whole) at_store(a.out + tokrow * a.ldo + (long long)(h * a.g + hd) * D + c + lane, v * by, a.bf16);
+                else sums[row * D + c + lane] = v;
+            }
+            if (lane == 0) {
+                if (!whole) {
+                    ml[2 * row] = top;
+                    ml[2 * row + 1] = sum;
+                } else if (a.lse) {
+                    a.lse[tokrow * (a.c.heads * a.g) + h * a.g + hd] = sum > 0.0f || sum != sum ? top * LN2 + logf(sum) : -INFINITY;
                 }
             }
-            asm volatile("fence.proxy.async.shared::cta;" ::: "memory");  // the next copies may overwrite what was read and written here
-            __syncthreads();
-            u += t1 - t0;
-            if (u - base >= (long long)tiles * per) { base += (long long)tiles * per; ++seq; }
         }
+        asm volatile("fence.proxy.async.shared::cta;" ::: "memory");  // the next copies may overwrite what was read and written here
+        __syncthreads();
+        u += t1 - t0;
+        if (u - base >= (long long)tiles * per) { base += (long long)tiles * per; ++seq; }
     }
 }
 
 // Joins the parts of the items that were cut, and writes the rows of sequences without tokens.  One block per row of an item.
-template <int D>
+template <int D, int ROWS>
 __global__ void __launch_bounds__(AT_THREADS) kv4_join_kernel(const AtArgs a) {
     constexpr float LN2 = 0.69314718055994531f;
-    __shared__ long long s_sum[AT_WARPS + 2];
+    __shared__ long long s_sum[2 * AT_WARPS];
     __shared__ float s_w[AT_THREADS];
     __shared__ int s_at[AT_THREADS];
+    const int seq = blockIdx.x, item = blockIdx.y, rt = item / a.c.heads, h = item - rt * a.c.heads, row = blockIdx.z, tid = threadIdx.x;
+    const int in = rt * ROWS + row, per = a.c.heads * a.row_tiles;
+    // The lengths are older than the first kernel, which lets this one begin only after its own wait: they may be read before the wait here.
+    int first;
+    const int tiles = at_tiles(a, seq, first);
+    long long all, before;
+    at_count(a, seq, s_sum, all, before);
+    const long long units = all * per, u0 = before * per + (long long)item * tiles;
     griddep_wait();
     griddep_launch_dependents();
-    const int seq = blockIdx.x, item = blockIdx.y, rt = item / a.c.heads, h = item - rt * a.c.heads, row = blockIdx.z, tid = threadIdx.x;
-    const int in = rt * AT_ROWS + row;
     if (in >= a.nq * a.g) return;
-    const int tok = in / a.g, hd = in - tok * a.g, per = a.c.heads * a.row_tiles;
+    const int tok = in / a.g, hd = in - tok * a.g;
     const long long tokrow = (long long)seq * a.nq + tok;
     unsigned short *out = a.out + tokrow * a.ldo + (long long)(h * a.g + hd) * D;
     float *lse = a.lse ? a.lse + tokrow * (a.c.heads * a.g) + h * a.g + hd : nullptr;
-    int first;
-    const int tiles = at_tiles(a, seq, first);
     if (tiles == 0) {
         for (int c = tid; c < D; c += AT_THREADS) at_store(out + c, 0.0f, a.bf16);
         if (lse && tid == 0) *lse = -INFINITY;
         return;
     }
-    long long all = 0, before = 0;
-    for (int b = tid; b < a.c.n_seqs; b += AT_THREADS) {
-        int f;
-        const int n = at_tiles(a, b, f);
-        all += n;
-        if (b < seq) before += n;
-    }
-    const long long units = at_block_sum(all, s_sum) * per, u0 = at_block_sum(before, s_sum) * per + (long long)item * tiles;
     const int ctas = at_ctas(units, a.ctas), i0 = at_cta_of(units, u0, ctas), i1 = at_cta_of(units, u0 + tiles - 1, ctas);
     if (i0 == i1) return;  // finished by its CTA
-    const float *ml = a.part + (size_t)2 * a.ctas * AT_ROWS * D;
+    const float *ml = a.part + (size_t)2 * a.ctas * ROWS * D;
     auto slot_of = [&](int i) { return 2 * i + (i == i0 ? 1 : 0); };
     // maximum over the parts
     float top = -INFINITY;
-    for (int i = i0 + tid; i <= i1; i += AT_THREADS) top = fmaxf(top, __ldcg(ml + ((size_t)slot_of(i) * AT_ROWS + row) * 2));
+    for (int i = i0 + tid; i <= i1; i += AT_THREADS) top = fmaxf(top, __ldcg(ml + ((size_t)slot_of(i) * ROWS + row) * 2));
 #pragma unroll
     for (int o = 16; o > 0; o /= 2) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, o));
     if ((tid & 31) == 0) s_w[tid >> 5] = top;
@@ -572,7 +642,7 @@ __global__ void __launch_bounds__(AT_THREADS) kv4_join_kernel(const AtArgs a) {
         __syncthreads();
         float part_l = 0.0f;
         if (tid < n) {
-            const float2 p = __ldcg(reinterpret_cast<const float2 *>(ml + ((size_t)slot_of(i + tid) * AT_ROWS + row) * 2));
+            const float2 p = __ldcg(reinterpret_cast<const float2 *>(ml + ((size_t)slot_of(i + tid) * ROWS + row) * 2));
             s_w[tid] = at_ex2(p.x - ref);
             s_at[tid] = slot_of(i + tid);
             part_l = s_w[tid] * p.y;
@@ -582,7 +652,7 @@ __global__ void __launch_bounds__(AT_THREADS) kv4_join_kernel(const AtArgs a) {
 #pragma unroll 8
         for (int k = 0; k < n; ++k) {
             const float w = s_w[k];
-            const float *src = a.part + ((size_t)s_at[k] * AT_ROWS + row) * D;
+            const float *src = a.part + ((size_t)s_at[k] * ROWS + row) * D;
 #pragma unroll
             for (int c = 0; c < (D + AT_THREADS - 1) / AT_THREADS; ++c)
                 if (D % AT_THREADS == 0 || tid < D) {
@@ -608,20 +678,25 @@ __global__ void __launch_bounds__(AT_THREADS) kv4_join_kernel(const AtArgs a) {
     if (lse && tid == 0) *lse = any ? top * LN2 + logf(sum) : -INFINITY;
 }
 
-template <int D, int G>
-static cudaError_t at_launch(const AtArgs &a, cudaStream_t st) {
+template <int D, int G, int RN>
+static cudaError_t at_launch_rn(const AtArgs &a, cudaStream_t st) {
     static SmemOptIn opt_in;
-    constexpr int SMEM = AT_WARPS * at_stages<D, G>() * kv_tile_bytes(D, G);
-    auto kern = kv4_attend_kernel<D, G>;
+    constexpr int SMEM = AT_WARPS * at_stages(D, G, RN) * kv_tile_bytes(D, G);
+    auto kern = kv4_attend_kernel<D, G, RN>;
     cudaError_t e = ensure_dynamic_smem(kern, SMEM, opt_in);
     if (e != cudaSuccess) return e;
     e = launch(kern, dim3(a.ctas), dim3(AT_THREADS), SMEM, st, g_tune.pdl != 0, a);
     if (e != cudaSuccess) return e;
-    const int rows = a.nq * a.g < AT_ROWS ? a.nq * a.g : AT_ROWS;
-    return launch(kv4_join_kernel<D>, dim3(a.c.n_seqs, a.c.heads * a.row_tiles, rows), dim3(AT_THREADS), 0, st, g_tune.pdl != 0, a);
+    const int rows = a.nq * a.g < 8 * RN ? a.nq * a.g : 8 * RN;
+    return launch(kv4_join_kernel<D, 8 * RN>, dim3(a.c.n_seqs, a.c.heads * a.row_tiles, rows), dim3(AT_THREADS), 0, st, g_tune.pdl != 0, a);
+}
+template <int D, int G>
+static cudaError_t at_launch(const AtArgs &a, int rn, cudaStream_t st) {
+    return rn == 1 ? at_launch_rn<D, G, 1>(a, st) : at_launch_rn<D, G, 2>(a, st);
 }
 
-static int at_grid(int D) { return sm_count() * (D == 256 ? at_resident<256>() : at_resident<128>()); }
+// Eight rows at a time where a head has no more than that, else sixteen: the cache is then read (and unpacked) half as often.
+static int at_row_groups(int rows) { return rows <= 8 ? 1 : 2; }
 
 }  // namespace scap
 
@@ -630,7 +705,8 @@ using namespace scap;
 extern "C" size_t scap_kv4_attend_workspace(int n_seqs, int nq, int q_heads, int heads, int head_dim) {
     if (n_seqs < 1 || n_seqs > SCAP_MAX_SEQS || nq < 1 || nq > SCAP_MAX_BATCH || heads < 1 || heads > 1024 || q_heads < heads || q_heads % heads || q_heads > 1024) return 0;
     if (head_dim != 64 && head_dim != 128 && head_dim != 256) return 0;
-    return (size_t)2 * at_grid(head_dim) * AT_ROWS * (head_dim + 2) * sizeof(float);
+    const int rn = at_row_groups(nq * (q_heads / heads));
+    return (size_t)2 * sm_count() * at_resident(head_dim, 1, rn) * 8 * rn * (head_dim + 2) * sizeof(float);  // (G = 1: the most CTAs)
 }
 
 extern "C" scap_status scap_kv4_attend(const scap_kv4 *cache, const void *q, int64_t ldq, void *out, int64_t ldo, float *lse, int nq, int q_heads, double scale, int window,
@@ -654,21 +730,22 @@ extern "C" scap_status scap_kv4_attend(const scap_kv4 *cache, const void *q, int
     a.lse = lse; a.ldq = ldq; a.ldo = ldo;
     a.part = reinterpret_cast<float *>(ws);
     a.nq = nq; a.g = q_heads / cache->heads;
-    a.row_tiles = (nq * a.g + AT_ROWS - 1) / AT_ROWS;
+    const int rn = at_row_groups(nq * a.g);
+    a.row_tiles = (nq * a.g + 8 * rn - 1) / (8 * rn);
     a.window = window;
     a.scale = (float)(scale * 1.4426950408889634);
-    a.ctas = at_grid(cache->head_dim);
+    a.ctas = sm_count() * at_resident(cache->head_dim, a.c.groups, rn);
     a.bf16 = dt == SCAP_BF16;
     a.limit = g_tune.tc_spin ? (uint32_t)g_tune.tc_spin : TRIES;
     a.status = tc_status_ptr();
     cudaStream_t st = reinterpret_cast<cudaStream_t>(stream);
     switch (cache->head_dim * 8 + a.c.groups) {
-        case 64 * 8 + 1: return cuda_status(at_launch<64, 1>(a, st));
-        case 64 * 8 + 2: return cuda_status(at_launch<64, 2>(a, st));
-        case 128 * 8 + 1: return cuda_status(at_launch<128, 1>(a, st));
-        case 128 * 8 + 2: return cuda_status(at_launch<128, 2>(a, st));
-        case 128 * 8 + 4: return cuda_status(at_launch<128, 4>(a, st));
-        case 256 * 8 + 2: return cuda_status(at_launch<256, 2>(a, st));
-        default: return cuda_status(at_launch<256, 4>(a, st));
+        case 64 * 8 + 1: return cuda_status(at_launch<64, 1>(a, rn, st));
+        case 64 * 8 + 2: return cuda_status(at_launch<64, 2>(a, rn, st));
+        case 128 * 8 + 1: return cuda_status(at_launch<128, 1>(a, rn, st));
+        case 128 * 8 + 2: return cuda_status(at_launch<128, 2>(a, rn, st));
+        case 128 * 8 + 4: return cuda_status(at_launch<128, 4>(a, rn, st));
+        case 256 * 8 + 2: return cuda_status(at_launch<256, 2>(a, rn, st));
+        default: return cuda_status(at_launch<256, 4>(a, rn, st));
     }
 }
