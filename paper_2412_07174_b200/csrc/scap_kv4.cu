@@ -181,9 +181,9 @@ __global__ void __launch_bounds__(KV_THREADS) kv4_append_kernel(const KvCache c,
                 if constexpr (CPL == 2) *to = (unsigned char)kc;
                 else if constexpr (CPL == 4) *reinterpret_cast<unsigned short *>(to) = (unsigned short)kc;
                 else *reinterpret_cast<uint32_t *>(to) = kc;
-                if (writes) kw[g * KV_TILE + tok] = word;
+                if (writes) kw[g * KV_TILE + kv_word_at(tok)] = word;
                 const uint32_t vc = kv_quantise<CPL, BF16>(vx[i], group_lanes, word);
-                if (writes) vw[g * KV_TILE + tok] = word;
+                if (writes) vw[g * KV_TILE + kv_word_at(tok)] = word;
 #pragma unroll
                 for (int k = 0; k < CPL; ++k) vcode[k] |= ((vc >> (4 * k)) & 15u) << nib;
                 mask |= 15u << nib;
@@ -235,8 +235,8 @@ __global__ void __launch_bounds__(KV_THREADS) kv4_read_kernel(const KvCache c, c
                 if constexpr (CPL == 2) kcode[i] = __ldcg(from);
                 else if constexpr (CPL == 4) kcode[i] = __ldcg(reinterpret_cast<const unsigned short *>(from));
                 else kcode[i] = __ldcg(reinterpret_cast<const uint32_t *>(from));
-                kword[i] = __ldcg(kw + tok);
-                vword[i] = __ldcg(vw + tok);
+                kword[i] = __ldcg(kw + kv_word_at(tok));
+                vword[i] = __ldcg(vw + kv_word_at(tok));
             }
 #pragma unroll
             for (int i = 0; i < 8; ++i) {

@@ -3,8 +3,8 @@
 // A page holds page_tokens tokens (a multiple of 32) of every key head.  Head by head, then tile by tile, a tile being 32 tokens:
 //   K codes  32 rows of D/2 bytes
 //   V codes  32 D/2 bytes
-//   K words  [groups][32]   one 32-bit word per token and group of channels: the scale, whose low four bits are the zero point
-//   V words  [groups][32]
+//   K words  [groups][32]   one 32-bit word per token and group of channels: the scale, whose low four bits are the zero point;
+//   V words  [groups][32]   token 8 j + i at place 4 i + j, so that the four tokens of a lane are one 16-byte load
 // A code q in 0..15 stands for s (q - zero).  s has 20 significant bits, so the low four bits of its binary32 form are free for the
 // zero point, and s (q - zero) is exact in binary32.
 //
@@ -31,6 +31,8 @@ __host__ __device__ constexpr int kv_v_words(int D, int groups) { return KV_TILE
 
 // Byte of a K row that holds channels c, c + 1 (c even).
 __host__ __device__ constexpr int kv_k_byte(int D, int c) { return (((c >> 3) & 3) * (D / 32) + (c >> 5)) * 4 + ((c & 7) >> 1); }
+// Place of a token's word.
+__host__ __device__ constexpr int kv_word_at(int tok) { return (tok & 7) * 4 + (tok >> 3); }
 // Word of the V codes that holds channel c of the tokens 8 j + 2 t + o.
 __host__ __device__ constexpr int kv_v_word(int c, int t) { return (((c >> 5) * 32 + (c & 7) * 4 + t) << 2) + ((c >> 3) & 3); }
 

@@ -221,31 +221,25 @@ __global__ void __launch_bounds__(AT_THREADS, at_resident(D, G, RN)) kv4_attend_
             return page < 0 ? 0ull : (unsigned long long)kv_tile(a.c, page, h, pos_of(i), TILE);
         };
         unsigned long long at_now = where(lane), at_next = where(32 + lane);
-        auto ask = [&](unsigned long long src, int st) {
-            if (lane == 0) {
-                const uint32_t bar = smem_addr(&s_full[warp][st]);
-                if (src) {
-                    mbarrier_arrive_expect(bar, TILE);
-                    asm volatile("cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];" ::"r"(smem_addr(ring + st * TILE)), "l"(src), "r"(TILE), "r"(bar)
-                                 : "memory");
-                } else {
-                    asm volatile("mbarrier.arrive.shared::cta.b64 _, [%0];" ::"r"(bar) : "memory");  // the tile is empty
-                }
+        unsigned there = __ballot_sync(0xffffffffu, at_now != 0);  // which of the present 32 tiles have a page
+        auto ask = [&](unsigned long long src, int st) {  // by the lane that has the address
+            const uint32_t bar = smem_addr(&s_full[warp][st]);
+            if (src) {
+                mbarrier_arrive_expect(bar, TILE);
+                asm volatile("cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];" ::"r"(smem_addr(ring + st * TILE)), "l"(src), "r"(TILE), "r"(bar)
+                             : "memory");
+            } else {
+                asm volatile("mbarrier.arrive.shared::cta.b64 _, [%0];" ::"r"(bar) : "memory");  // the tile is empty
             }
         };
-        {
-            int st = slot;
-            for (int i = 0; i < ST && i < count; ++i) {
-                ask(__shfl_sync(0xffffffffu, at_now, i), st);
-                if (++st == ST) st = 0;
-            }
-        }
+        if (lane < ST && lane < count) ask(at_now, slot + lane < ST ? slot + lane : slot + lane - ST);
 
-        // ---- queries: rows 8 rn + qg as B operands, scaled to just below 2^12 by a power of two; channels 32 j + 8 qt + i, the
+        // ---- queries: rows 8 rn + qg as B operands, scaled by one power of two so that the largest lies just below 2^12 (what is lost of
+        // a row that is smaller by 2^x is 2^-36 of the largest scores); channels 32 j + 8 qt + i, the
         // even and odd nibbles of a code word in the two k halves of an MMA, the odd ones 16 times smaller as their codes are larger.
         // zq: minus the sum of a group, in two fp16 parts, against the zero points (times 2^6, as zero 2^-18 is the subnormal used)
         uint32_t qb[RN][2 * W][2], zq[RN][G];
-        float f[RN][2];  // what turns an accumulator of row 8 rn + 2 qt + k into a score in units of log 2
+        float f[RN];  // what turns an accumulator into a score in units of log 2
 #pragma unroll
         for (int rn = 0; rn < RN; ++rn) {
             const int row = 8 * rn + qg;
@@ -263,8 +257,9 @@ __global__ void __launch_bounds__(AT_THREADS, at_resident(D, G, RN)) kv4_attend_
                     v[j][i] = at_widen((unsigned short)(i & 1 ? w >> 16 : w), a.bf16);
                     top = fmaxf(top, fabsf(v[j][i]));
                 }
-            top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 1));
-            top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 2));
+            if (!(top < INFINITY)) top = 0.0f;  // (a row that is not finite has no say)
+#pragma unroll
+            for (int k = 1; k < 32; k *= 2) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, k));
             int e = top > 0.0f ? 11 - ((__float_as_int(top) >> 23) - 127) : 0;
             e = e > 100 ? 100 : (e < -100 ? -100 : e);
             const float up = at_pow2(e);
@@ -288,9 +283,7 @@ __global__ void __launch_bounds__(AT_THREADS, at_resident(D, G, RN)) kv4_attend_
                 const float x = -sum[n] * up * 0.015625f, x_hi = __half2float(__float2half_rn(x));
                 zq[rn][n] = at_pack(x_hi, x - x_hi);
             }
-            const float mine = at_pow2(24 - e) * a.scale;
-#pragma unroll
-            for (int k = 0; k < 2; ++k) f[rn][k] = __shfl_sync(0xffffffffu, mine, (2 * qt + k) * 4);
+            f[rn] = at_pow2(24 - e) * a.scale;
         }
         // keys that a row sees: lo .. hi
         int hi[RN][2], lo[RN][2];
@@ -339,7 +332,7 @@ __global__ void __launch_bounds__(AT_THREADS, at_resident(D, G, RN)) kv4_attend_
             }
             const unsigned char *tile = ring + slot * TILE;
             const int pos = pos_of(i);
-            if (__shfl_sync(0xffffffffu, at_now, i & 31) != 0) {
+            if ((there >> (i & 31)) & 1u) {
                 // keys that not every row sees: tokens behind the last, before a window, or newer than the row's own
                 const bool edge = pos + KV_TILE - 1 > hi_all || pos < lo_all;
                 // ---- scores: s[rn][j][k] is row 8 rn + 2 qt + k at token 8 j + qg.  The four blocks of eight tokens are two A operands.
@@ -347,8 +340,7 @@ __global__ void __launch_bounds__(AT_THREADS, at_resident(D, G, RN)) kv4_attend_
                 uint32_t kw[G][4];
 #pragma unroll
                 for (int n = 0; n < G; ++n)
-#pragma unroll
-                    for (int j = 0; j < 4; ++j) kw[n][j] = *reinterpret_cast<const uint32_t *>(tile + kv_k_words(D) + (n * KV_TILE + 8 * j + qg) * 4);
+                    *reinterpret_cast<uint4 *>(kw[n]) = *reinterpret_cast<const uint4 *>(tile + kv_k_words(D) + (n * KV_TILE + 4 * qg) * 4);
                 {
                     float acc[2][RN][G][4];
                     uint32_t w[4][W];
@@ -389,12 +381,14 @@ __global__ void __launch_bounds__(AT_THREADS, at_resident(D, G, RN)) kv4_attend_
                         for (int n = 0; n < G; ++n) {
                             const float ks = __uint_as_float(kw[n][j] & ~15u);
 #pragma unroll
-                            for (int rn = 0; rn < RN; ++rn)
+                            for (int rn = 0; rn < RN; ++rn) {
+                                const float by = ks * f[rn];
 #pragma unroll
                                 for (int k = 0; k < 2; ++k) {
-                                    const float t = (ks * f[rn][k]) * acc[j >> 1][rn][n][2 * (j & 1) + k];
-                                    s[rn][j][k] = n == 0 ? t : s[rn][j][k] + t;
+                                    const float x = acc[j >> 1][rn][n][2 * (j & 1) + k];
+                                    s[rn][j][k] = n == 0 ? by * x : s[rn][j][k] + by * x;
                                 }
+                            }
                         }
                 }
                 if (edge) {
@@ -408,13 +402,24 @@ __global__ void __launch_bounds__(AT_THREADS, at_resident(D, G, RN)) kv4_attend_
                                 if (at > hi[rn][k] || at < lo[rn][k]) s[rn][j][k] = -INFINITY;
                             }
                 }
-                // ---- largest scale of the values, a token per lane; tokens that no row sees have none, whatever lies there
-                uint32_t big = 0;
+                // ---- largest scale of the values; tokens that no row sees have none, whatever lies there
+                uint32_t vw[G][4], big = 0;
 #pragma unroll
                 for (int n = 0; n < G; ++n) {
-                    uint32_t w = *reinterpret_cast<const uint32_t *>(tile + kv_v_words(D, G) + (n * KV_TILE + lane) * 4);
-                    if (edge && (pos + lane >= len || pos + lane <= lo_all - a.nq)) w = 0;
-                    big = max(big, w < 0x7f800000u ? w : 0u);
+                    *reinterpret_cast<uint4 *>(vw[n]) = *reinterpret_cast<const uint4 *>(tile + kv_v_words(D, G) + (n * KV_TILE + 4 * qg) * 4);
+                    if (edge) {
+#pragma unroll
+                        for (int j = 0; j < 4; ++j)
+                            if (pos + 8 * j + qg >= len || pos + 8 * j + qg <= lo_all - a.nq) vw[n][j] = 0;
+                    }
+                    big = max(max(big, max(vw[n][0], vw[n][1])), max(vw[n][2], vw[n][3]));
+                }
+                if (__any_sync(0xffffffffu, big >= 0x7f800000u)) {  // a NaN has no say
+                    big = 0;
+#pragma unroll
+                    for (int n = 0; n < G; ++n)
+#pragma unroll
+                        for (int j = 0; j < 4; ++j) big = max(big, vw[n][j] < 0x7f800000u ? vw[n][j] : 0u);
                 }
                 const int e = (int)(__reduce_max_sync(0xffffffffu, big) >> 23);
                 // ---- reference of the weights: the largest score, but left as it is while weights stay below 2^8, so that the
@@ -474,7 +479,7 @@ __global__ void __launch_bounds__(AT_THREADS, at_resident(D, G, RN)) kv4_attend_
                     uint32_t pb[RN][4];
 #pragma unroll
                     for (int j = 0; j < 4; ++j) {
-                        const float vs = __uint_as_float(*reinterpret_cast<const uint32_t *>(tile + kv_v_words(D, G) + (n * KV_TILE + 8 * j + qg) * 4) & ~15u) * (j & 1 ? up16 : up);
+                        const float vs = __uint_as_float(vw[n][j] & ~15u) * (j & 1 ? up16 : up);
 #pragma unroll
                         for (int rn = 0; rn < RN; ++rn) {
                             float x0 = s[rn][j][0] * vs, x1 = s[rn][j][1] * vs;
@@ -486,11 +491,12 @@ __global__ void __launch_bounds__(AT_THREADS, at_resident(D, G, RN)) kv4_attend_
                             pb[rn][j] = at_trans(at_pack(x0, x1));
                         }
                     }
+                    uint32_t w0[4], w1[4];  // tokens 8 j + 2 qt and the next
+                    *reinterpret_cast<uint4 *>(w0) = *reinterpret_cast<const uint4 *>(tile + kv_v_words(D, G) + (n * KV_TILE + 8 * qt) * 4);
+                    *reinterpret_cast<uint4 *>(w1) = *reinterpret_cast<const uint4 *>(tile + kv_v_words(D, G) + (n * KV_TILE + 8 * qt + 4) * 4);
 #pragma unroll
                     for (int ks = 0; ks < 2; ++ks) {
-                        const uint2 w0 = *reinterpret_cast<const uint2 *>(tile + kv_v_words(D, G) + (n * KV_TILE + 16 * ks + 2 * qt) * 4);
-                        const uint2 w1 = *reinterpret_cast<const uint2 *>(tile + kv_v_words(D, G) + (n * KV_TILE + 16 * ks + 8 + 2 * qt) * 4);
-                        const uint32_t z0 = __byte_perm(w0.x, w0.y, 0x5410) & 0x000f000fu, z1 = (__byte_perm(w1.x, w1.y, 0x5410) & 0x000f000fu) << 4;
+                        const uint32_t z0 = __byte_perm(w0[2 * ks], w1[2 * ks], 0x5410) & 0x000f000fu, z1 = (__byte_perm(w0[2 * ks + 1], w1[2 * ks + 1], 0x5410) & 0x000f000fu) << 4;
 #pragma unroll
                         for (int rn = 0; rn < RN; ++rn) at_mma(z[rn][n], z0, z0, z1, z1, pb[rn][2 * ks], pb[rn][2 * ks + 1]);
                     }
@@ -512,13 +518,12 @@ __global__ void __launch_bounds__(AT_THREADS, at_resident(D, G, RN)) kv4_attend_
             }
             // ---- the slot is free: the tile ST further on
             __syncwarp();
-            if (i + ST < count) {
-                const int ni = i + ST;
-                // (at_now has those of the block of 32 that tile i lies in, at_next the block behind it)
-                ask(__shfl_sync(0xffffffffu, (ni >> 5) == (i >> 5) ? at_now : at_next, ni & 31), slot);
-            }
+            const int ni = i + ST;
+            // (at_now has the addresses of the block of 32 that tile i lies in, at_next those of the block behind it)
+            if (ni < count && lane == (ni & 31)) ask((ni >> 5) == (i >> 5) ? at_now : at_next, slot);
             if ((i & 31) == 31) {
                 at_now = at_next;
+                there = __ballot_sync(0xffffffffu, at_now != 0);
                 at_next = where(i + 33 + lane);
             }
             if (++slot == ST) { slot = 0; phase ^= 1; }
