@@ -602,8 +602,7 @@ template <int D, int ROWS>
 __global__ void __launch_bounds__(AT_THREADS) kv4_join_kernel(const AtArgs a) {
     constexpr float LN2 = 0.69314718055994531f;
     __shared__ long long s_sum[2 * AT_WARPS];
-    __shared__ float s_w[AT_THREADS];
-    __shared__ int s_at[AT_THREADS];
+    __shared__ float s_w[AT_WARPS], s_v[AT_WARPS][D];
     const int seq = blockIdx.x, item = blockIdx.y, rt = item / a.c.heads, h = item - rt * a.c.heads, row = blockIdx.z, tid = threadIdx.x;
     const int in = rt * ROWS + row, per = a.c.heads * a.row_tiles;
     // The lengths are older than the first kernel, which lets this one begin only after its own wait: they may be read before the wait here.
@@ -628,58 +627,57 @@ __global__ void __launch_bounds__(AT_THREADS) kv4_join_kernel(const AtArgs a) {
     if (i0 == i1) return;  // finished by its CTA
     const float *ml = a.part + (size_t)2 * a.ctas * ROWS * D;
     auto slot_of = [&](int i) { return 2 * i + (i == i0 ? 1 : 0); };
-    // maximum over the parts
+    // Each warp takes every fourth part, a lane D/32 neighbouring channels of them, several parts under way at a time.
+    constexpr int CPL = D / 32, AHEAD = 8;
+    const int warp = tid >> 5, lane = tid & 31, parts = i1 - i0 + 1;
     float top = -INFINITY;
-    for (int i = i0 + tid; i <= i1; i += AT_THREADS) top = fmaxf(top, __ldcg(ml + ((size_t)slot_of(i) * ROWS + row) * 2));
+    for (int i = tid; i < parts; i += AT_THREADS) top = fmaxf(top, __ldcg(ml + ((size_t)slot_of(i0 + i) * ROWS + row) * 2));
 #pragma unroll
     for (int o = 16; o > 0; o /= 2) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, o));
-    if ((tid & 31) == 0) s_w[tid >> 5] = top;
+    if (lane == 0) s_w[warp] = top;
     __syncthreads();
     top = s_w[0];
 #pragma unroll
     for (int w = 1; w < AT_WARPS; ++w) top = fmaxf(top, s_w[w]);
     const float ref = top == -INFINITY ? 0.0f : top;
-    float sum = 0.0f, v[(D + AT_THREADS - 1) / AT_THREADS];
+    float sum = 0.0f, v[CPL];
 #pragma unroll
-    for (int k = 0; k < (D + AT_THREADS - 1) / AT_THREADS; ++k) v[k] = 0.0f;
-    for (int i = i0; i <= i1; i += AT_THREADS) {
-        const int n = min(AT_THREADS, i1 - i + 1);
-        __syncthreads();
-        float part_l = 0.0f;
-        if (tid < n) {
-            const float2 p = __ldcg(reinterpret_cast<const float2 *>(ml + ((size_t)slot_of(i + tid) * ROWS + row) * 2));
-            s_w[tid] = at_ex2(p.x - ref);
-            s_at[tid] = slot_of(i + tid);
-            part_l = s_w[tid] * p.y;
+    for (int k = 0; k < CPL; ++k) v[k] = 0.0f;
+    for (int i = warp; i < parts; i += AT_WARPS * AHEAD) {
+        float2 p[AHEAD];
+        float x[AHEAD][CPL];
+#pragma unroll
+        for (int k = 0; k < AHEAD; ++k) {
+            const int at = slot_of(i0 + min(i + k * AT_WARPS, parts - 1));
+            p[k] = __ldcg(reinterpret_cast<const float2 *>(ml + ((size_t)at * ROWS + row) * 2));
+            const float *src = a.part + ((size_t)at * ROWS + row) * D + lane * CPL;
+#pragma unroll
+            for (int c = 0; c < CPL; c += 2) {
+                const float2 y = __ldcg(reinterpret_cast<const float2 *>(src + c));
+                x[k][c] = y.x;
+                x[k][c + 1] = y.y;
+            }
         }
-        __syncthreads();
-        sum += part_l;
-#pragma unroll 8
-        for (int k = 0; k < n; ++k) {
-            const float w = s_w[k];
-            const float *src = a.part + ((size_t)s_at[k] * ROWS + row) * D;
 #pragma unroll
-            for (int c = 0; c < (D + AT_THREADS - 1) / AT_THREADS; ++c)
-                if (D % AT_THREADS == 0 || tid < D) {
-                    const float x = __ldcg(src + c * AT_THREADS + tid);
-                    v[c] += w > 0.0f || x != x ? w * x : 0.0f;
-                }
+        for (int k = 0; k < AHEAD; ++k) {
+            const float w = i + k * AT_WARPS < parts ? at_ex2(p[k].x - ref) : 0.0f;
+            if (i + k * AT_WARPS < parts) {
+                sum += w * p[k].y;
+#pragma unroll
+                for (int c = 0; c < CPL; ++c) v[c] += w > 0.0f || x[k][c] != x[k][c] ? w * x[k][c] : 0.0f;
+            }
         }
     }
-    // the sums of the threads in one order
-#pragma unroll
-    for (int o = 16; o > 0; o /= 2) sum += __shfl_xor_sync(0xffffffffu, sum, o);
+    // the four warps in order
     __syncthreads();
-    if ((tid & 31) == 0) s_w[tid >> 5] = sum;
-    __syncthreads();
-    sum = s_w[0];
 #pragma unroll
-    for (int w = 1; w < AT_WARPS; ++w) sum += s_w[w];
+    for (int c = 0; c < CPL; ++c) s_v[warp][lane * CPL + c] = v[c];
+    if (lane == 0) s_w[warp] = sum;
+    __syncthreads();
+    sum = ((s_w[0] + s_w[1]) + s_w[2]) + s_w[3];
     const bool any = sum > 0.0f || sum != sum;
     const float by = any ? 1.0f / sum : 0.0f;
-#pragma unroll
-    for (int c = 0; c < (D + AT_THREADS - 1) / AT_THREADS; ++c)
-        if (D % AT_THREADS == 0 || tid < D) at_store(out + c * AT_THREADS + tid, v[c] * by, a.bf16);
+    for (int c = tid; c < D; c += AT_THREADS) at_store(out + c, (((s_v[0][c] + s_v[1][c]) + s_v[2][c]) + s_v[3][c]) * by, a.bf16);
     if (lse && tid == 0) *lse = any ? top * LN2 + logf(sum) : -INFINITY;
 }
 
