@@ -44,6 +44,7 @@ struct AtArgs {
     float *lse;
     long long ldq, ldo;   // elements between tokens
     float *part;          // [2 C][8 RN][D] weighted sums, then [2 C][8 RN][2] reference and sum
+    int2 *where;          // [n_seqs][items]: first and last CTA of an item that was cut, equal where it was not
     int nq, g, row_tiles, window;
     float scale;          // times log2 e
     int ctas;
@@ -65,38 +66,27 @@ __device__ __forceinline__ int at_tiles(const AtArgs &a, int b, int &first) {
 }
 
 __device__ __forceinline__ long long at_cut(long long units, int i, int ctas) { return units * i / ctas; }
-__device__ __forceinline__ int at_cta_of(long long units, long long u, int ctas) { return (int)(((u + 1) * ctas - 1) / units); }
 __device__ __forceinline__ int at_ctas(long long units, int ctas) {
     const long long n = (units + AT_MIN_UNITS - 1) / AT_MIN_UNITS;
     return n < ctas ? (int)n : ctas;
 }
 
-// Number of tiles of all sequences and of those before `seq` (the whole block takes part).
-__device__ __forceinline__ void at_count(const AtArgs &a, int seq, long long *s, long long &all, long long &before) {
-    all = before = 0;
+// Number of tiles of all sequences (the whole block takes part).
+__device__ __forceinline__ long long at_count(const AtArgs &a, long long *s) {
+    long long all = 0;
     for (int b = threadIdx.x; b < a.c.n_seqs; b += AT_THREADS) {
         int first;
-        const int n = at_tiles(a, b, first);
-        all += n;
-        if (b < seq) before += n;
+        all += at_tiles(a, b, first);
     }
 #pragma unroll
-    for (int o = 16; o > 0; o /= 2) {
-        all += __shfl_xor_sync(0xffffffffu, all, o);
-        before += __shfl_xor_sync(0xffffffffu, before, o);
-    }
+    for (int o = 16; o > 0; o /= 2) all += __shfl_xor_sync(0xffffffffu, all, o);
+    if ((threadIdx.x & 31) == 0) s[threadIdx.x >> 5] = all;
     __syncthreads();
-    if ((threadIdx.x & 31) == 0) {
-        s[threadIdx.x >> 5] = all;
-        s[AT_WARPS + (threadIdx.x >> 5)] = before;
-    }
-    __syncthreads();
-    all = before = 0;
+    all = 0;
 #pragma unroll
-    for (int w = 0; w < AT_WARPS; ++w) {
-        all += s[w];
-        before += s[AT_WARPS + w];
-    }
+    for (int w = 0; w < AT_WARPS; ++w) all += s[w];
+    __syncthreads();
+    return all;
 }
 
 // This CTA's units [u, u1), the sequence that u belongs to and the first unit of that sequence (the whole block takes part); per = items
@@ -105,12 +95,7 @@ __device__ __forceinline__ bool at_begin(const AtArgs &a, int per, long long *s,
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
     long long units = 0, before = 0;
     const bool one = a.c.n_seqs <= AT_THREADS;  // one look at the lengths gives the sum and the place
-    if (!one) {
-        long long all;
-        at_count(a, 0, s, all, before);
-        units = all * per;
-        __syncthreads();
-    }
+    if (!one) units = at_count(a, s) * per;
     for (int b0 = 0; b0 < a.c.n_seqs; b0 += AT_THREADS) {
         const int b = b0 + (int)threadIdx.x;
         int first;
@@ -186,7 +171,7 @@ __global__ void __launch_bounds__(AT_THREADS, at_resident(D, G, RN)) kv4_attend_
     static_assert(ST * TILE >= ROWS * PITCH * 4, "a warp's part of the join goes where its ring was");
     extern __shared__ __align__(128) unsigned char at_raw[];
     __shared__ unsigned long long s_full[AT_WARPS][ST];
-    __shared__ long long s_sum[2 * AT_WARPS];
+    __shared__ long long s_sum[AT_WARPS + 2];
     __shared__ float s_m[AT_WARPS][ROWS], s_l[AT_WARPS][ROWS];
 
     const int tid = threadIdx.x, warp = __shfl_sync(0xffffffffu, tid >> 5, 0), lane = tid & 31, qg = lane >> 2, qt = lane & 3;
@@ -555,6 +540,12 @@ __global__ void __launch_bounds__(AT_THREADS, at_resident(D, G, RN)) kv4_attend_
             }
         __syncthreads();
         const bool whole = t0 == 0 && t1 == tiles;
+        if (tid == 0) {
+            int2 *at = a.where + (long long)seq * per + item;
+            if (whole) *at = make_int2(-1, -1);
+            else if (t0 == 0) at->x = blockIdx.x;
+            else if (t1 == tiles) at->y = blockIdx.x;
+        }
         const int slot_out = 2 * (int)blockIdx.x + (t0 == 0 ? 1 : 0);
         float *sums = a.part + (size_t)slot_out * ROWS * D, *ml = a.part + (size_t)2 * a.ctas * ROWS * D + (size_t)slot_out * ROWS * 2;
         for (int row = warp; row < rows; row += AT_WARPS) {
@@ -601,46 +592,29 @@ __global__ void __launch_bounds__(AT_THREADS, at_resident(D, G, RN)) kv4_attend_
 template <int D, int ROWS>
 __global__ void __launch_bounds__(AT_THREADS) kv4_join_kernel(const AtArgs a) {
     constexpr float LN2 = 0.69314718055994531f;
-    __shared__ long long s_sum[2 * AT_WARPS];
-    __shared__ float s_w[AT_WARPS], s_v[AT_WARPS][D];
+    __shared__ float s_w[AT_WARPS], s_top[AT_WARPS], s_v[AT_WARPS][D];
     const int seq = blockIdx.x, item = blockIdx.y, rt = item / a.c.heads, h = item - rt * a.c.heads, row = blockIdx.z, tid = threadIdx.x;
-    const int in = rt * ROWS + row, per = a.c.heads * a.row_tiles;
-    // The lengths are older than the first kernel, which lets this one begin only after its own wait: they may be read before the wait here.
-    int first;
-    const int tiles = at_tiles(a, seq, first);
-    long long all, before;
-    at_count(a, seq, s_sum, all, before);
-    const long long units = all * per, u0 = before * per + (long long)item * tiles;
-    griddep_wait();
-    griddep_launch_dependents();
-    if (in >= a.nq * a.g) return;
-    const int tok = in / a.g, hd = in - tok * a.g;
+    const int in = rt * ROWS + row, per = a.c.heads * a.row_tiles, tok = in / a.g, hd = in - tok * a.g;
     const long long tokrow = (long long)seq * a.nq + tok;
     unsigned short *out = a.out + tokrow * a.ldo + (long long)(h * a.g + hd) * D;
     float *lse = a.lse ? a.lse + tokrow * (a.c.heads * a.g) + h * a.g + hd : nullptr;
-    if (tiles == 0) {
+    const float *ml = a.part + (size_t)2 * a.ctas * ROWS * D;
+    griddep_wait();
+    griddep_launch_dependents();
+    if (in >= a.nq * a.g) return;
+    const int2 range = __ldcg(a.where + (long long)seq * per + item);
+    if (__ldcg(a.c.lens + seq) <= 0) {
         for (int c = tid; c < D; c += AT_THREADS) at_store(out + c, 0.0f, a.bf16);
         if (lse && tid == 0) *lse = -INFINITY;
         return;
     }
-    const int ctas = at_ctas(units, a.ctas), i0 = at_cta_of(units, u0, ctas), i1 = at_cta_of(units, u0 + tiles - 1, ctas);
+    const int i0 = range.x, i1 = range.y;
     if (i0 == i1) return;  // finished by its CTA
-    const float *ml = a.part + (size_t)2 * a.ctas * ROWS * D;
     auto slot_of = [&](int i) { return 2 * i + (i == i0 ? 1 : 0); };
     // Each warp takes every fourth part, a lane D/32 neighbouring channels of them, several parts under way at a time.
     constexpr int CPL = D / 32, AHEAD = 8;
     const int warp = tid >> 5, lane = tid & 31, parts = i1 - i0 + 1;
-    float top = -INFINITY;
-    for (int i = tid; i < parts; i += AT_THREADS) top = fmaxf(top, __ldcg(ml + ((size_t)slot_of(i0 + i) * ROWS + row) * 2));
-#pragma unroll
-    for (int o = 16; o > 0; o /= 2) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, o));
-    if (lane == 0) s_w[warp] = top;
-    __syncthreads();
-    top = s_w[0];
-#pragma unroll
-    for (int w = 1; w < AT_WARPS; ++w) top = fmaxf(top, s_w[w]);
-    const float ref = top == -INFINITY ? 0.0f : top;
-    float sum = 0.0f, v[CPL];
+    float top = -INFINITY, sum = 0.0f, v[CPL];
 #pragma unroll
     for (int k = 0; k < CPL; ++k) v[k] = 0.0f;
     for (int i = warp; i < parts; i += AT_WARPS * AHEAD) {
@@ -658,18 +632,33 @@ __global__ void __launch_bounds__(AT_THREADS) kv4_join_kernel(const AtArgs a) {
                 x[k][c + 1] = y.y;
             }
         }
+        float t = top;
 #pragma unroll
-        for (int k = 0; k < AHEAD; ++k) {
-            const float w = i + k * AT_WARPS < parts ? at_ex2(p[k].x - ref) : 0.0f;
+        for (int k = 0; k < AHEAD; ++k) t = i + k * AT_WARPS < parts ? fmaxf(t, p[k].x) : t;
+        const float ref = t == -INFINITY ? 0.0f : t, down = at_ex2(top - ref);
+        top = t;
+        sum *= down;
+#pragma unroll
+        for (int c = 0; c < CPL; ++c) v[c] *= down;
+#pragma unroll
+        for (int k = 0; k < AHEAD; ++k)
             if (i + k * AT_WARPS < parts) {
+                const float w = at_ex2(p[k].x - ref);
                 sum += w * p[k].y;
 #pragma unroll
                 for (int c = 0; c < CPL; ++c) v[c] += w > 0.0f || x[k][c] != x[k][c] ? w * x[k][c] : 0.0f;
             }
-        }
     }
-    // the four warps in order
+    if (lane == 0) s_top[warp] = top;
     __syncthreads();
+    float mine = top;
+#pragma unroll
+    for (int w = 0; w < AT_WARPS; ++w) top = fmaxf(top, s_top[w]);
+    mine = at_ex2(mine - (top == -INFINITY ? 0.0f : top));
+    sum *= mine;
+#pragma unroll
+    for (int c = 0; c < CPL; ++c) v[c] *= mine;
+    // the four warps in order
 #pragma unroll
     for (int c = 0; c < CPL; ++c) s_v[warp][lane * CPL + c] = v[c];
     if (lane == 0) s_w[warp] = sum;
@@ -709,7 +698,9 @@ extern "C" size_t scap_kv4_attend_workspace(int n_seqs, int nq, int q_heads, int
     if (n_seqs < 1 || n_seqs > SCAP_MAX_SEQS || nq < 1 || nq > SCAP_MAX_BATCH || heads < 1 || heads > 1024 || q_heads < heads || q_heads % heads || q_heads > 1024) return 0;
     if (head_dim != 64 && head_dim != 128 && head_dim != 256) return 0;
     const int rn = at_row_groups(nq * (q_heads / heads));
-    return (size_t)2 * sm_count() * at_resident(head_dim, 1, rn) * 8 * rn * (head_dim + 2) * sizeof(float);  // (G = 1: the most CTAs)
+    const int items = heads * ((nq * (q_heads / heads) + 8 * rn - 1) / (8 * rn));
+    return (size_t)2 * sm_count() * at_resident(head_dim, 1, rn) * 8 * rn * (head_dim + 2) * sizeof(float)  // (G = 1: the most CTAs)
+           + (size_t)n_seqs * items * sizeof(int2);
 }
 
 extern "C" scap_status scap_kv4_attend(const scap_kv4 *cache, const void *q, int64_t ldq, void *out, int64_t ldo, float *lse, int nq, int q_heads, double scale, int window,
@@ -738,6 +729,7 @@ extern "C" scap_status scap_kv4_attend(const scap_kv4 *cache, const void *q, int
     a.window = window;
     a.scale = (float)(scale * 1.4426950408889634);
     a.ctas = sm_count() * at_resident(cache->head_dim, a.c.groups, rn);
+    a.where = reinterpret_cast<int2 *>(a.part + (size_t)2 * a.ctas * 8 * rn * (cache->head_dim + 2));
     a.bf16 = dt == SCAP_BF16;
     a.limit = g_tune.tc_spin ? (uint32_t)g_tune.tc_spin : TRIES;
     a.status = tc_status_ptr();
