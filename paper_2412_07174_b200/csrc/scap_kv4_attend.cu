@@ -43,11 +43,12 @@ struct AtArgs {
     unsigned short *out;
     float *lse;
     long long ldq, ldo;   // elements between tokens
-    float *part;          // [2 C][8 RN][D] weighted sums, then [2 C][8 RN][2] reference and sum
+    float *part;          // [4 resident][8 RN][D] weighted sums, then [4 resident][8 RN][2] reference and sum
     int2 *where;          // [n_seqs][items]: first and last CTA of an item that was cut, equal where it was not
     int nq, g, row_tiles, window;
     float scale;          // times log2 e
-    int ctas;
+    int tile_cap;         // tiles that a row of the table has room for
+    int resident;         // CTAs that the device holds at once
     bool bf16;
     uint32_t limit;
     int *status;
@@ -62,13 +63,18 @@ __device__ __forceinline__ int at_tiles(const AtArgs &a, int b, int &first) {
         const long long lo = (long long)len - a.nq + 1 - a.window;  // of the first new token
         first = lo > 0 ? (int)(lo / KV_TILE) : 0;
     }
-    return (int)(((long long)len + KV_TILE - 1) / KV_TILE) - first;
+    // (what a table has no room for is not seen)
+    return max(0, min((int)(((long long)len + KV_TILE - 1) / KV_TILE), a.tile_cap) - first);
 }
 
 __device__ __forceinline__ long long at_cut(long long units, int i, int ctas) { return units * i / ctas; }
-__device__ __forceinline__ int at_ctas(long long units, int ctas) {
+// CTAs that share the units.  Where there is much to do twice as many as the device holds: the SMs favour the older ones of their CTAs, and
+// the younger ones of a second wave take over from those (83 units per resident CTA: 75 -> 71 us; 55 units: 42 -> 52).
+constexpr int AT_TWO_WAVES = 64;
+__device__ __forceinline__ int at_ctas(const AtArgs &a, long long units) {
     const long long n = (units + AT_MIN_UNITS - 1) / AT_MIN_UNITS;
-    return n < ctas ? (int)n : ctas;
+    const int most = units >= (long long)AT_TWO_WAVES * a.resident ? 2 * a.resident : a.resident;
+    return n < most ? (int)n : most;
 }
 
 // Number of tiles of all sequences (the whole block takes part).
@@ -115,7 +121,7 @@ __device__ __forceinline__ bool at_begin(const AtArgs &a, int per, long long *s,
             all += s[w];
         }
         if (one) units = all;
-        const int ctas = at_ctas(units, a.ctas);
+        const int ctas = at_ctas(a, units);
         if ((int)blockIdx.x >= ctas) return false;
         u = at_cut(units, blockIdx.x, ctas);
         u1 = at_cut(units, blockIdx.x + 1, ctas);
@@ -217,7 +223,8 @@ __global__ void __launch_bounds__(AT_THREADS, at_resident(D, G, RN)) kv4_attend_
                 asm volatile("mbarrier.arrive.shared::cta.b64 _, [%0];" ::"r"(bar) : "memory");  // the tile is empty
             }
         };
-        if (lane < ST && lane < count) ask(at_now, slot + lane < ST ? slot + lane : slot + lane - ST);
+        // (the first tile alone: those of all warps of the device are then under way before anybody's second)
+        if (lane == 0 && count > 0) ask(at_now, slot);
 
         // ---- queries: rows 8 rn + qg as B operands, scaled by one power of two so that the largest lies just below 2^12 (what is lost of
         // a row that is smaller by 2^x is 2^-36 of the largest scores); channels 32 j + 8 qt + i, the
@@ -270,6 +277,7 @@ __global__ void __launch_bounds__(AT_THREADS, at_resident(D, G, RN)) kv4_attend_
             }
             f[rn] = at_pow2(24 - e) * a.scale;
         }
+        if (lane > 0 && lane < ST && lane < count) ask(at_now, slot + lane < ST ? slot + lane : slot + lane - ST);
         // keys that a row sees: lo .. hi
         int hi[RN][2], lo[RN][2];
 #pragma unroll
@@ -547,7 +555,7 @@ __global__ void __launch_bounds__(AT_THREADS, at_resident(D, G, RN)) kv4_attend_
             else if (t1 == tiles) at->y = blockIdx.x;
         }
         const int slot_out = 2 * (int)blockIdx.x + (t0 == 0 ? 1 : 0);
-        float *sums = a.part + (size_t)slot_out * ROWS * D, *ml = a.part + (size_t)2 * a.ctas * ROWS * D + (size_t)slot_out * ROWS * 2;
+        float *sums = a.part + (size_t)slot_out * ROWS * D, *ml = a.part + (size_t)4 * a.resident * ROWS * D + (size_t)slot_out * ROWS * 2;
         for (int row = warp; row < rows; row += AT_WARPS) {
             float top = -INFINITY, wt[AT_WARPS], sum = 0.0f;
 #pragma unroll
@@ -598,12 +606,13 @@ __global__ void __launch_bounds__(AT_THREADS) kv4_join_kernel(const AtArgs a) {
     const long long tokrow = (long long)seq * a.nq + tok;
     unsigned short *out = a.out + tokrow * a.ldo + (long long)(h * a.g + hd) * D;
     float *lse = a.lse ? a.lse + tokrow * (a.c.heads * a.g) + h * a.g + hd : nullptr;
-    const float *ml = a.part + (size_t)2 * a.ctas * ROWS * D;
+    const float *ml = a.part + (size_t)4 * a.resident * ROWS * D;
     griddep_wait();
     griddep_launch_dependents();
     if (in >= a.nq * a.g) return;
     const int2 range = __ldcg(a.where + (long long)seq * per + item);
-    if (__ldcg(a.c.lens + seq) <= 0) {
+    int first;
+    if (at_tiles(a, seq, first) == 0) {
         for (int c = tid; c < D; c += AT_THREADS) at_store(out + c, 0.0f, a.bf16);
         if (lse && tid == 0) *lse = -INFINITY;
         return;
@@ -671,20 +680,20 @@ __global__ void __launch_bounds__(AT_THREADS) kv4_join_kernel(const AtArgs a) {
 }
 
 template <int D, int G, int RN>
-static cudaError_t at_launch_rn(const AtArgs &a, cudaStream_t st) {
+static cudaError_t at_launch_rn(const AtArgs &a, int grid, cudaStream_t st) {
     static SmemOptIn opt_in;
     constexpr int SMEM = AT_WARPS * at_stages(D, G, RN) * kv_tile_bytes(D, G);
     auto kern = kv4_attend_kernel<D, G, RN>;
     cudaError_t e = ensure_dynamic_smem(kern, SMEM, opt_in);
     if (e != cudaSuccess) return e;
-    e = launch(kern, dim3(a.ctas), dim3(AT_THREADS), SMEM, st, g_tune.pdl != 0, a);
+    e = launch(kern, dim3(grid), dim3(AT_THREADS), SMEM, st, g_tune.pdl != 0, a);
     if (e != cudaSuccess) return e;
     const int rows = a.nq * a.g < 8 * RN ? a.nq * a.g : 8 * RN;
     return launch(kv4_join_kernel<D, 8 * RN>, dim3(a.c.n_seqs, a.c.heads * a.row_tiles, rows), dim3(AT_THREADS), 0, st, g_tune.pdl != 0, a);
 }
 template <int D, int G>
-static cudaError_t at_launch(const AtArgs &a, int rn, cudaStream_t st) {
-    return rn == 1 ? at_launch_rn<D, G, 1>(a, st) : at_launch_rn<D, G, 2>(a, st);
+static cudaError_t at_launch(const AtArgs &a, int rn, int grid, cudaStream_t st) {
+    return rn == 1 ? at_launch_rn<D, G, 1>(a, grid, st) : at_launch_rn<D, G, 2>(a, grid, st);
 }
 
 // Eight rows at a time where a head has no more than that, else sixteen: the cache is then read (and unpacked) half as often.
@@ -699,7 +708,7 @@ extern "C" size_t scap_kv4_attend_workspace(int n_seqs, int nq, int q_heads, int
     if (head_dim != 64 && head_dim != 128 && head_dim != 256) return 0;
     const int rn = at_row_groups(nq * (q_heads / heads));
     const int items = heads * ((nq * (q_heads / heads) + 8 * rn - 1) / (8 * rn));
-    return (size_t)2 * sm_count() * at_resident(head_dim, 1, rn) * 8 * rn * (head_dim + 2) * sizeof(float)  // (G = 1: the most CTAs)
+    return (size_t)4 * sm_count() * at_resident(head_dim, 1, rn) * 8 * rn * (head_dim + 2) * sizeof(float)  // (G = 1: the most CTAs)
            + (size_t)n_seqs * items * sizeof(int2);
 }
 
@@ -728,19 +737,25 @@ extern "C" scap_status scap_kv4_attend(const scap_kv4 *cache, const void *q, int
     a.row_tiles = (nq * a.g + 8 * rn - 1) / (8 * rn);
     a.window = window;
     a.scale = (float)(scale * 1.4426950408889634);
-    a.ctas = sm_count() * at_resident(cache->head_dim, a.c.groups, rn);
-    a.where = reinterpret_cast<int2 *>(a.part + (size_t)2 * a.ctas * 8 * rn * (cache->head_dim + 2));
+    a.resident = sm_count() * at_resident(cache->head_dim, a.c.groups, rn);
+    // What the tables have room for bounds the work: no more CTAs than that takes.
+    const long long cap = (long long)cache->table_stride * (cache->page_tokens / KV_TILE), seen = window > 0 ? ((long long)window + nq) / KV_TILE + 2 : cap;
+    a.tile_cap = (int)(cap < (1ll << 30) ? cap : (1ll << 30));
+    const long long units = (cap < seen ? cap : seen) * cache->n_seqs * cache->heads * a.row_tiles, few = (units + AT_MIN_UNITS - 1) / AT_MIN_UNITS;
+    const int most = units >= (long long)AT_TWO_WAVES * a.resident ? 2 * a.resident : a.resident;
+    const int grid = few < most ? (int)few : most;
+    a.where = reinterpret_cast<int2 *>(a.part + (size_t)4 * a.resident * 8 * rn * (cache->head_dim + 2));
     a.bf16 = dt == SCAP_BF16;
     a.limit = g_tune.tc_spin ? (uint32_t)g_tune.tc_spin : TRIES;
     a.status = tc_status_ptr();
     cudaStream_t st = reinterpret_cast<cudaStream_t>(stream);
     switch (cache->head_dim * 8 + a.c.groups) {
-        case 64 * 8 + 1: return cuda_status(at_launch<64, 1>(a, rn, st));
-        case 64 * 8 + 2: return cuda_status(at_launch<64, 2>(a, rn, st));
-        case 128 * 8 + 1: return cuda_status(at_launch<128, 1>(a, rn, st));
-        case 128 * 8 + 2: return cuda_status(at_launch<128, 2>(a, rn, st));
-        case 128 * 8 + 4: return cuda_status(at_launch<128, 4>(a, rn, st));
-        case 256 * 8 + 2: return cuda_status(at_launch<256, 2>(a, rn, st));
-        default: return cuda_status(at_launch<256, 4>(a, rn, st));
+        case 64 * 8 + 1: return cuda_status(at_launch<64, 1>(a, rn, grid, st));
+        case 64 * 8 + 2: return cuda_status(at_launch<64, 2>(a, rn, grid, st));
+        case 128 * 8 + 1: return cuda_status(at_launch<128, 1>(a, rn, grid, st));
+        case 128 * 8 + 2: return cuda_status(at_launch<128, 2>(a, rn, grid, st));
+        case 128 * 8 + 4: return cuda_status(at_launch<128, 4>(a, rn, grid, st));
+        case 256 * 8 + 2: return cuda_status(at_launch<256, 2>(a, rn, grid, st));
+        default: return cuda_status(at_launch<256, 4>(a, rn, grid, st));
     }
 }
