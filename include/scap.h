@@ -72,6 +72,7 @@ typedef struct CUstream_st *scap_stream_t;
 #define SCAP_MAX_BATCH 16
 #define SCAP_MAX_ROWS 1048576 /* of scap_fc_act */
 #define SCAP_MAX_SEQS 4096   /* of a 4-bit cache */
+#define SCAP_MAX_PAGES 1048576
 #define SCAP_MAX_EXPERTS 32
 #define SCAP_MAX_TOP_K 4
 
@@ -427,6 +428,29 @@ scap_status scap_kv4_read(const scap_kv4 *cache, void *k, int64_t ldk, void *v, 
 size_t scap_kv4_attend_workspace(int n_seqs, int nq, int q_heads, int heads, int head_dim);
 scap_status scap_kv4_attend(const scap_kv4 *cache, const void *q, int64_t ldq, void *out, int64_t ldo, float *lse, int nq, int q_heads,
                             double scale, int window, scap_dtype dt, void *ws, size_t ws_bytes, scap_stream_t stream);
+
+/* Pages of the cache: fork, free, reserve and compact keep table, lens and refs of a scap_kv4 in step on the device (heads, head_dim and
+ * group do not matter here).  A page is all of its page_stride bytes, so `pages` is the pool's own start, not that of a layer inside it.
+ * The state must be consistent: refs[p] the number of rows that hold page p, a row's entries behind its length -1, every entry before it a
+ * page; n_pages up to SCAP_MAX_PAGES.  What goes where does not depend on timing: free pages are given out from the lowest on, in the order of the
+ * request.  Row numbers outside 0..n_seqs-1 are left out.  fail_out[1] (int32, may be NULL) receives the number of requests that were
+ * not carried out.  Workspace: scap_kv4_pages_workspace(n_pages, n), n = number of forks (1 for reserve and compact).
+ *   copy     pages[dst[i]] = pages[src[i]], i < n; a destination may be named once, and be no source.  Needs pages, page_stride, n_pages only
+ *   fork     row dst[i] becomes a copy of row src[i], n <= n_seqs: the full pages are shared (refs + 1), the last and partial one is copied
+ *            into a free page.  A source may be named often.  Not carried out: a destination that is not empty (lens > 0) or was named
+ *            before, a source that is somebody's destination, a source longer than its row, no free page (the row then stays empty)
+ *   free     the pages of the rows are let go (refs - 1), the rows are empty after it; a row that is named twice is freed once
+ *   reserve  room for add[b] more tokens of every sequence b (add[n_seqs] int32): lens[b] += add[b], and free pages for them.  All of a
+ *            sequence's pages or none: one that would have to take more than are left after those before it (carried out or not) stays
+ *            as it is, and so does one whose row of the table is too short
+ *   compact  the used pages move to the front of the pool: with U of them, the used ones at U and behind go, in order, into the free
+ *            ones before U; table and refs follow.  used_out[1] (int32, may be NULL) receives U.  Only that many pages are copied      */
+size_t scap_kv4_pages_workspace(int n_pages, int n);
+scap_status scap_kv4_copy(const scap_kv4 *cache, const int *src, const int *dst, int n, scap_stream_t stream);
+scap_status scap_kv4_fork(const scap_kv4 *cache, const int *src, const int *dst, int n, int *fail_out, void *ws, size_t ws_bytes, scap_stream_t stream);
+scap_status scap_kv4_free(const scap_kv4 *cache, const int *rows, int n, scap_stream_t stream);
+scap_status scap_kv4_reserve(const scap_kv4 *cache, const int *add, int *fail_out, void *ws, size_t ws_bytes, scap_stream_t stream);
+scap_status scap_kv4_compact(const scap_kv4 *cache, int *used_out, void *ws, size_t ws_bytes, scap_stream_t stream);
 
 #ifdef __cplusplus
 }

@@ -21,6 +21,7 @@ __all__ = [
     "scap_moe_ffn", "ScapExpert", "dtype_of", "EXPORTS",
     "SCAP_ACT_NONE", "SCAP_ACT_RELU", "SCAP_ACT_SILU", "SCAP_ACT_GELU", "SCAP_ACT_GELU_TANH", "scap_fc_act_workspace", "scap_fc_act",
     "ScapKv4", "scap_kv4_page_bytes", "scap_kv4_append", "scap_kv4_read", "scap_kv4_attend_workspace", "scap_kv4_attend",
+    "scap_kv4_pages_workspace", "scap_kv4_copy", "scap_kv4_fork", "scap_kv4_free", "scap_kv4_reserve", "scap_kv4_compact",
 ]
 
 SCAP_F16, SCAP_BF16, SCAP_F32 = 0, 1, 2
@@ -35,6 +36,7 @@ EXPORTS = [
     "scap_grouped_workspace", "scap_sparse_fc_grouped", "scap_fc_host_workspace", "scap_sparse_fc_host", "scap_glu_workspace", "scap_glu_ffn", "scap_gelu_ffn_workspace",
     "scap_gelu_ffn", "scap_glu_static_capacity", "scap_glu_ffn_static", "scap_moe_workspace", "scap_moe_ffn",
     "scap_fc_act_workspace", "scap_fc_act", "scap_kv4_page_bytes", "scap_kv4_append", "scap_kv4_read", "scap_kv4_attend_workspace", "scap_kv4_attend",
+    "scap_kv4_pages_workspace", "scap_kv4_copy", "scap_kv4_fork", "scap_kv4_free", "scap_kv4_reserve", "scap_kv4_compact",
 ]
 
 
@@ -143,6 +145,11 @@ def lib():
     L.scap_kv4_attend_workspace.restype = sz
     L.scap_kv4_attend.argtypes = [vp, vp, i64, vp, i64, vp, i, i, d, i, i, vp, sz, vp]
     L.scap_kv4_attend.restype = i
+    L.scap_kv4_pages_workspace.argtypes = [i, i]
+    L.scap_kv4_pages_workspace.restype = sz
+    for n, a in (("copy", [vp, vp, vp, i, vp]), ("fork", [vp, vp, vp, i, vp, vp, sz, vp]), ("free", [vp, vp, i, vp]), ("reserve", [vp, vp, vp, vp, sz, vp]), ("compact", [vp, vp, vp, sz, vp])):
+        getattr(L, "scap_kv4_" + n).argtypes = a
+        getattr(L, "scap_kv4_" + n).restype = i
     global _call, _call_real
     try:
         from ._scap_call import call, call_real
@@ -512,3 +519,46 @@ def scap_kv4_attend(cache, q, out, scale: float, ws, window: int = 0, lse=None, 
     p, n = _ws(ws)
     _invoke_real("scap_kv4_attend", float(scale), 8, cache.address, q, _queries(q, cache.head_dim, "q"), out, _queries(out, cache.head_dim, "out"), lse, q.shape[1],
                  q.shape[2], int(window), dtype_of(q), p, n, _stream(stream))
+
+
+def scap_kv4_pages_workspace(n_pages: int, n: int) -> int:
+    return lib().scap_kv4_pages_workspace(int(n_pages), int(n))
+
+
+def _numbers(name: str, *tensors) -> int:
+    """Length that the int32 tensors share."""
+    n = tensors[0].numel()
+    for t in tensors:
+        if t.dtype is not torch.int32 or t.numel() != n or not t.is_contiguous():
+            raise ValueError("%s must be contiguous int32 tensors of one length" % name)
+    return n
+
+
+def scap_kv4_copy(cache, src, dst, stream=None) -> None:
+    """Copies page src[i] to page dst[i]."""
+    _invoke("scap_kv4_copy", cache.address, src, dst, _numbers("src and dst", src, dst), _stream(stream))
+
+
+def scap_kv4_fork(cache, src, dst, fail, ws, stream=None) -> None:
+    """Row dst[i] becomes a copy of row src[i]: full pages shared, the last one copied.  fail [1] int32 or None: requests not carried out."""
+    p, n = _ws(ws)
+    _invoke("scap_kv4_fork", cache.address, src, dst, _numbers("src and dst", src, dst), fail, p, n, _stream(stream))
+
+
+def scap_kv4_free(cache, rows, stream=None) -> None:
+    """Lets go the pages of the rows; the rows are empty after it."""
+    _invoke("scap_kv4_free", cache.address, rows, _numbers("rows", rows), _stream(stream))
+
+
+def scap_kv4_reserve(cache, add, fail, ws, stream=None) -> None:
+    """lens[b] += add[b], with free pages for the new tokens.  fail [1] int32 or None: sequences that did not get them."""
+    if _numbers("add", add) != cache.n_seqs:
+        raise ValueError("add must be int32 [n_seqs]")
+    p, n = _ws(ws)
+    _invoke("scap_kv4_reserve", cache.address, add, fail, p, n, _stream(stream))
+
+
+def scap_kv4_compact(cache, used, ws, stream=None) -> None:
+    """Moves the used pages to the front of the pool; used [1] int32 or None: how many there are."""
+    p, n = _ws(ws)
+    _invoke("scap_kv4_compact", cache.address, used, p, n, _stream(stream))
