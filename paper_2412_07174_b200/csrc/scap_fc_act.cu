@@ -37,6 +37,11 @@ constexpr int FA_THREADS = (FA_EPI_WARPS + 2) * 32;
 constexpr int FA_BK = 128;                   // channels per stage: eight MMAs per round of waits (64: the issuing lanes fall behind the tensor core)
 constexpr int FA_TN = 128;                   // output channels per CTA
 constexpr int FA_ABYTES = FA_TN * FA_BK * 2; // 32 KB of W per stage
+// The tensor core truncates where it adds to an accumulator, always towards zero, so a sum is off by about 2^-25 of itself per addition: 3e-6
+// at K = 2560, nothing beside a rounding to 16 bits but much beside one to fp32.  For an fp32 result an accumulator takes 512 channels (32
+// additions) and the epilogue warps add those sums up in registers, rounding to nearest, while the next 512 are under way.
+constexpr int FA_CHUNK = 4;
+constexpr int FA_MAX_BN_F32 = 192;           // rows per tile then: the sums of half of them are a thread's registers
 constexpr int FA_MAX_STAGES = 12;
 constexpr int FA_SMEM = 226 * 1024;          // of the 227 KB that a CTA may have; the barriers are inside
 
@@ -118,14 +123,30 @@ __device__ __forceinline__ void fa_ld16(uint32_t (&v)[16], uint32_t addr) {
         : "r"(addr));
 }
 
-__device__ __forceinline__ float fa_act(float u, int act) {
+// Activations of four values.  A function of its own, not inlined: sixteen copies of it in an epilogue's loop do not fit the
+// instruction cache.  (The fast division is good to 2 units of the last place; where its divisor overflows the result is 0, as it should be.)
+__device__ __noinline__ float4 fa_act4(float4 v, int act) {
+    float u[4] = {v.x, v.y, v.z, v.w};
     switch (act) {
-        case SCAP_ACT_RELU: return u > 0.0f || u != u ? u : 0.0f;
-        case SCAP_ACT_SILU: return u / (1.0f + expf(-u));
-        case SCAP_ACT_GELU: return 0.5f * u * erfcf(-0.70710678118654752f * u);  // 1 + erf(a) = erfc(-a), without its cancellation
-        case SCAP_ACT_GELU_TANH: return u / (1.0f + expf(-1.5957691216057308f * (u + 0.044715f * u * u * u)));  // (1 + tanh a) / 2 = 1 / (1 + e^(-2a))
-        default: return u;
+        case SCAP_ACT_RELU:
+#pragma unroll
+            for (int j = 0; j < 4; ++j) u[j] = u[j] > 0.0f || u[j] != u[j] ? u[j] : 0.0f;
+            break;
+        case SCAP_ACT_SILU:
+#pragma unroll
+            for (int j = 0; j < 4; ++j) u[j] = __fdividef(u[j], 1.0f + expf(-u[j]));
+            break;
+        case SCAP_ACT_GELU:
+#pragma unroll
+            for (int j = 0; j < 4; ++j) u[j] = 0.5f * u[j] * erfcf(-0.70710678118654752f * u[j]);  // 1 + erf(a) = erfc(-a), without its cancellation
+            break;
+        case SCAP_ACT_GELU_TANH:  // (1 + tanh a) / 2 = 1 / (1 + e^(-2a))
+#pragma unroll
+            for (int j = 0; j < 4; ++j) u[j] = __fdividef(u[j], 1.0f + expf(-1.5957691216057308f * (u[j] + 0.044715f * u[j] * u[j] * u[j])));
+            break;
+        default: break;
     }
+    return make_float4(u[0], u[1], u[2], u[3]);
 }
 
 // Elements of y and r: fp32, or 16 bits of the type of x.  A load gives the bits, 0 where it is off (no branch, and nothing that
@@ -173,6 +194,7 @@ __global__ void __launch_bounds__(FA_THREADS, 1) fc_act_kernel(const FaArgs a, c
     const int tiles = a.tiles_n * a.tiles_m;
     const int nkb_all = (a.K + FA_BK - 1) / FA_BK;
     const int kb0 = (int)((long long)nkb_all * srank / S), nkb = (int)((long long)nkb_all * (srank + 1) / S) - kb0;
+    const int chunk = F32 ? FA_CHUNK : nkb;  // stages that are added up in one accumulator
     volatile int *abort_flag = &sh->abort_flag;
 
     if (tid == 0) {
@@ -261,31 +283,36 @@ __global__ void __launch_bounds__(FA_THREADS, 1) fc_act_kernel(const FaArgs a, c
                                    ((uint32_t)(a.BN >> 3) << 17) | ((uint32_t)((FA_TN * CG) >> 4) << 24);
             const uint64_t dw0 = tc_desc(smem_u32(ring), FA_ABYTES / 2, 1024, 2), dx0 = tc_desc(smem_u32(ring) + FA_ABYTES, 16, 1024, 2);
             const uint32_t full0 = smem_u32(&sh->full[0]), empty0 = smem_u32(&sh->empty[0]);
-            int st = 0, n = 0;
+            int st = 0, n = 0;  // n: accumulations so far, in turn in the two accumulators
             uint32_t par = 0;
             bool ok = true, issued = false;
-            for (int t = first; t < tiles && ok; t += clusters, ++n) {
-                const int acc = n & 1;
-                if (n >= 2) {
-                    ok = fa_wait(smem_u32(&sh->tempty[acc]), (uint32_t)((n >> 1) - 1) & 1u, a, abort_flag);
-                    if (!ok) break;
-                    tc_fence_after();
-                }
-                const uint32_t d = tmem + (uint32_t)acc * (uint32_t)a.BN;
-                for (int kb = 0; kb < nkb; ++kb) {
-                    ok = fa_wait(full0 + 8 * st, par, a, abort_flag);
-                    if (!ok) break;
-                    tc_fence_after();
-                    const uint64_t dw = dw0 + (uint64_t)((uint32_t)st * (stage >> 4)), dx = dx0 + (uint64_t)((uint32_t)st * (stage >> 4));
-                    // (the channels beyond K of the last block are zeros in both operands)
+            for (int t = first; t < tiles && ok; t += clusters) {
+                for (int kb = 0; kb < nkb;) {
+                    const int acc = n & 1, stop = min(nkb, kb + chunk);
+                    if (n >= 2) {
+                        ok = fa_wait(smem_u32(&sh->tempty[acc]), (uint32_t)((n >> 1) - 1) & 1u, a, abort_flag);
+                        if (!ok) break;
+                        tc_fence_after();
+                    }
+                    const uint32_t d = tmem + (uint32_t)acc * (uint32_t)a.BN;
+                    bool more = false;
+                    for (; kb < stop; ++kb) {
+                        ok = fa_wait(full0 + 8 * st, par, a, abort_flag);
+                        if (!ok) break;
+                        tc_fence_after();
+                        const uint64_t dw = dw0 + (uint64_t)((uint32_t)st * (stage >> 4)), dx = dx0 + (uint64_t)((uint32_t)st * (stage >> 4));
+                        // (the channels beyond K of the last block are zeros in both operands)
 #pragma unroll
-                    for (uint32_t k = 0; k < FA_BK / 16; ++k)
-                        fa_mma<CG>(d, dw + k * (2048 >> 4), dx + (k >> 2) * ((uint32_t)bn_cta * 128 >> 4) + (k & 3) * (32 >> 4), idesc, (kb > 0 || k > 0) ? 1u : 0u);
-                    fa_commit<CG>(empty0 + 8 * st);
-                    issued = true;
-                    if (++st == a.stages) { st = 0; par ^= 1u; }
+                        for (uint32_t k = 0; k < FA_BK / 16; ++k)
+                            fa_mma<CG>(d, dw + k * (2048 >> 4), dx + (k >> 2) * ((uint32_t)bn_cta * 128 >> 4) + (k & 3) * (32 >> 4), idesc, (more || k > 0) ? 1u : 0u);
+                        fa_commit<CG>(empty0 + 8 * st);
+                        more = issued = true;
+                        if (++st == a.stages) { st = 0; par ^= 1u; }
+                    }
+                    if (!ok) break;
+                    fa_commit<CG>(smem_u32(&sh->tfull[acc]));
+                    ++n;
                 }
-                if (ok) fa_commit<CG>(smem_u32(&sh->tfull[acc]));
             }
             if (!ok && issued) {  // let the MMAs under way finish before shared memory and TMEM go
                 if constexpr (CG == 2)
@@ -302,13 +329,13 @@ __global__ void __launch_bounds__(FA_THREADS, 1) fc_act_kernel(const FaArgs a, c
         const uint32_t lane_at = tmem + ((uint32_t)(quarter * 32) << 16);
         griddep_wait();  // b and r may come from the work just before; y may still be read by it
         int n = 0;
-        for (int t = first; t < tiles; t += clusters, ++n) {
+        for (int t = first; t < tiles; t += clusters) {
             int tn, tm;
             fa_tile(a, t, tn, tm);
             const int col = tn * FA_TN * CG + rank * FA_TN + quarter * 32 + lane;  // output channel of this lane
             const bool on = col < a.N;
             const float bias = on && a.b ? ld_act(a.b + col) : 0.0f;
-            const int m0 = tm * a.BN, rows = min(a.BN, a.M - m0), acc = n & 1;
+            const int m0 = tm * a.BN, rows = min(a.BN, a.M - m0);
             // The residual of 16 rows is asked for ahead of their accumulators: while the MMAs run, and while the 16 rows before are worked on.
             uint32_t r[16];
             auto ask_r = [&](int c) {
@@ -316,44 +343,98 @@ __global__ void __launch_bounds__(FA_THREADS, 1) fc_act_kernel(const FaArgs a, c
                 for (int j = 0; j < 16; ++j) r[j] = fa_load<F32>(a.r, (long long)(m0 + c + j) * a.ldr + col, on && c + j < rows);
             };
             if (S == 1 && a.r) ask_r(half * 16);
-            bool ok = fa_wait(smem_u32(&sh->tfull[acc]), (uint32_t)(n >> 1) & 1u, a, abort_flag);
-            ok = __all_sync(0xffffffffu, ok);
-            if (!ok) break;
-            tc_fence_after();
-            if (S == 1) {
-                for (int c = half * 16; c < rows; c += 32) {
-                    uint32_t v[16];
-                    fa_ld16(v, lane_at + (uint32_t)(acc * a.BN + c));
-                    asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory");
-                    float u[16];
-#pragma unroll
-                    for (int j = 0; j < 16; ++j) u[j] = fa_act(__uint_as_float(v[j]) + bias, a.act);
-                    if (a.r) {
-#pragma unroll
-                        for (int j = 0; j < 16; ++j) u[j] += fa_widen<BF16, F32>(r[j]);
-                        ask_r(c + 32);
-                    }
-#pragma unroll
-                    for (int j = 0; j < 16; ++j)
-                        if (on && c + j < rows) fa_store<BF16, F32>(a.y, (long long)(m0 + c + j) * a.ldy + col, u[j]);
-                }
+            bool ok = true;
+            auto wait_acc = [&]() {
+                ok = fa_wait(smem_u32(&sh->tfull[n & 1]), (uint32_t)(n >> 1) & 1u, a, abort_flag);
+                ok = __all_sync(0xffffffffu, ok);
+                tc_fence_after();
+                return ok;
+            };
+            auto done_acc = [&]() {
                 tc_fence_before();
                 __syncwarp();
                 if (lane == 0) {
-                    if constexpr (CG == 2) fa_arrive_cluster(cluster_addr(smem_u32(&sh->tempty[acc]), 0));
-                    else mbar_arrive(&sh->tempty[acc]);
+                    if constexpr (CG == 2) fa_arrive_cluster(cluster_addr(smem_u32(&sh->tempty[n & 1]), 0));
+                    else mbar_arrive(&sh->tempty[n & 1]);
                 }
-            } else {
-                // partial tile of this rank into the ring, which nobody uses any more: [row of y][channel]
-                float *part = reinterpret_cast<float *>(ring);
-                for (int c = half * 16; c < rows; c += 32) {
-                    uint32_t v[16];
-                    fa_ld16(v, lane_at + (uint32_t)c);
-                    asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory");
+                ++n;
+            };
+            // sixteen rows: either into y, or (a rank of several) as part of the sum into the ring, which nobody uses any more: [row of y][channel]
+            auto finish = [&](int c, const float (&v)[16]) {
+                if (S > 1) {
+                    float *part = reinterpret_cast<float *>(ring);
 #pragma unroll
                     for (int j = 0; j < 16; ++j)
-                        if (c + j < rows) part[(c + j) * FA_TN + quarter * 32 + lane] = __uint_as_float(v[j]);
+                        if (c + j < rows) part[(c + j) * FA_TN + quarter * 32 + lane] = v[j];
+                    return;
                 }
+                float u[16];
+#pragma unroll
+                for (int j = 0; j < 16; ++j) u[j] = v[j] + bias;
+                if (a.act != SCAP_ACT_NONE) {
+#pragma unroll
+                    for (int j = 0; j < 16; j += 4) {
+                        const float4 w = fa_act4(make_float4(u[j], u[j + 1], u[j + 2], u[j + 3]), a.act);
+                        u[j] = w.x; u[j + 1] = w.y; u[j + 2] = w.z; u[j + 3] = w.w;
+                    }
+                }
+                if (a.r) {
+#pragma unroll
+                    for (int j = 0; j < 16; ++j) u[j] += fa_widen<BF16, F32>(r[j]);
+                    ask_r(c + 32);
+                }
+#pragma unroll
+                for (int j = 0; j < 16; ++j)
+                    if (on && c + j < rows) fa_store<BF16, F32>(a.y, (long long)(m0 + c + j) * a.ldy + col, u[j]);
+            };
+            if constexpr (F32) {
+                constexpr int NC = FA_MAX_BN_F32 / 32;
+                float sum[NC][16];
+#pragma unroll
+                for (int i = 0; i < NC; ++i)
+#pragma unroll
+                    for (int j = 0; j < 16; ++j) sum[i][j] = 0.0f;
+                for (int kb = 0; kb < nkb; kb += chunk) {
+                    if (!wait_acc()) break;
+#pragma unroll
+                    for (int i = 0; i < NC; i += 2) {
+                        const int c = half * 16 + 32 * i;
+                        if (c < rows) {
+                            uint32_t v[2][16];
+                            const bool both = c + 32 < rows;
+                            fa_ld16(v[0], lane_at + (uint32_t)((n & 1) * a.BN + c));
+                            fa_ld16(v[1], lane_at + (uint32_t)((n & 1) * a.BN + (both ? c + 32 : c)));
+                            asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory");
+#pragma unroll
+                            for (int j = 0; j < 16; ++j) {
+                                sum[i][j] += __uint_as_float(v[0][j]);
+                                sum[i + 1][j] += both ? __uint_as_float(v[1][j]) : 0.0f;
+                            }
+                        }
+                    }
+                    done_acc();
+                }
+                if (!ok) break;
+#pragma unroll 1
+                for (int c = half * 16; c < rows; c += 32) {  // (rolled, the sums move up: the code unrolled does not fit the instruction cache)
+                    finish(c, sum[0]);
+#pragma unroll
+                    for (int i = 0; i + 1 < NC; ++i)
+#pragma unroll
+                        for (int j = 0; j < 16; ++j) sum[i][j] = sum[i + 1][j];
+                }
+            } else {
+                if (!wait_acc()) break;
+                for (int c = half * 16; c < rows; c += 32) {
+                    uint32_t v[16];
+                    fa_ld16(v, lane_at + (uint32_t)((n & 1) * a.BN + c));
+                    asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory");
+                    float x[16];
+#pragma unroll
+                    for (int j = 0; j < 16; ++j) x[j] = __uint_as_float(v[j]);
+                    finish(c, x);
+                }
+                done_acc();
             }
         }
     }
@@ -395,11 +476,18 @@ __global__ void __launch_bounds__(FA_THREADS, 1) fc_act_kernel(const FaArgs a, c
 #pragma unroll
                         for (int i = 0; i < 4; ++i) u[i] += s0 + s < S ? v[s][i] : 0.0f;
                 }
+                if (a.act != SCAP_ACT_NONE) {
+                    const float4 w = fa_act4(make_float4(u[0] + bias, u[1] + bias, u[2] + bias, u[3] + bias), a.act);
+                    u[0] = w.x; u[1] = w.y; u[2] = w.z; u[3] = w.w;
+                } else {
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) u[i] += bias;
+                }
 #pragma unroll
                 for (int i = 0; i < 4; ++i) {
                     const int c = c0 + 2 * S * i;
                     if (c < rows && col < a.N) {
-                        float w = fa_act(u[i] + bias, a.act);
+                        float w = u[i];
                         if (a.r) w += fa_widen<BF16, F32>(r[i]);
                         fa_store<BF16, F32>(a.y, (long long)(m0 + c) * a.ldy + col, w);
                     }
@@ -442,13 +530,13 @@ static int fa_stages(int cg, int BN) {
 
 // The form with the shortest estimate, in cycles: waves of tiles x blocks of 128 channels x the slower of a block's MMAs and its loads (60
 // bytes per cycle and SM, from L2), W at the rate of the memory, and what the epilogue and the sum over ranks cost.
-static FaPlan fa_plan(int M, int K, int N) {
+static FaPlan fa_plan(int M, int K, int N, bool f32) {
     const int sms = sm_count(), nkb = (K + FA_BK - 1) / FA_BK;
     FaPlan best = {1, 16, 1, 0};
     const double floor = 0.3 * K * (double)N * 2 / 1000.0;  // W at the rate of the memory, in cycles
     double best_t = 1e300;
     for (int cg = 1; cg <= 2; ++cg)
-        for (int BN = 16 * cg; BN <= 256; BN += 16 * cg) {
+        for (int BN = 16 * cg; BN <= (f32 ? FA_MAX_BN_F32 : 256); BN += 16 * cg) {
             if (BN >= M + 16 * cg) break;
             const long long tiles = (long long)((N + FA_TN * cg - 1) / (FA_TN * cg)) * ((M + BN - 1) / BN);
             const int most = cg == 1 ? MAX_CLUSTER : 1;
@@ -536,7 +624,7 @@ extern "C" scap_status scap_fc_act(const void *x, int64_t ldx, const void *W, co
     if (dev != SCAP_OK) return dev;
     cudaStream_t st = reinterpret_cast<cudaStream_t>(stream);
 
-    const FaPlan p = fa_plan(M, K, N);
+    const FaPlan p = fa_plan(M, K, N, ydt == SCAP_F32);
     FaArgs a = {};
     a.b = b; a.r = r; a.y = y; a.ldr = ldr; a.ldy = ldy;
     a.M = M; a.K = K; a.N = N; a.act = act;
