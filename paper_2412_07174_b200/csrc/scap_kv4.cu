@@ -1,8 +1,9 @@
 // The 4-bit key / value cache: new tokens into it, and the values it holds out of it.
 //
-// Both kernels take their rows in runs: the rows of one sequence that fall into one 32-token tile.  One warp has a run and one head,
-// because a word of V codes holds eight tokens: whoever writes one of them has to write back the other seven.  A lane has D/32
-// neighbouring channels.  Bound by memory (prompts) or by the latency of a few dependent loads (single tokens).
+// Both kernels take their rows in runs: the rows of one sequence that fall into one 32-token tile.  A block has a run and one head: a
+// word of V codes holds the eight tokens 8 j + 2 t + o, and whoever writes one of them has to write back the other seven, so warp t of
+// four has those.  A lane has D/32 neighbouring channels.  Bound by instruction issue (prompts: about 100 instructions per token, head and
+// side, 524000 of these for 8191 tokens of 32 heads) or by the latency of a few dependent loads (single tokens).
 //
 // Quantisation is decided exactly as its definition in real numbers: (hi - lo) / 15 in binary64 and rounded to 20 bits there, and
 // x / s in binary32 unless it comes near a tie, which is then decided in binary64.
@@ -10,17 +11,18 @@
 
 namespace scap {
 
-constexpr int KV_THREADS = 128;
+constexpr int KV_THREADS = 128;  // four warps: one for each word of eight tokens
 
 struct KvRows {
     const void *k, *v;       // append: read; read: written
     long long ldk, ldv;      // elements between tokens
     const int *row_start;    // [n_seqs + 1], or NULL: row b is the one new token of sequence b
-    int rows, per_warp;      // rows of k and v; rows a warp looks through for the beginnings of runs
+    int rows, per_block;     // rows of k and v; rows among which a block looks for the beginnings of runs
 };
 
 struct KvRun {
-    int row, seq, pos, n;  // first row, its sequence and position, number of rows
+    int seq, pos, n;  // sequence and position of the first row, number of rows; 0 rows: no run begins here
+    int next;         // where to look on
 };
 
 // Sequence of a row: the last one that does not begin behind it (one load of 32 lanes per factor of 32).
@@ -37,39 +39,39 @@ __device__ __forceinline__ int kv_find(const int *start, int n, int row, int lan
 }
 
 // The run that begins at `row`, if one does.
-__device__ __forceinline__ bool kv_run(const KvCache &c, const KvRows &r, int row, int lane, KvRun &run) {
-    int first = row, end = row + 1;
+__device__ __forceinline__ KvRun kv_run(const KvCache &c, const KvRows &r, int row, int lane) {
+    KvRun run;
+    int first = row, stop = row + 1;
     run.seq = row;
     if (r.row_start) {
         run.seq = kv_find(r.row_start, c.n_seqs, row, lane);
         first = __ldcg(r.row_start + run.seq);
-        end = min(__ldcg(r.row_start + run.seq + 1), r.rows);
+        stop = __ldcg(r.row_start + run.seq + 1);
     }
-    if (row < first || row >= end) return false;  // before the first sequence, or behind the last one
-    const int all = r.row_start ? __ldcg(r.row_start + run.seq + 1) - first : 1;
-    run.row = row;
-    run.pos = __ldcg(c.lens + run.seq) - all + (row - first);
-    if (run.pos < 0) return false;
-    if (row != first && run.pos % KV_TILE != 0) return false;
-    run.n = min(KV_TILE - run.pos % KV_TILE, end - row);
-    return true;
+    const int len = __ldcg(c.lens + run.seq), end = min(stop, r.rows);
+    run.n = 0;
+    run.pos = 0;
+    run.next = row < first ? first : r.rows;  // before the first sequence, or behind the last one
+    if (row < first || row >= end) return run;
+    const long long pos = (long long)len - ((long long)stop - first) + (row - first);
+    if (pos < 0) {  // (more rows than the sequence has tokens: those in front have no place)
+        run.next = (int)min((long long)end, row - pos);
+        return run;
+    }
+    run.pos = (int)pos;
+    run.next = min(end, row + KV_TILE - run.pos % KV_TILE);
+    if (row == first || run.pos % KV_TILE == 0) run.n = run.next - row;
+    return run;
 }
 
 // s of a group whose values reach from lo to hi: (hi - lo) / 15 to 20 significant bits (to a multiple of 2^-145 where that is coarser).
+// The quotient is a product with the rounded 1 / 15 and one correction of it, which gives the correctly rounded one (Markstein).
 __device__ __forceinline__ float kv_scale(float lo, float hi) {
-    const double r = ((double)hi - (double)lo) / 15.0;
+    const double d = (double)hi - (double)lo, q = d * (1.0 / 15.0), r = fma(fma(-15.0, q, d), 1.0 / 15.0, q);
     if (r < 1.1754943508222875e-38) return (float)(rint(r * 0x1p145) * 0x1p-145);
     unsigned long long u = (unsigned long long)__double_as_longlong(r);
     u += 0xffffffffull + ((u >> 33) & 1ull);
     return (float)__longlong_as_double((long long)(u & ~0x1ffffffffull));
-}
-
-// round(x / s), ties to even, as in real numbers.  inv = 1 / s; |x / s| is at most a little over 15, so the product is off by less than
-// 3e-6, and a result that far from a tie is right.
-__device__ __forceinline__ float kv_round(float x, float s, float inv) {
-    const float t = x * inv, n = rintf(t);
-    if (fabsf(t - n) < 0.4999f) return n;
-    return (float)rint((double)x / (double)s);
 }
 
 template <bool BF16>
@@ -77,6 +79,12 @@ __device__ __forceinline__ uint32_t kv_min2(uint32_t a, uint32_t b) {  // of bot
     uint32_t r;
     if constexpr (BF16) asm("min.NaN.bf16x2 %0, %1, %2;" : "=r"(r) : "r"(a), "r"(b));
     else asm("min.NaN.f16x2 %0, %1, %2;" : "=r"(r) : "r"(a), "r"(b));
+    return r;
+}
+
+__device__ __forceinline__ float kv_rcp(float v) {
+    float r;
+    asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(v));
     return r;
 }
 
@@ -100,12 +108,12 @@ __device__ __forceinline__ KvVec<CPL> kv_load(const void *p, long long i, bool o
 
 // Codes of a lane's channels (nibble i = channel i) and the word of its group.  All lanes of the warp take part.
 template <int CPL, bool BF16>
-__device__ __forceinline__ uint32_t kv_quantise(const KvVec<CPL> &x, int group_lanes, uint32_t &word) {
+__device__ __forceinline__ uint32_t kv_quantise(const KvVec<CPL> &v, int group_lanes, uint32_t &word) {
     // smallest value and smallest negative in one register, per group of lanes
     uint32_t m = 0;  // (0, 0): the range always holds zero
 #pragma unroll
     for (int k = 0; k < CPL / 2; ++k) {
-        const uint32_t a = x.w[k];
+        const uint32_t a = v.w[k];
         m = kv_min2<BF16>(m, __byte_perm(a, a ^ 0x80008000u, 0x5410));  // (x0, -x0)
         m = kv_min2<BF16>(m, __byte_perm(a, a ^ 0x80008000u, 0x7632));  // (x1, -x1)
     }
@@ -124,19 +132,38 @@ __device__ __forceinline__ uint32_t kv_quantise(const KvVec<CPL> &x, int group_l
         word = 0;
         return 0;
     }
-    const bool tiny = s < 0x1p-100f;  // no use of 1 / s: binary64 throughout
-    const float inv = tiny ? 0.0f : 1.0f / s;
-    auto rnd = [&](float v) { return tiny ? (float)rint((double)v / (double)s) : kv_round(v, s, inv); };
-    const float zero = fminf(15.0f, fmaxf(0.0f, rnd(-lo)));
+    // round(x / s), ties to even, as in real numbers: by the product with 1 / s (good to 2^-23), which is at most a little over 15, so
+    // it is off by less than 3e-6 - right unless it comes that near a tie; rounded by adding 1.5 2^23, whose last bit is one.
+    constexpr float BIG = 12582912.0f;
+    const float inv = kv_rcp(s);
+    float x[CPL];
+#pragma unroll
+    for (int k = 0; k < CPL / 2; ++k) widen2<BF16>(v.w[k], x[2 * k], x[2 * k + 1]);
+    const float tz = -lo * inv, nz = (tz + BIG) - BIG;
+    bool near = fabsf(tz - nz) > 0.4999f || s < 0x1p-100f;  // (no use of 1 / s there)
+    int zero = (int)(__float_as_uint(tz + BIG) - __float_as_uint(BIG)), n[CPL];
+#pragma unroll
+    for (int k = 0; k < CPL; ++k) {
+        const float t = x[k] * inv, m = t + BIG;
+        n[k] = (int)(__float_as_uint(m) - __float_as_uint(BIG));
+        near = near || fabsf(t - (m - BIG)) > 0.4999f;
+    }
+    if (near) {
+        zero = (int)rint(-(double)lo / (double)s);
+#pragma unroll 1
+        for (int k = 0; k < CPL; ++k) {
+            const int q = (int)rint((double)x[0] / (double)s);
+#pragma unroll
+            for (int i = 0; i < CPL; ++i) n[i] = i == k ? q : n[i];
+#pragma unroll
+            for (int i = 0; i + 1 < CPL; ++i) x[i] = x[i + 1];  // (rolled: one copy of the division)
+        }
+    }
+    zero = min(15, max(0, zero));
     word = __float_as_uint(s) | (uint32_t)zero;
     uint32_t codes = 0;
 #pragma unroll
-    for (int k = 0; k < CPL / 2; ++k) {
-        float a, b;
-        widen2<BF16>(x.w[k], a, b);
-        codes |= (uint32_t)fminf(15.0f, fmaxf(0.0f, rnd(a) + zero)) << (8 * k);
-        codes |= (uint32_t)fminf(15.0f, fmaxf(0.0f, rnd(b) + zero)) << (8 * k + 4);
-    }
+    for (int k = 0; k < CPL; ++k) codes |= (uint32_t)min(15, max(0, n[k] + zero)) << (4 * k);
     return codes;
 }
 
@@ -145,65 +172,82 @@ __global__ void __launch_bounds__(KV_THREADS) kv4_append_kernel(const KvCache c,
     constexpr int CPL = D / 32;  // channels of a lane
     griddep_wait();
     griddep_launch_dependents();
-    const int lane = threadIdx.x & 31, h = blockIdx.y;
-    const int group_lanes = group / CPL, tile_bytes = kv_tile_bytes(D, c.groups);
-    const long long row0 = ((long long)blockIdx.x * (KV_THREADS / 32) + (threadIdx.x >> 5)) * r.per_warp;
-    for (long long row = row0; row < row0 + r.per_warp && row < r.rows; ++row) {
-        KvRun run;
-        if (!kv_run(c, r, (int)row, lane, run)) continue;
+    const int lane = threadIdx.x & 31, t = threadIdx.x >> 5, h = blockIdx.y;
+    const int group_lanes = group / CPL, tile_bytes = kv_tile_bytes(D, c.groups), ch = lane * CPL, g = ch / group;
+    const bool writes = lane % group_lanes == 0;
+    const int row0 = blockIdx.x * r.per_block, row1 = min(row0 + r.per_block, r.rows);
+    for (int row = row0; row < row1;) {
+        const KvRun run = kv_run(c, r, row, lane);
+        const int first = row, tok0 = run.pos % KV_TILE;
+        row = run.next;
+        if (run.n == 0) continue;
+        // this warp's tokens 8 j + 2 t + o that lie in the run, as nibbles of the words of V codes
+        uint32_t mask = 0;
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            const int n = 8 * (i >> 1) + 2 * t + (i & 1) - tok0;
+            if (n >= 0 && n < run.n) mask |= 15u << (4 * ((i >> 1) + 4 * (i & 1)));
+        }
+        if (mask == 0) continue;
         const int page = kv_page(c, run.seq, run.pos);
         if (page < 0) continue;
         unsigned char *tile = kv_tile(c, page, h, run.pos, tile_bytes);
-        uint32_t *kw = reinterpret_cast<uint32_t *>(tile + kv_k_words(D)), *vw = reinterpret_cast<uint32_t *>(tile + kv_v_words(D, c.groups));
-        const int tok0 = run.pos % KV_TILE, ch = lane * CPL, g = ch / group;
-        const bool writes = lane % group_lanes == 0;
-        for (int t = 0; t < 4; ++t) {
-            // the eight tokens 8 j + 2 t + o of a word of V codes
-            KvVec<CPL> kx[8], vx[8];
+        uint32_t *kw = reinterpret_cast<uint32_t *>(tile + kv_k_words(D)) + g * KV_TILE, *vw = reinterpret_cast<uint32_t *>(tile + kv_v_words(D, c.groups)) + g * KV_TILE;
+        uint32_t *vcodes = reinterpret_cast<uint32_t *>(tile + kv_v_codes(D));
+        uint32_t vcode[CPL];
 #pragma unroll
-            for (int i = 0; i < 8; ++i) {
-                const int n = 8 * (i >> 1) + 2 * t + (i & 1) - tok0;  // row of the run
-                const bool on = n >= 0 && n < run.n;
-                kx[i] = kv_load<CPL>(r.k, (long long)(run.row + n) * r.ldk + (long long)h * D + ch, on);
-                vx[i] = kv_load<CPL>(r.v, (long long)(run.row + n) * r.ldv + (long long)h * D + ch, on);
-            }
-            uint32_t vcode[CPL], mask = 0;
+        for (int k = 0; k < CPL; ++k) vcode[k] = mask == 0xffffffffu ? 0u : __ldcg(vcodes + kv_v_word(ch + k, t)) & ~mask;
+        // (rolled, with the next token's values under way: unrolled the code does not fit the instruction cache)
+        auto tok_of = [&](int i) { return 8 * (i >> 1) + 2 * t + (i & 1); };
+        auto ask = [&](int i, KvVec<CPL> &kx, KvVec<CPL> &vx) {
+            const int n = tok_of(i) - tok0;
+            const bool on = i < 8 && n >= 0 && n < run.n;
+            kx = kv_load<CPL>(r.k, (long long)(first + n) * r.ldk + (long long)h * D + ch, on);
+            vx = kv_load<CPL>(r.v, (long long)(first + n) * r.ldv + (long long)h * D + ch, on);
+        };
+        KvVec<CPL> kx[2], vx[2];
+        ask(0, kx[0], vx[0]);
+        ask(1, kx[1], vx[1]);
+#pragma unroll 1
+        for (int i = 0; i < 8; ++i) {
+            const KvVec<CPL> k0 = kx[0], v0 = vx[0];
+            kx[0] = kx[1];
+            vx[0] = vx[1];
+            ask(i + 2, kx[1], vx[1]);
+            const int tok = tok_of(i);
+            if (tok < tok0 || tok >= tok0 + run.n) continue;  // (the same for all lanes)
+            uint32_t word;
+            const uint32_t kc = kv_quantise<CPL, BF16>(k0, group_lanes, word);
+            unsigned char *to = tile + tok * (D / 2) + kv_k_byte(D, ch);
+            if constexpr (CPL == 2) *to = (unsigned char)kc;
+            else if constexpr (CPL == 4) *reinterpret_cast<unsigned short *>(to) = (unsigned short)kc;
+            else *reinterpret_cast<uint32_t *>(to) = kc;
+            if (writes) kw[kv_word_at(tok)] = word;
+            const uint32_t vc = kv_quantise<CPL, BF16>(v0, group_lanes, word);
+            if (writes) vw[kv_word_at(tok)] = word;
+            const int nib = 4 * ((i >> 1) + 4 * (i & 1));
 #pragma unroll
-            for (int k = 0; k < CPL; ++k) vcode[k] = 0;
-#pragma unroll
-            for (int i = 0; i < 8; ++i) {
-                const int tok = 8 * (i >> 1) + 2 * t + (i & 1);
-                if (tok < tok0 || tok >= tok0 + run.n) continue;  // (the same for all lanes)
-                const int nib = 4 * ((i >> 1) + 4 * (i & 1));
-                uint32_t word;
-                const uint32_t kc = kv_quantise<CPL, BF16>(kx[i], group_lanes, word);
-                unsigned char *to = tile + tok * (D / 2) + kv_k_byte(D, ch);
-                if constexpr (CPL == 2) *to = (unsigned char)kc;
-                else if constexpr (CPL == 4) *reinterpret_cast<unsigned short *>(to) = (unsigned short)kc;
-                else *reinterpret_cast<uint32_t *>(to) = kc;
-                if (writes) kw[g * KV_TILE + kv_word_at(tok)] = word;
-                const uint32_t vc = kv_quantise<CPL, BF16>(vx[i], group_lanes, word);
-                if (writes) vw[g * KV_TILE + kv_word_at(tok)] = word;
-#pragma unroll
-                for (int k = 0; k < CPL; ++k) vcode[k] |= ((vc >> (4 * k)) & 15u) << nib;
-                mask |= 15u << nib;
-            }
-            if (mask) {
-                uint32_t *vcodes = reinterpret_cast<uint32_t *>(tile + kv_v_codes(D));
-#pragma unroll
-                for (int k = 0; k < CPL; ++k) {
-                    uint32_t *at = vcodes + kv_v_word(ch + k, t);
-                    *at = mask == 0xffffffffu ? vcode[k] : (__ldcg(at) & ~mask) | vcode[k];
-                }
-            }
+            for (int k = 0; k < CPL; ++k) vcode[k] |= ((vc >> (4 * k)) & 15u) << nib;
         }
+#pragma unroll
+        for (int k = 0; k < CPL; ++k) vcodes[kv_v_word(ch + k, t)] = vcode[k];
     }
 }
 
-template <int D, bool BF16>
-__device__ __forceinline__ unsigned short kv_narrow(float v) {
-    if constexpr (BF16) return __bfloat16_as_ushort(__float2bfloat16_rn(v));
-    else return __half_as_ushort(__float2half_rn(v));
+// Two values to a word of two 16-bit ones.
+template <bool BF16>
+__device__ __forceinline__ uint32_t kv_narrow2(float a, float b) {
+    uint32_t r;
+    if constexpr (BF16) asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(r) : "f"(b), "f"(a));
+    else asm("cvt.rn.f16x2.f32 %0, %1, %2;" : "=r"(r) : "f"(b), "f"(a));
+    return r;
+}
+template <int CPL>
+__device__ __forceinline__ void kv_put(void *p, long long i, const uint32_t (&w)[CPL / 2]) {
+    unsigned short *q = reinterpret_cast<unsigned short *>(p) + i;
+    if constexpr (CPL == 2) *reinterpret_cast<uint32_t *>(q) = w[0];
+    else if constexpr (CPL == 4) *reinterpret_cast<uint2 *>(q) = make_uint2(w[0], w[1]);
+    else *reinterpret_cast<uint4 *>(q) = make_uint4(w[0], w[1], w[2], w[3]);
 }
 
 template <int D, bool BF16>
@@ -211,60 +255,47 @@ __global__ void __launch_bounds__(KV_THREADS) kv4_read_kernel(const KvCache c, c
     constexpr int CPL = D / 32;
     griddep_wait();
     griddep_launch_dependents();
-    const int lane = threadIdx.x & 31, h = blockIdx.y, tile_bytes = kv_tile_bytes(D, c.groups);
-    unsigned short *ko = reinterpret_cast<unsigned short *>(const_cast<void *>(r.k)), *vo = reinterpret_cast<unsigned short *>(const_cast<void *>(r.v));
-    const long long row0 = ((long long)blockIdx.x * (KV_THREADS / 32) + (threadIdx.x >> 5)) * r.per_warp;
-    for (long long row = row0; row < row0 + r.per_warp && row < r.rows; ++row) {
-        KvRun run;
-        if (!kv_run(c, r, (int)row, lane, run)) continue;
+    const int lane = threadIdx.x & 31, t = threadIdx.x >> 5, h = blockIdx.y, tile_bytes = kv_tile_bytes(D, c.groups), ch = lane * CPL, g = ch / group;
+    const int row0 = blockIdx.x * r.per_block, row1 = min(row0 + r.per_block, r.rows);
+    for (int row = row0; row < row1;) {
+        const KvRun run = kv_run(c, r, row, lane);
+        const int first = row, tok0 = run.pos % KV_TILE;
+        row = run.next;
+        if (run.n == 0) continue;
         const int page = kv_page(c, run.seq, run.pos);
         if (page < 0) continue;
         const unsigned char *tile = kv_tile(c, page, h, run.pos, tile_bytes);
-        const int tok0 = run.pos % KV_TILE, ch = lane * CPL, g = ch / group;
         const uint32_t *kw = reinterpret_cast<const uint32_t *>(tile + kv_k_words(D)) + g * KV_TILE, *vw = reinterpret_cast<const uint32_t *>(tile + kv_v_words(D, c.groups)) + g * KV_TILE;
-        for (int t = 0; t < 4; ++t) {
-            uint32_t vcode[CPL], kcode[8], kword[8], vword[8];
+        uint32_t vcode[CPL], kcode[8], kword[8], vword[8];
 #pragma unroll
-            for (int k = 0; k < CPL; ++k) vcode[k] = __ldcg(reinterpret_cast<const uint32_t *>(tile + kv_v_codes(D)) + kv_v_word(ch + k, t));
+        for (int k = 0; k < CPL; ++k) vcode[k] = __ldcg(reinterpret_cast<const uint32_t *>(tile + kv_v_codes(D)) + kv_v_word(ch + k, t));
 #pragma unroll
-            for (int i = 0; i < 8; ++i) {
-                const int tok = 8 * (i >> 1) + 2 * t + (i & 1);
-                kcode[i] = kword[i] = vword[i] = 0;
-                if (tok < tok0 || tok >= tok0 + run.n) continue;
-                const unsigned char *from = tile + tok * (D / 2) + kv_k_byte(D, ch);
-                if constexpr (CPL == 2) kcode[i] = __ldcg(from);
-                else if constexpr (CPL == 4) kcode[i] = __ldcg(reinterpret_cast<const unsigned short *>(from));
-                else kcode[i] = __ldcg(reinterpret_cast<const uint32_t *>(from));
-                kword[i] = __ldcg(kw + kv_word_at(tok));
-                vword[i] = __ldcg(vw + kv_word_at(tok));
+        for (int i = 0; i < 8; i += 4) {  // the words of tokens 2 t + o lie side by side
+            *reinterpret_cast<uint4 *>(kword + i) = __ldcg(reinterpret_cast<const uint4 *>(kw + kv_word_at(2 * t + i / 4)));
+            *reinterpret_cast<uint4 *>(vword + i) = __ldcg(reinterpret_cast<const uint4 *>(vw + kv_word_at(2 * t + i / 4)));
+        }
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {  // (in the order of the words: token 8 (i % 4) + 2 t + i / 4; the tile is there whether the token is or not)
+            const unsigned char *from = tile + (8 * (i & 3) + 2 * t + (i >> 2)) * (D / 2) + kv_k_byte(D, ch);
+            if constexpr (CPL == 2) kcode[i] = __ldcg(from);
+            else if constexpr (CPL == 4) kcode[i] = __ldcg(reinterpret_cast<const unsigned short *>(from));
+            else kcode[i] = __ldcg(reinterpret_cast<const uint32_t *>(from));
+        }
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            const int j = i & 3, o = i >> 2, n = 8 * j + 2 * t + o - tok0;
+            if (n < 0 || n >= run.n) continue;
+            const int nib = 4 * (j + 4 * o);
+            const float ks = __uint_as_float(kword[i] & ~15u), vs = __uint_as_float(vword[i] & ~15u);
+            const int kz = kword[i] & 15u, vz = vword[i] & 15u;
+            uint32_t ka[CPL / 2], va[CPL / 2];
+#pragma unroll
+            for (int k = 0; k < CPL / 2; ++k) {
+                ka[k] = kv_narrow2<BF16>(ks * (float)((int)((kcode[i] >> (8 * k)) & 15u) - kz), ks * (float)((int)((kcode[i] >> (8 * k + 4)) & 15u) - kz));
+                va[k] = kv_narrow2<BF16>(vs * (float)((int)((vcode[2 * k] >> nib) & 15u) - vz), vs * (float)((int)((vcode[2 * k + 1] >> nib) & 15u) - vz));
             }
-#pragma unroll
-            for (int i = 0; i < 8; ++i) {
-                const int tok = 8 * (i >> 1) + 2 * t + (i & 1), n = tok - tok0;
-                if (n < 0 || n >= run.n) continue;
-                const int nib = 4 * ((i >> 1) + 4 * (i & 1));
-                const float ks = __uint_as_float(kword[i] & ~15u), kz = (float)(kword[i] & 15u);
-                const float vs = __uint_as_float(vword[i] & ~15u), vz = (float)(vword[i] & 15u);
-                uint32_t ka[CPL / 2], va[CPL / 2];
-#pragma unroll
-                for (int k = 0; k < CPL / 2; ++k) {
-                    const float a = ks * ((float)((kcode[i] >> (8 * k)) & 15u) - kz), b = ks * ((float)((kcode[i] >> (8 * k + 4)) & 15u) - kz);
-                    ka[k] = (uint32_t)kv_narrow<D, BF16>(a) | ((uint32_t)kv_narrow<D, BF16>(b) << 16);
-                    const float e = vs * ((float)((vcode[2 * k] >> nib) & 15u) - vz), f = vs * ((float)((vcode[2 * k + 1] >> nib) & 15u) - vz);
-                    va[k] = (uint32_t)kv_narrow<D, BF16>(e) | ((uint32_t)kv_narrow<D, BF16>(f) << 16);
-                }
-                unsigned short *kt = ko + (long long)(run.row + n) * r.ldk + (long long)h * D + ch, *vt = vo + (long long)(run.row + n) * r.ldv + (long long)h * D + ch;
-                if constexpr (CPL == 2) {
-                    *reinterpret_cast<uint32_t *>(kt) = ka[0];
-                    *reinterpret_cast<uint32_t *>(vt) = va[0];
-                } else if constexpr (CPL == 4) {
-                    *reinterpret_cast<uint2 *>(kt) = make_uint2(ka[0], ka[1]);
-                    *reinterpret_cast<uint2 *>(vt) = make_uint2(va[0], va[1]);
-                } else {
-                    *reinterpret_cast<uint4 *>(kt) = make_uint4(ka[0], ka[1], ka[2], ka[3]);
-                    *reinterpret_cast<uint4 *>(vt) = make_uint4(va[0], va[1], va[2], va[3]);
-                }
-            }
+            kv_put<CPL>(const_cast<void *>(r.k), (long long)(first + n) * r.ldk + (long long)h * D + ch, ka);
+            kv_put<CPL>(const_cast<void *>(r.v), (long long)(first + n) * r.ldv + (long long)h * D + ch, va);
         }
     }
 }
@@ -280,16 +311,15 @@ scap_status kv_check(const scap_kv4 *c) {
     return SCAP_OK;
 }
 
-// Rows a warp looks through: few where there are few, so that single tokens of many sequences go side by side.
-static int kv_per_warp(long long rows, int heads) {
-    const long long warps = rows * heads / (16LL * sm_count());
-    return warps < 1 ? 1 : (warps > 8 ? 8 : (int)warps);
+// Rows a block looks through: a tile's worth, fewer where there are few, so that single tokens of many sequences go side by side.
+static int kv_per_block(long long rows, int heads) {
+    const long long n = rows * heads / (8LL * sm_count());
+    return n < 1 ? 1 : (n > KV_TILE ? KV_TILE : (int)n);
 }
 
 template <int D>
 static cudaError_t kv_launch(bool append, bool bf16, const KvCache &c, const KvRows &r, int group, cudaStream_t st) {
-    const long long warps = ((long long)r.rows + r.per_warp - 1) / r.per_warp;
-    const dim3 grid((unsigned)((warps + KV_THREADS / 32 - 1) / (KV_THREADS / 32)), c.heads), block(KV_THREADS);
+    const dim3 grid((r.rows + r.per_block - 1) / r.per_block, c.heads), block(KV_THREADS);
     const bool pdl = g_tune.pdl != 0;
     if (append) return bf16 ? launch(kv4_append_kernel<D, true>, grid, block, 0, st, pdl, c, r, group) : launch(kv4_append_kernel<D, false>, grid, block, 0, st, pdl, c, r, group);
     return bf16 ? launch(kv4_read_kernel<D, true>, grid, block, 0, st, pdl, c, r, group) : launch(kv4_read_kernel<D, false>, grid, block, 0, st, pdl, c, r, group);
@@ -310,7 +340,7 @@ static scap_status kv_rows(bool append, const scap_kv4 *cache, const void *k, in
     const KvCache c = kv_cache(cache);
     KvRows r = {};
     r.k = k; r.v = v; r.ldk = ldk; r.ldv = ldv; r.row_start = row_start; r.rows = rows;
-    r.per_warp = kv_per_warp(rows, cache->heads);
+    r.per_block = kv_per_block(rows, cache->heads);
     cudaStream_t st = reinterpret_cast<cudaStream_t>(stream);
     const bool bf16 = dt == SCAP_BF16;
     switch (cache->head_dim) {
