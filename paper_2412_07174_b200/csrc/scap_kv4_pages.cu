@@ -140,7 +140,7 @@ __global__ void __launch_bounds__(PG_COPY_THREADS) kv4_copy_kernel(const PgCache
 __global__ void __launch_bounds__(PG_THREADS) kv4_fork_kernel(const PgCache c, const int *src, const int *dst, int n, int *fail, int *from, int *to, int *count, int *list) {
     __shared__ PgShared s;
     __shared__ int s_owner[SCAP_MAX_SEQS];  // first request that names a row as its destination
-    __shared__ int s_rank[PG_THREADS];
+    __shared__ int s_src[PG_THREADS], s_dst[PG_THREADS], s_len[PG_THREADS], s_rank[PG_THREADS];
     constexpr int NOBODY = 0x7fffffff;
     griddep_wait();
     auto row_ok = [&](int b) { return b >= 0 && b < c.n_seqs; };
@@ -151,53 +151,69 @@ __global__ void __launch_bounds__(PG_THREADS) kv4_fork_kernel(const PgCache c, c
         if (row_ok(b)) atomicMin(&s_owner[b], i);
     }
     __syncthreads();
-    // 0: left out, 1: shares all pages, 2: needs one of its own.  (A row's length changes only after its request has been looked at.)
-    auto kind = [&](int i) {
-        const int a = __ldcg(src + i), b = __ldcg(dst + i);
-        if (!row_ok(a) || !row_ok(b) || s_owner[b] != i || s_owner[a] != NOBODY || __ldcg(c.lens + b) > 0) return 0;
-        const int len = __ldcg(c.lens + a);
-        if ((long long)len > (long long)c.table_stride * c.page_tokens) return 0;
-        return len > 0 && len % c.page_tokens != 0 ? 2 : 1;
+    // This thread's request of a block of 1024: its rows and length into shared memory, and what it is - 0: left out, 1: shares all
+    // pages, 2: needs one of its own.  (A destination's length changes only after its own request has been looked at for the last time.)
+    auto look = [&](int i) {
+        int what = 1;
+        if (i < n) {
+            const int a = __ldcg(src + i), b = __ldcg(dst + i);
+            what = 0;
+            if (row_ok(a) && row_ok(b) && s_owner[b] == i && s_owner[a] == NOBODY) {
+                const int len = __ldcg(c.lens + a), there = __ldcg(c.lens + b);
+                if (there <= 0 && (long long)len <= (long long)c.table_stride * c.page_tokens) what = len > 0 && len % c.page_tokens != 0 ? 2 : 1;
+                s_len[threadIdx.x] = max(0, len);
+            }
+            s_src[threadIdx.x] = a;
+            s_dst[threadIdx.x] = b;
+        }
+        return what;
     };
-    int want = 0;
+    int want = 0, what = 1;
     for (int i0 = 0; i0 < n; i0 += PG_THREADS) {
-        const int i = i0 + (int)threadIdx.x;
-        want += __syncthreads_count(i < n && kind(i) == 2);
+        what = look(i0 + (int)threadIdx.x);
+        want += __syncthreads_count(what == 2);
     }
     const int have = pg_free_pages(c, want, list, s);
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
     int before = 0, failed = 0;
     for (int i0 = 0; i0 < n; i0 += PG_THREADS) {
-        const int i = i0 + (int)threadIdx.x;
-        const int what = i < n ? kind(i) : 1;
+        if (n > PG_THREADS) what = look(i0 + (int)threadIdx.x);  // (else it is as it was)
         int total;
         const int rank = before + pg_scan(what == 2 ? 1 : 0, s, total);
         before += total;
         const bool lost = what == 2 && rank >= have;  // no page was left: the row stays empty
-        if (what == 2 && !lost) {
-            const int a = __ldcg(src + i), page = list[rank];
-            from[rank] = __ldcg(c.table + (long long)a * c.table_stride + __ldcg(c.lens + a) / c.page_tokens);
-            to[rank] = page;
-            c.refs[page] = 1;
-        }
         s_rank[threadIdx.x] = what == 0 || lost ? -2 : (what == 2 ? rank : -1);
         failed += __syncthreads_count(what == 0 || lost);
-        // rows, a warp per request
-        for (int k = warp; k < PG_THREADS && i0 + k < n; k += PG_THREADS / 32) {
-            const int r = s_rank[k];
-            if (r == -2) continue;
-            const int a = __ldcg(src + i0 + k), b = __ldcg(dst + i0 + k), len = max(0, __ldcg(c.lens + a)), full = len / c.page_tokens;
+        // rows, a warp per request, two at a time
+        for (int k0 = warp; k0 < PG_THREADS && i0 + k0 < n; k0 += 2 * (PG_THREADS / 32)) {
             for (int t = lane; t < c.table_stride; t += 32) {
-                int page = -1;
-                if (t < full) {
-                    page = __ldcg(c.table + (long long)a * c.table_stride + t);
-                    if (pg_valid(c, page)) atomicAdd(c.refs + page, 1);
-                } else if (t == full && r >= 0) {
-                    page = list[r];
+                int page[2];
+                bool on[2];
+#pragma unroll
+                for (int m = 0; m < 2; ++m) {
+                    const int k = k0 + m * (PG_THREADS / 32);
+                    on[m] = k < PG_THREADS && i0 + k < n && s_rank[k] != -2;
+                    const int full = on[m] ? s_len[k] / c.page_tokens : -1;
+                    page[m] = t < full || (t == full && s_rank[k] >= 0) ? __ldcg(c.table + (long long)s_src[k] * c.table_stride + t) : -1;
                 }
-                c.table[(long long)b * c.table_stride + t] = page;
+#pragma unroll
+                for (int m = 0; m < 2; ++m) {
+                    const int k = k0 + m * (PG_THREADS / 32);
+                    if (!on[m]) continue;
+                    const int r = s_rank[k];
+                    if (t == s_len[k] / c.page_tokens && r >= 0) {  // the partial page
+                        const int fresh = list[r];
+                        from[r] = page[m];
+                        to[r] = fresh;
+                        c.refs[fresh] = 1;
+                        page[m] = fresh;
+                    } else if (pg_valid(c, page[m])) {
+                        atomicAdd(c.refs + page[m], 1);
+                    }
+                    c.table[(long long)s_dst[k] * c.table_stride + t] = page[m];
+                    if (t == 0) c.lens[s_dst[k]] = s_len[k];
+                }
             }
-            if (lane == 0) c.lens[b] = len;
         }
         __syncthreads();
     }
@@ -242,21 +258,28 @@ __global__ void __launch_bounds__(PG_THREADS) kv4_reserve_kernel(const PgCache c
         return min(pg_pages(c, (int)sum) - pg_pages(c, (int)len), c.n_pages + 1);
     };
     long long want = 0;
+    int m = 0, first_of = 0;
     for (int b0 = 0; b0 < c.n_seqs; b0 += PG_THREADS) {
         const int b = b0 + (int)threadIdx.x;
         int total;
-        pg_scan(b < c.n_seqs ? max(0, more(b)) : 0, s, total);
+        m = b < c.n_seqs ? more(b) : 0;
+        first_of = pg_scan(max(0, m), s, total);
         want += total;
     }
     const int have = pg_free_pages(c, (int)min(want, (long long)c.n_pages), list, s);
     long long before = 0;
-    int failed = 0;
+    int failed = 0, first_before = 0;  // pages asked for by the blocks of sequences before, and by the last of these
     for (int b0 = 0; b0 < c.n_seqs; b0 += PG_THREADS) {
         const int b = b0 + (int)threadIdx.x;
-        const int m = b < c.n_seqs ? more(b) : 0;
-        int total;
-        const long long first = before + pg_scan(max(0, m), s, total);
-        before += total;
+        if (c.n_seqs > PG_THREADS) {  // (else all is as it was)
+            int total;
+            m = b < c.n_seqs ? more(b) : 0;
+            first_of = pg_scan(max(0, m), s, total);
+            __syncthreads();
+            before += first_before;
+            first_before = total;
+        }
+        const long long first = before + first_of;
         const bool ok = m == 0 || (m > 0 && first + m <= have);
         if (b < c.n_seqs && ok) {
             const int len = max(0, __ldcg(c.lens + b)), held = pg_pages(c, len);
