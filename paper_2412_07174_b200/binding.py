@@ -417,11 +417,12 @@ def scap_moe_ffn(h, logits, experts, top_k: int, y, ws, expert_out=None, weight_
                               _ptr(weight_out), p, n, _stream(stream)), "scap_moe_ffn")
 
 
-def _rows(t, name: str) -> int:
-    """Row stride of a matrix whose rows are contiguous, in elements."""
-    if t.dim() != 2 or (t.stride(1) != 1 and t.shape[1] > 1):
-        raise ValueError("%s must be a matrix with contiguous rows" % name)
-    return max(t.stride(0), t.shape[1]) if t.shape[0] <= 1 else t.stride(0)
+def _rows(t, rows: int, cols: int, name: str) -> int:
+    """Row stride of a matrix [rows, cols] whose rows are contiguous, in elements."""
+    ld, one = t.stride()
+    if one != 1 and cols > 1:
+        raise ValueError("%s must have contiguous rows" % name)
+    return ld if rows > 1 else max(ld, cols)
 
 
 def scap_fc_act_workspace(M: int, K: int, N: int, ldx: int | None = None) -> int:
@@ -431,19 +432,20 @@ def scap_fc_act_workspace(M: int, K: int, N: int, ldx: int | None = None) -> int
 def scap_fc_act(x, W, b, y, ws, act: int = SCAP_ACT_NONE, res=None, stream=None) -> None:
     """y = act(x W + b) + res on any number of rows; rows of x, res and y may lie apart (views of wider matrices)."""
     M, K = x.shape
-    N = W.shape[1]
+    K_, N = shape = W.shape
+    dt = dtype_of(x)
     ydt = SCAP_F32 if y.dtype is torch.float32 else dtype_of(y)
-    if x.dtype is not W.dtype or W.shape[0] != K or not W.is_contiguous() or y.shape != (M, N):
-        raise ValueError("x [M, K] and W [K, N] must have one dtype, W contiguous rows, y the shape [M, N]")
+    if x.dtype is not W.dtype or K_ != K or not W.is_contiguous() or y.shape != (M, N):
+        raise ValueError("x [M, K] and W [K, N] must have one dtype, W contiguous rows, y the shape [M, N]: %s" % (shape,))
     if b is not None and (b.dtype is not torch.float32 or b.numel() != N or not b.is_contiguous()):
         raise ValueError("b must be float32 [N]")
     ldr = 0
     if res is not None:
-        if res.shape != y.shape or res.dtype is not y.dtype:
+        if res.dtype is not y.dtype or res.shape != (M, N):
             raise ValueError("res must have the shape and dtype of y")
-        ldr = _rows(res, "res")
+        ldr = _rows(res, M, N, "res")
     p, n = _ws(ws)
-    _invoke("scap_fc_act", x, _rows(x, "x"), W, b, int(act), res, ldr, y, _rows(y, "y"), M, K, N, dtype_of(x), ydt, p, n, _stream(stream))
+    _invoke("scap_fc_act", x, _rows(x, M, K, "x"), W, b, int(act), res, ldr, y, _rows(y, M, N, "y"), M, K, N, dt, ydt, p, n, _stream(stream))
 
 
 class ScapKv4(C.Structure):
@@ -454,38 +456,46 @@ class ScapKv4(C.Structure):
                 ("lens", C.c_void_p), ("refs", C.c_void_p)]
 
     def __init__(self, pages, page_tokens: int, heads: int, head_dim: int, group: int, table, lens, refs=None):
-        if pages.dtype is not torch.uint8 or pages.dim() != 2 or pages.stride(1) != 1:
+        n_pages, width = pages.shape
+        n_seqs, row = table.shape
+        stride, one = pages.stride()
+        if pages.dtype is not torch.uint8 or one != 1:
             raise ValueError("pages must be uint8 [n_pages, bytes] with contiguous rows")
-        for t, shape, name in ((table, (lens.shape[0], table.shape[-1]), "table"), (lens, (lens.shape[0],), "lens"), (refs, (pages.shape[0],), "refs")):
-            if t is not None and (t.dtype is not torch.int32 or tuple(t.shape) != shape or not t.is_contiguous()):
-                raise ValueError("%s must be a contiguous int32 tensor of shape %s" % (name, shape))
-        need = scap_kv4_page_bytes(page_tokens, heads, head_dim, group)
-        if pages.shape[1] < need:
-            raise ValueError("a page needs %d bytes, has %d" % (need, pages.shape[1]))
-        super().__init__(pages.data_ptr(), max(pages.stride(0), pages.shape[1]), pages.shape[0], int(page_tokens), int(heads), int(head_dim), int(group), table.shape[1],
-                         table.shape[0], table.data_ptr(), lens.data_ptr(), None if refs is None else refs.data_ptr())
+        if table.dtype is not torch.int32 or not table.is_contiguous():
+            raise ValueError("table must be contiguous int32 [n_seqs, pages of a sequence]")
+        if lens.dtype is not torch.int32 or lens.shape != (n_seqs,) or not lens.is_contiguous():
+            raise ValueError("lens must be contiguous int32 [%d]" % n_seqs)
+        if refs is not None and (refs.dtype is not torch.int32 or refs.shape != (n_pages,) or not refs.is_contiguous()):
+            raise ValueError("refs must be contiguous int32 [%d]" % n_pages)
+        if heads and width < scap_kv4_page_bytes(page_tokens, heads, head_dim, group):
+            raise ValueError("a page needs %d bytes, has %d" % (scap_kv4_page_bytes(page_tokens, heads, head_dim, group), width))
+        super().__init__(pages.data_ptr(), stride if n_pages > 1 else max(stride, width), n_pages, page_tokens, heads, head_dim, group, row, n_seqs, table.data_ptr(),
+                         lens.data_ptr(), None if refs is None else refs.data_ptr())
         self.tensors = (pages, table, lens, refs)  # kept alive with the description
         self.address = C.addressof(self)
+        self.shape = (n_seqs, heads, head_dim)
 
 
 def scap_kv4_page_bytes(page_tokens: int, heads: int, head_dim: int, group: int) -> int:
     return lib().scap_kv4_page_bytes(int(page_tokens), int(heads), int(head_dim), int(group))
 
 
-def _tokens(t, heads: int, D: int, name: str) -> int:
-    """Elements between the tokens of [tokens, heads, D], which may be a slice of a wider row."""
-    if t.dim() != 3 or t.shape[1] != heads or t.shape[2] != D or t.stride(2) != 1 or (heads > 1 and t.stride(1) != D):
+def _tokens(t, rows: int, heads: int, D: int, name: str) -> int:
+    """Elements between the tokens of [rows, heads, D], which may be a slice of a wider row."""
+    ld, of_head, one = t.stride()
+    if one != 1 or (heads > 1 and of_head != D):
         raise ValueError("%s must be [tokens, %d, %d] with contiguous heads" % (name, heads, D))
-    return t.stride(0) if t.shape[0] > 1 else max(t.stride(0), heads * D)
+    return ld if rows > 1 else max(ld, heads * D)
 
 
 def _kv4_rows(name: str, cache, k, v, row_start, stream) -> None:
-    if k.dtype is not v.dtype or k.shape != v.shape:
-        raise ValueError("k and v must have one dtype and shape")
-    if row_start is not None and (row_start.dtype is not torch.int32 or row_start.numel() != cache.n_seqs + 1 or not row_start.is_contiguous()):
+    n_seqs, heads, D = cache.shape
+    rows = k.shape[0]
+    if k.shape != (rows, heads, D) or v.shape != (rows, heads, D) or k.dtype is not v.dtype:
+        raise ValueError("k and v must be [rows, %d, %d] of one dtype" % (heads, D))
+    if row_start is not None and (row_start.dtype is not torch.int32 or row_start.numel() != n_seqs + 1 or not row_start.is_contiguous()):
         raise ValueError("row_start must be int32 [n_seqs + 1]")
-    _invoke(name, cache.address, k, _tokens(k, cache.heads, cache.head_dim, "k"), v, _tokens(v, cache.heads, cache.head_dim, "v"), row_start, k.shape[0],
-            dtype_of(k), _stream(stream))
+    _invoke(name, cache.address, k, _tokens(k, rows, heads, D, "k"), v, _tokens(v, rows, heads, D, "v"), row_start, rows, dtype_of(k), _stream(stream))
 
 
 def scap_kv4_append(cache, k, v, row_start=None, stream=None) -> None:
@@ -502,23 +512,26 @@ def scap_kv4_attend_workspace(n_seqs: int, nq: int, q_heads: int, heads: int, he
     return lib().scap_kv4_attend_workspace(int(n_seqs), int(nq), int(q_heads), int(heads), int(head_dim))
 
 
-def _queries(t, D: int, name: str) -> int:
+def _queries(t, n_seqs: int, nq: int, heads: int, D: int, name: str) -> int:
     """Elements between the tokens of [n_seqs, nq, heads, D], which may be a slice of a wider row."""
-    B, nq, heads, _ = t.shape
-    if t.stride(3) != 1 or (heads > 1 and t.stride(2) != D) or (B > 1 and nq > 1 and t.stride(0) != nq * t.stride(1)):
+    of_seq, ld, of_head, one = t.stride()
+    if one != 1 or (heads > 1 and of_head != D) or (n_seqs > 1 and nq > 1 and of_seq != nq * ld):
         raise ValueError("%s must have contiguous heads, and evenly spaced tokens" % name)
-    return t.stride(1) if nq > 1 else (t.stride(0) if B > 1 else heads * D)
+    return ld if nq > 1 else (of_seq if n_seqs > 1 else heads * D)
 
 
 def scap_kv4_attend(cache, q, out, scale: float, ws, window: int = 0, lse=None, stream=None) -> None:
     """out[b, i, h]: attention of the last nq tokens of every sequence, q [n_seqs, nq, q_heads, head_dim], over its tokens in the cache."""
-    if q.dim() != 4 or q.shape[0] != cache.n_seqs or q.shape[3] != cache.head_dim or out.shape != q.shape or out.dtype is not q.dtype:
-        raise ValueError("q and out must be [%d, nq, q_heads, %d] of one dtype" % (cache.n_seqs, cache.head_dim))
-    if lse is not None and (lse.dtype is not torch.float32 or lse.shape != q.shape[:3] or not lse.is_contiguous()):
+    n_seqs, _, D = cache.shape
+    shape = q.shape
+    B, nq, heads, D_ = shape
+    if B != n_seqs or D_ != D or out.shape != shape or out.dtype is not q.dtype:
+        raise ValueError("q and out must be [%d, nq, q_heads, %d] of one dtype" % (n_seqs, D))
+    if lse is not None and (lse.dtype is not torch.float32 or lse.shape != (B, nq, heads) or not lse.is_contiguous()):
         raise ValueError("lse must be contiguous float32 [n_seqs, nq, q_heads]")
     p, n = _ws(ws)
-    _invoke_real("scap_kv4_attend", float(scale), 8, cache.address, q, _queries(q, cache.head_dim, "q"), out, _queries(out, cache.head_dim, "out"), lse, q.shape[1],
-                 q.shape[2], int(window), dtype_of(q), p, n, _stream(stream))
+    _invoke_real("scap_kv4_attend", float(scale), 8, cache.address, q, _queries(q, B, nq, heads, D, "q"), out, _queries(out, B, nq, heads, D, "out"), lse, nq, heads, int(window),
+                 dtype_of(q), p, n, _stream(stream))
 
 
 def scap_kv4_pages_workspace(n_pages: int, n: int) -> int:
@@ -552,7 +565,7 @@ def scap_kv4_free(cache, rows, stream=None) -> None:
 
 def scap_kv4_reserve(cache, add, fail, ws, stream=None) -> None:
     """lens[b] += add[b], with free pages for the new tokens.  fail [1] int32 or None: sequences that did not get them."""
-    if _numbers("add", add) != cache.n_seqs:
+    if _numbers("add", add) != cache.shape[0]:
         raise ValueError("add must be int32 [n_seqs]")
     p, n = _ws(ws)
     _invoke("scap_kv4_reserve", cache.address, add, fail, p, n, _stream(stream))
