@@ -26,7 +26,7 @@ namespace scap {
 
 constexpr int AT_WARPS = 4;
 constexpr int AT_THREADS = AT_WARPS * 32;
-constexpr int AT_MIN_UNITS = 4;  // tiles per CTA at least
+constexpr int AT_MIN_UNITS = 4;  // tiles per CTA, one for each warp, unless the items are shorter: an item after another takes 4 us each
 constexpr int AT_UP = 133;       // a scale of exponent field e is below 2^(e - 126), a weight at most 2^8: their product below 2^15 as held
 
 // CTAs per SM and tiles in a warp's ring, as registers and shared memory allow (RN groups of eight rows, G groups of channels).
@@ -71,18 +71,22 @@ __device__ __forceinline__ long long at_cut(long long units, int i, int ctas) { 
 // CTAs that share the units.  Where there is much to do twice as many as the device holds: the SMs favour the older ones of their CTAs, and
 // the younger ones of a second wave take over from those (83 units per resident CTA: 75 -> 71 us; 55 units: 42 -> 52).
 constexpr int AT_TWO_WAVES = 64;
-__device__ __forceinline__ int at_ctas(const AtArgs &a, long long units) {
-    const long long n = (units + AT_MIN_UNITS - 1) / AT_MIN_UNITS;
+__device__ __forceinline__ int at_ctas(const AtArgs &a, long long units, long long items) {
+    const long long n = max((units + AT_MIN_UNITS - 1) / AT_MIN_UNITS, items);
     const int most = units >= (long long)AT_TWO_WAVES * a.resident ? 2 * a.resident : a.resident;
     return n < most ? (int)n : most;
 }
 
-// Number of tiles of all sequences (the whole block takes part).
-__device__ __forceinline__ long long at_count(const AtArgs &a, long long *s) {
+// Number of tiles of all sequences, and of the sequences that have any (the whole block takes part).
+__device__ __forceinline__ long long at_count(const AtArgs &a, long long *s, int &some) {
     long long all = 0;
-    for (int b = threadIdx.x; b < a.c.n_seqs; b += AT_THREADS) {
+    some = 0;
+    for (int b0 = 0; b0 < a.c.n_seqs; b0 += AT_THREADS) {
+        const int b = b0 + (int)threadIdx.x;
         int first;
-        all += at_tiles(a, b, first);
+        const int n = b < a.c.n_seqs ? at_tiles(a, b, first) : 0;
+        all += n;
+        some += __syncthreads_count(n > 0);
     }
 #pragma unroll
     for (int o = 16; o > 0; o /= 2) all += __shfl_xor_sync(0xffffffffu, all, o);
@@ -101,7 +105,8 @@ __device__ __forceinline__ bool at_begin(const AtArgs &a, int per, long long *s,
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
     long long units = 0, before = 0;
     const bool one = a.c.n_seqs <= AT_THREADS;  // one look at the lengths gives the sum and the place
-    if (!one) units = at_count(a, s) * per;
+    int some = 0;
+    if (!one) units = at_count(a, s, some) * per;
     for (int b0 = 0; b0 < a.c.n_seqs; b0 += AT_THREADS) {
         const int b = b0 + (int)threadIdx.x;
         int first;
@@ -113,7 +118,8 @@ __device__ __forceinline__ bool at_begin(const AtArgs &a, int per, long long *s,
             if (lane >= o) incl += up;
         }
         if (lane == 31) s[warp] = incl;
-        __syncthreads();
+        const int here = __syncthreads_count(n > 0);
+        if (one) some = here;
         long long off = before, all = before;
 #pragma unroll
         for (int w = 0; w < AT_WARPS; ++w) {
@@ -121,7 +127,7 @@ __device__ __forceinline__ bool at_begin(const AtArgs &a, int per, long long *s,
             all += s[w];
         }
         if (one) units = all;
-        const int ctas = at_ctas(a, units);
+        const int ctas = at_ctas(a, units, (long long)some * per);
         if ((int)blockIdx.x >= ctas) return false;
         u = at_cut(units, blockIdx.x, ctas);
         u1 = at_cut(units, blockIdx.x + 1, ctas);
@@ -741,7 +747,8 @@ extern "C" scap_status scap_kv4_attend(const scap_kv4 *cache, const void *q, int
     // What the tables have room for bounds the work: no more CTAs than that takes.
     const long long cap = (long long)cache->table_stride * (cache->page_tokens / KV_TILE), seen = window > 0 ? ((long long)window + nq) / KV_TILE + 2 : cap;
     a.tile_cap = (int)(cap < (1ll << 30) ? cap : (1ll << 30));
-    const long long units = (cap < seen ? cap : seen) * cache->n_seqs * cache->heads * a.row_tiles, few = (units + AT_MIN_UNITS - 1) / AT_MIN_UNITS;
+    const long long items = (long long)cache->n_seqs * cache->heads * a.row_tiles, units = (cap < seen ? cap : seen) * items;
+    const long long few = (units + AT_MIN_UNITS - 1) / AT_MIN_UNITS > items ? (units + AT_MIN_UNITS - 1) / AT_MIN_UNITS : items;
     const int most = units >= (long long)AT_TWO_WAVES * a.resident ? 2 * a.resident : a.resident;
     const int grid = few < most ? (int)few : most;
     a.where = reinterpret_cast<int2 *>(a.part + (size_t)4 * a.resident * 8 * rn * (cache->head_dim + 2));
