@@ -34,7 +34,7 @@ __host__ __device__ constexpr int at_resident(int D, int G, int RN) {
     return D == 64 ? (RN == 1 ? 5 : 4) : (D == 128 ? (RN == 1 && G < 4 ? 4 : 3) : (RN == 1 ? 3 : 2));
 }
 __host__ __device__ constexpr int at_stages(int D, int G, int RN) {
-    return D == 64 ? 4 : (D == 128 ? (RN == 2 && G < 4 ? 4 : 3) : (RN == 1 ? 2 : 3));
+    return D == 64 ? 4 : (D == 128 ? 3 : 2);
 }
 
 struct AtArgs {
@@ -181,7 +181,12 @@ __global__ void __launch_bounds__(AT_THREADS, at_resident(D, G, RN)) kv4_attend_
     constexpr int PITCH = D + 4;         // of a row of the join
     constexpr float LN2 = 0.69314718055994531f;
     static_assert(ST * TILE >= ROWS * PITCH * 4, "a warp's part of the join goes where its ring was");
+    // Sixteen rows: the queries are B operands in shared memory, one 16-byte load for two MMAs, where their registers would spill.
+    constexpr bool QS = RN == 2;
     extern __shared__ __align__(128) unsigned char at_raw[];
+    uint4 *s_q = reinterpret_cast<uint4 *>(at_raw + AT_WARPS * ST * TILE);  // [RN][W][32 lanes]
+    __shared__ uint32_t s_zq[QS ? RN : 1][G][32];
+    __shared__ float s_f[RN];
     __shared__ unsigned long long s_full[AT_WARPS][ST];
     __shared__ long long s_sum[AT_WARPS + 2];
     __shared__ float s_m[AT_WARPS][ROWS], s_l[AT_WARPS][ROWS];
@@ -214,8 +219,12 @@ __global__ void __launch_bounds__(AT_THREADS, at_resident(D, G, RN)) kv4_attend_
         // ---- addresses of the next 32 tiles of this warp, one per lane (0: no page), and the first copies
         auto pos_of = [&](int i) { return (first_tile + t0 + warp + AT_WARPS * i) * KV_TILE; };
         auto where = [&](int i) -> unsigned long long {
-            const int page = i < count ? kv_page(a.c, seq, pos_of(i)) : -1;
-            return page < 0 ? 0ull : (unsigned long long)kv_tile(a.c, page, h, pos_of(i), TILE);
+            if (i >= count) return 0ull;
+            const int per_page = a.c.page_tokens / KV_TILE, t = first_tile + t0 + warp + AT_WARPS * i, at = t / per_page;
+            if (at >= a.c.table_stride) return 0ull;
+            const int page = __ldcg(a.c.table + (long long)seq * a.c.table_stride + at);
+            if (page < 0 || page >= a.c.n_pages) return 0ull;
+            return (unsigned long long)(a.c.pages + (long long)page * a.c.page_stride + (long long)(h * per_page + t - at * per_page) * TILE);
         };
         unsigned long long at_now = where(lane), at_next = where(32 + lane);
         unsigned there = __ballot_sync(0xffffffffu, at_now != 0);  // which of the present 32 tiles have a page
@@ -236,11 +245,10 @@ __global__ void __launch_bounds__(AT_THREADS, at_resident(D, G, RN)) kv4_attend_
         // a row that is smaller by 2^x is 2^-36 of the largest scores); channels 32 j + 8 qt + i, the
         // even and odd nibbles of a code word in the two k halves of an MMA, the odd ones 16 times smaller as their codes are larger.
         // zq: minus the sum of a group, in two fp16 parts, against the zero points (times 2^6, as zero 2^-18 is the subnormal used)
-        uint32_t qb[RN][2 * W][2], zq[RN][G];
+        uint32_t qb[QS ? 1 : 2 * W][2], zq[QS ? 1 : G];
         float f[RN];  // what turns an accumulator into a score in units of log 2
-#pragma unroll
-        for (int rn = 0; rn < RN; ++rn) {
-            const int row = 8 * rn + qg;
+        if (!QS || warp < RN) {  // (in shared memory: warp rn for its eight rows)
+            const int rn = QS ? warp : 0, row = 8 * rn + qg;
             uint4 raw[W];
             const int in = rt * ROWS + row, tok = in / a.g, hd = in - tok * a.g;
             const unsigned short *src = a.q + ((long long)seq * a.nq + tok) * a.ldq + (long long)(h * a.g + hd) * D + 8 * qt;
@@ -268,22 +276,34 @@ __global__ void __launch_bounds__(AT_THREADS, at_resident(D, G, RN)) kv4_attend_
             for (int j = 0; j < W; ++j) {
 #pragma unroll
                 for (int i = 0; i < 8; ++i) sum[j * G / W] += v[j][i];
+                uint32_t w[2][2];
 #pragma unroll
                 for (int hi = 0; hi < 2; ++hi) {
-                    qb[rn][2 * j + hi][0] = at_pack(v[j][2 * hi] * up, v[j][2 * hi + 4] * up);
-                    qb[rn][2 * j + hi][1] = at_pack(v[j][2 * hi + 1] * (up * 0.0625f), v[j][2 * hi + 5] * (up * 0.0625f));
+                    w[hi][0] = at_pack(v[j][2 * hi] * up, v[j][2 * hi + 4] * up);
+                    w[hi][1] = at_pack(v[j][2 * hi + 1] * (up * 0.0625f), v[j][2 * hi + 5] * (up * 0.0625f));
+                    if constexpr (!QS) { qb[2 * j + hi][0] = w[hi][0]; qb[2 * j + hi][1] = w[hi][1]; }
                 }
+                if constexpr (QS) s_q[(rn * W + j) * 32 + lane] = make_uint4(w[0][0], w[0][1], w[1][0], w[1][1]);
             }
 #pragma unroll
             for (int n = 0; n < G; ++n) {
                 sum[n] += __shfl_xor_sync(0xffffffffu, sum[n], 1);
                 sum[n] += __shfl_xor_sync(0xffffffffu, sum[n], 2);
                 const float x = -sum[n] * up * 0.015625f, x_hi = __half2float(__float2half_rn(x));
-                zq[rn][n] = at_pack(x_hi, x - x_hi);
+                if constexpr (QS) s_zq[rn][n][lane] = at_pack(x_hi, x - x_hi);
+                else zq[n] = at_pack(x_hi, x - x_hi);
             }
-            f[rn] = at_pow2(24 - e) * a.scale;
+            f[0] = at_pow2(24 - e) * a.scale;
+            if constexpr (QS) {
+                if (lane == 0) s_f[rn] = f[0];
+            }
         }
         if (lane > 0 && lane < ST && lane < count) ask(at_now, slot + lane < ST ? slot + lane : slot + lane - ST);
+        if constexpr (QS) {
+            __syncthreads();
+#pragma unroll
+            for (int rn = 0; rn < RN; ++rn) f[rn] = s_f[rn];
+        }
         // keys that a row sees: lo .. hi
         int hi[RN][2], lo[RN][2];
 #pragma unroll
@@ -360,11 +380,22 @@ __global__ void __launch_bounds__(AT_THREADS, at_resident(D, G, RN)) kv4_attend_
                             for (int rn = 0; rn < RN; ++rn) {
 #pragma unroll
                                 for (int k = 0; k < 4; ++k) acc[mt][rn][n][k] = 0.0f;
-                                at_mma(acc[mt][rn][n], z0, z1, 0u, 0u, zq[rn][n], 0u);
+                                at_mma(acc[mt][rn][n], z0, z1, 0u, 0u, QS ? s_zq[QS ? rn : 0][n][lane] : zq[QS ? 0 : n], 0u);
                             }
                         }
 #pragma unroll
-                    for (int k = 0; k < W; ++k)
+                    for (int k = 0; k < W; ++k) {
+                        uint32_t q[RN][2][2];
+#pragma unroll
+                        for (int rn = 0; rn < RN; ++rn) {
+                            if constexpr (QS) {
+                                const uint4 x = s_q[(rn * W + k) * 32 + lane];
+                                q[rn][0][0] = x.x; q[rn][0][1] = x.y; q[rn][1][0] = x.z; q[rn][1][1] = x.w;
+                            } else {
+#pragma unroll
+                                for (int i = 0; i < 4; ++i) q[rn][i >> 1][i & 1] = qb[2 * k + (i >> 1)][i & 1];
+                            }
+                        }
 #pragma unroll
                         for (int hi8 = 0; hi8 < 2; ++hi8)
 #pragma unroll
@@ -372,8 +403,9 @@ __global__ void __launch_bounds__(AT_THREADS, at_resident(D, G, RN)) kv4_attend_
                                 const uint32_t x = w[2 * mt][k] >> (8 * hi8), y = w[2 * mt + 1][k] >> (8 * hi8);
                                 const uint32_t a0 = x & 0x000f000fu, a1 = y & 0x000f000fu, a2 = x & 0x00f000f0u, a3 = y & 0x00f000f0u;
 #pragma unroll
-                                for (int rn = 0; rn < RN; ++rn) at_mma(acc[mt][rn][k * G / W], a0, a1, a2, a3, qb[rn][2 * k + hi8][0], qb[rn][2 * k + hi8][1]);
+                                for (int rn = 0; rn < RN; ++rn) at_mma(acc[mt][rn][k * G / W], a0, a1, a2, a3, q[rn][hi8][0], q[rn][hi8][1]);
                             }
+                    }
 #pragma unroll
                     for (int j = 0; j < 4; ++j)
 #pragma unroll
@@ -688,7 +720,7 @@ __global__ void __launch_bounds__(AT_THREADS) kv4_join_kernel(const AtArgs a) {
 template <int D, int G, int RN>
 static cudaError_t at_launch_rn(const AtArgs &a, int grid, cudaStream_t st) {
     static SmemOptIn opt_in;
-    constexpr int SMEM = AT_WARPS * at_stages(D, G, RN) * kv_tile_bytes(D, G);
+    constexpr int SMEM = AT_WARPS * at_stages(D, G, RN) * kv_tile_bytes(D, G) + (RN == 2 ? RN * D / 32 * 32 * 16 : 0);
     auto kern = kv4_attend_kernel<D, G, RN>;
     cudaError_t e = ensure_dynamic_smem(kern, SMEM, opt_in);
     if (e != cudaSuccess) return e;
