@@ -63,6 +63,7 @@ struct FaShared {
     unsigned long long full[FA_MAX_STAGES], empty[FA_MAX_STAGES], tfull[2], tempty[2], drain;
     uint32_t tmem_base;
     int abort_flag;
+    int sent, peer_sent, peer_abort;  // stages asked for; with CG = 2 also what the other CTA leaves here at the end
 };
 
 __device__ __forceinline__ bool fa_wait(uint32_t bar, uint32_t parity, const FaArgs &a, volatile int *abort_flag) {
@@ -207,7 +208,7 @@ __global__ void __launch_bounds__(FA_THREADS, 1) fc_act_kernel(const FaArgs a, c
             mbar_init(&sh->tempty[i], FA_EPI_WARPS * CG);
         }
         mbar_init(&sh->drain, 1);
-        sh->abort_flag = 0;
+        sh->abort_flag = sh->sent = sh->peer_sent = sh->peer_abort = 0;
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     }
     if (warp == FA_EPI_WARPS + 1) {
@@ -268,11 +269,7 @@ __global__ void __launch_bounds__(FA_THREADS, 1) fc_act_kernel(const FaArgs a, c
                 }
             }
             griddep_launch_dependents();
-            // After a wait that ran out nobody consumes the stages, but the copies under way still write here: wait for them, with a limit.
-            if (*abort_flag && rank == 0) {
-                for (int i = sent > a.stages ? sent - a.stages : 0; i < sent; ++i)
-                    for (uint32_t n = 0; n < TRIES / 16 && !mbarrier_try_wait(smem_u32(&sh->full[i % a.stages]), (uint32_t)(i / a.stages) & 1u); ++n) {}
-            }
+            sh->sent = sent;
         }
         __syncwarp();
     } else if (warp == FA_EPI_WARPS + 1) {
@@ -497,7 +494,27 @@ __global__ void __launch_bounds__(FA_THREADS, 1) fc_act_kernel(const FaArgs a, c
     }
     tc_fence_before();
     __syncthreads();
+    if constexpr (CG == 2) {
+        if (tid == 0) {
+            const uint32_t other = (uint32_t)rank ^ 1u;
+            asm volatile("st.shared::cluster.u32 [%0], %1;" ::"r"(cluster_addr(smem_u32(&sh->peer_sent), other)), "r"(sh->sent) : "memory");
+            asm volatile("st.shared::cluster.u32 [%0], %1;" ::"r"(cluster_addr(smem_u32(&sh->peer_abort), other)), "r"(sh->abort_flag) : "memory");
+        }
+    }
     if (CG == 2 || S > 1) { cluster_arrive(); cluster_wait(); }  // nobody leaves while the other may still use its shared memory
+    // After a wait that ran out nobody consumes the stages, but the copies under way still write here: wait for them, with a limit.  With
+    // CG = 2 those of both CTAs count on the first one's barriers; for stages that only the other one asked for there was no announcement yet.
+    if (*abort_flag || (CG == 2 && sh->peer_abort)) {
+        if (rank == 0 && tid == 0) {
+            const int mine_sent = sh->sent, all = CG == 2 ? max(mine_sent, sh->peer_sent) : mine_sent;
+            for (int i = all > a.stages ? all - a.stages : 0; i < all; ++i) {
+                if (i >= mine_sent) mbar_arrive_expect_tx(&sh->full[i % a.stages], stage);
+                for (uint32_t n = 0; n < TRIES / 16 && !mbarrier_try_wait(smem_u32(&sh->full[i % a.stages]), (uint32_t)(i / a.stages) & 1u); ++n) {}
+            }
+        }
+        __syncthreads();
+        if constexpr (CG == 2) { cluster_arrive(); cluster_wait(); }
+    }
     tc_fence_after();
     if (warp == FA_EPI_WARPS + 1) {
         if constexpr (CG == 2)

@@ -134,6 +134,27 @@ def test_same_bits_in_a_graph_and_on_another_stream():
 
 
 @pytest.mark.gpu
+@pytest.mark.parametrize("M,K,N,ydt", [(600, 4096, 4096, BF), (600, 4096, 4096, F32), (5, 8192, 256, BF), (300, 1000, 520, F32)])
+def test_a_wait_that_runs_out_is_reported(M, K, N, ydt):
+    import paper_2412_07174_b200 as scap
+    x, W = torch.randn(M, K, device="cuda").to(BF), (0.05 * torch.randn(K, N, device="cuda")).to(BF)
+    y = torch.empty(M, N, dtype=ydt, device="cuda")
+    ws = torch.empty(scap.scap_fc_act_workspace(M, K, N), dtype=torch.uint8, device="cuda")
+    torch.cuda.synchronize()
+    scap.scap_tune("tc_spin", 1)
+    try:
+        scap.scap_fc_act(x, W, None, y, ws)
+        try:
+            scap.scap_device_status()
+        except scap.ScapError as e:
+            assert e.code == 7
+    finally:
+        scap.scap_tune("tc_spin", 0)
+    run_case(M, K, N, BF, ydt, res=True, seed=5)  # and the next call is right
+    scap.scap_device_status()
+
+
+@pytest.mark.gpu
 def test_non_finite_rows_stay_in_their_row():
     import paper_2412_07174_b200 as scap
     x = torch.randn(40, 128, device="cuda").to(BF)
