@@ -25,30 +25,33 @@ struct KvRun {
     int next;         // where to look on
 };
 
-// Sequence of a row: the last one that does not begin behind it (one load of 32 lanes per factor of 32).
-__device__ __forceinline__ int kv_find(const int *start, int n, int row, int lane) {
-    int lo = 0, len = n;  // start[lo] <= row (or lo = 0), the answer in lo .. lo + len - 1
-    while (len > 1) {
-        const int step = (len + 31) / 32, at = lo + lane * step;
-        const unsigned below = __ballot_sync(0xffffffffu, lane * step < len && __ldcg(start + at) <= row);
-        const int k = below ? 31 - __clz(below) : 0;
-        lo += k * step;
-        len = min(step, len - k * step);
-    }
-    return lo;
-}
-
-// The run that begins at `row`, if one does.
+// The run that begins at `row`, if one does.  Its sequence is the last one that does not begin behind the row: every look at 32 places of
+// row_start narrows it down by a factor of 32, and the last look brings the lengths with it.
 __device__ __forceinline__ KvRun kv_run(const KvCache &c, const KvRows &r, int row, int lane) {
     KvRun run;
-    int first = row, stop = row + 1;
+    int first = row, stop = row + 1, len;
     run.seq = row;
     if (r.row_start) {
-        run.seq = kv_find(r.row_start, c.n_seqs, row, lane);
-        first = __ldcg(r.row_start + run.seq);
-        stop = __ldcg(r.row_start + run.seq + 1);
+        int lo = 0, many = c.n_seqs;  // row_start[lo] <= row (or lo = 0), the answer in lo .. lo + many - 1
+        while (many > 31) {
+            const int step = (many + 31) / 32;
+            const unsigned below = __ballot_sync(0xffffffffu, lane * step < many && __ldcg(r.row_start + lo + lane * step) <= row);
+            const int k = below ? 31 - __clz(below) : 0;
+            lo += k * step;
+            many = min(step, many - k * step);
+        }
+        const bool on = lane <= many;  // (one place more: where the last sequence ends)
+        const int at = on ? __ldcg(r.row_start + lo + lane) : 0, tokens = lane < many ? __ldcg(c.lens + lo + lane) : 0;
+        const unsigned below = __ballot_sync(0xffffffffu, lane < many && at <= row);
+        const int k = below ? 31 - __clz(below) : 0;
+        run.seq = lo + k;
+        first = __shfl_sync(0xffffffffu, at, k);
+        stop = __shfl_sync(0xffffffffu, at, k + 1);
+        len = __shfl_sync(0xffffffffu, tokens, k);
+    } else {
+        len = __ldcg(c.lens + run.seq);
     }
-    const int len = __ldcg(c.lens + run.seq), end = min(stop, r.rows);
+    const int end = min(stop, r.rows);
     run.n = 0;
     run.pos = 0;
     run.next = row < first ? first : r.rows;  // before the first sequence, or behind the last one
@@ -107,8 +110,8 @@ __device__ __forceinline__ KvVec<CPL> kv_load(const void *p, long long i, bool o
 }
 
 // Codes of a lane's channels (nibble i = channel i) and the word of its group.  All lanes of the warp take part.
-template <int CPL, bool BF16>
-__device__ __forceinline__ uint32_t kv_quantise(const KvVec<CPL> &v, int group_lanes, uint32_t &word) {
+template <int CPL, int GL, bool BF16>
+__device__ __forceinline__ uint32_t kv_quantise(const KvVec<CPL> &v, uint32_t &word) {
     // smallest value and smallest negative in one register, per group of lanes
     uint32_t m = 0;  // (0, 0): the range always holds zero
 #pragma unroll
@@ -118,8 +121,7 @@ __device__ __forceinline__ uint32_t kv_quantise(const KvVec<CPL> &v, int group_l
         m = kv_min2<BF16>(m, __byte_perm(a, a ^ 0x80008000u, 0x7632));  // (x1, -x1)
     }
 #pragma unroll
-    for (int o = 1; o < 32; o *= 2)
-        if (o < group_lanes) m = kv_min2<BF16>(m, __shfl_xor_sync(0xffffffffu, m, o));
+    for (int o = 1; o < GL; o *= 2) m = kv_min2<BF16>(m, __shfl_xor_sync(0xffffffffu, m, o));
     float lo, hi;
     widen2<BF16>(m, lo, hi);
     hi = -hi;
@@ -167,14 +169,15 @@ __device__ __forceinline__ uint32_t kv_quantise(const KvVec<CPL> &v, int group_l
     return codes;
 }
 
-template <int D, bool BF16>
-__global__ void __launch_bounds__(KV_THREADS) kv4_append_kernel(const KvCache c, const KvRows r, int group) {
-    constexpr int CPL = D / 32;  // channels of a lane
+template <int D, int GROUP, bool BF16>
+__global__ void __launch_bounds__(KV_THREADS) kv4_append_kernel(const KvCache c, const KvRows r) {
+    constexpr int CPL = D / 32, GL = GROUP / CPL, GROUPS = D / GROUP;  // channels of a lane, lanes of a group
     griddep_wait();
     griddep_launch_dependents();
     const int lane = threadIdx.x & 31, t = threadIdx.x >> 5, h = blockIdx.y;
-    const int group_lanes = group / CPL, tile_bytes = kv_tile_bytes(D, c.groups), ch = lane * CPL, g = ch / group;
-    const bool writes = lane % group_lanes == 0;
+    constexpr int tile_bytes = kv_tile_bytes(D, GROUPS);
+    const int ch = lane * CPL, g = ch / GROUP;
+    const bool writes = lane % GL == 0;
     const int row0 = blockIdx.x * r.per_block, row1 = min(row0 + r.per_block, r.rows);
     for (int row = row0; row < row1;) {
         const KvRun run = kv_run(c, r, row, lane);
@@ -192,7 +195,7 @@ __global__ void __launch_bounds__(KV_THREADS) kv4_append_kernel(const KvCache c,
         const int page = kv_page(c, run.seq, run.pos);
         if (page < 0) continue;
         unsigned char *tile = kv_tile(c, page, h, run.pos, tile_bytes);
-        uint32_t *kw = reinterpret_cast<uint32_t *>(tile + kv_k_words(D)) + g * KV_TILE, *vw = reinterpret_cast<uint32_t *>(tile + kv_v_words(D, c.groups)) + g * KV_TILE;
+        uint32_t *kw = reinterpret_cast<uint32_t *>(tile + kv_k_words(D)) + g * KV_TILE, *vw = reinterpret_cast<uint32_t *>(tile + kv_v_words(D, GROUPS)) + g * KV_TILE;
         uint32_t *vcodes = reinterpret_cast<uint32_t *>(tile + kv_v_codes(D));
         uint32_t vcode[CPL];
 #pragma unroll
@@ -217,13 +220,13 @@ __global__ void __launch_bounds__(KV_THREADS) kv4_append_kernel(const KvCache c,
             const int tok = tok_of(i);
             if (tok < tok0 || tok >= tok0 + run.n) continue;  // (the same for all lanes)
             uint32_t word;
-            const uint32_t kc = kv_quantise<CPL, BF16>(k0, group_lanes, word);
+            const uint32_t kc = kv_quantise<CPL, GL, BF16>(k0, word);
             unsigned char *to = tile + tok * (D / 2) + kv_k_byte(D, ch);
             if constexpr (CPL == 2) *to = (unsigned char)kc;
             else if constexpr (CPL == 4) *reinterpret_cast<unsigned short *>(to) = (unsigned short)kc;
             else *reinterpret_cast<uint32_t *>(to) = kc;
             if (writes) kw[kv_word_at(tok)] = word;
-            const uint32_t vc = kv_quantise<CPL, BF16>(v0, group_lanes, word);
+            const uint32_t vc = kv_quantise<CPL, GL, BF16>(v0, word);
             if (writes) vw[kv_word_at(tok)] = word;
             const int nib = 4 * ((i >> 1) + 4 * (i & 1));
 #pragma unroll
@@ -250,12 +253,12 @@ __device__ __forceinline__ void kv_put(void *p, long long i, const uint32_t (&w)
     else *reinterpret_cast<uint4 *>(q) = make_uint4(w[0], w[1], w[2], w[3]);
 }
 
-template <int D, bool BF16>
-__global__ void __launch_bounds__(KV_THREADS) kv4_read_kernel(const KvCache c, const KvRows r, int group) {
-    constexpr int CPL = D / 32;
+template <int D, int GROUP, bool BF16>
+__global__ void __launch_bounds__(KV_THREADS) kv4_read_kernel(const KvCache c, const KvRows r) {
+    constexpr int CPL = D / 32, GROUPS = D / GROUP, tile_bytes = kv_tile_bytes(D, GROUPS);
     griddep_wait();
     griddep_launch_dependents();
-    const int lane = threadIdx.x & 31, t = threadIdx.x >> 5, h = blockIdx.y, tile_bytes = kv_tile_bytes(D, c.groups), ch = lane * CPL, g = ch / group;
+    const int lane = threadIdx.x & 31, t = threadIdx.x >> 5, h = blockIdx.y, ch = lane * CPL, g = ch / GROUP;
     const int row0 = blockIdx.x * r.per_block, row1 = min(row0 + r.per_block, r.rows);
     for (int row = row0; row < row1;) {
         const KvRun run = kv_run(c, r, row, lane);
@@ -265,7 +268,7 @@ __global__ void __launch_bounds__(KV_THREADS) kv4_read_kernel(const KvCache c, c
         const int page = kv_page(c, run.seq, run.pos);
         if (page < 0) continue;
         const unsigned char *tile = kv_tile(c, page, h, run.pos, tile_bytes);
-        const uint32_t *kw = reinterpret_cast<const uint32_t *>(tile + kv_k_words(D)) + g * KV_TILE, *vw = reinterpret_cast<const uint32_t *>(tile + kv_v_words(D, c.groups)) + g * KV_TILE;
+        const uint32_t *kw = reinterpret_cast<const uint32_t *>(tile + kv_k_words(D)) + g * KV_TILE, *vw = reinterpret_cast<const uint32_t *>(tile + kv_v_words(D, GROUPS)) + g * KV_TILE;
         uint32_t vcode[CPL], kcode[8], kword[8], vword[8];
 #pragma unroll
         for (int k = 0; k < CPL; ++k) vcode[k] = __ldcg(reinterpret_cast<const uint32_t *>(tile + kv_v_codes(D)) + kv_v_word(ch + k, t));
@@ -317,12 +320,12 @@ static int kv_per_block(long long rows, int heads) {
     return n < 1 ? 1 : (n > KV_TILE ? KV_TILE : (int)n);
 }
 
-template <int D>
-static cudaError_t kv_launch(bool append, bool bf16, const KvCache &c, const KvRows &r, int group, cudaStream_t st) {
+template <int D, int GROUP>
+static cudaError_t kv_launch(bool append, bool bf16, const KvCache &c, const KvRows &r, cudaStream_t st) {
     const dim3 grid((r.rows + r.per_block - 1) / r.per_block, c.heads), block(KV_THREADS);
     const bool pdl = g_tune.pdl != 0;
-    if (append) return bf16 ? launch(kv4_append_kernel<D, true>, grid, block, 0, st, pdl, c, r, group) : launch(kv4_append_kernel<D, false>, grid, block, 0, st, pdl, c, r, group);
-    return bf16 ? launch(kv4_read_kernel<D, true>, grid, block, 0, st, pdl, c, r, group) : launch(kv4_read_kernel<D, false>, grid, block, 0, st, pdl, c, r, group);
+    if (append) return bf16 ? launch(kv4_append_kernel<D, GROUP, true>, grid, block, 0, st, pdl, c, r) : launch(kv4_append_kernel<D, GROUP, false>, grid, block, 0, st, pdl, c, r);
+    return bf16 ? launch(kv4_read_kernel<D, GROUP, true>, grid, block, 0, st, pdl, c, r) : launch(kv4_read_kernel<D, GROUP, false>, grid, block, 0, st, pdl, c, r);
 }
 
 static scap_status kv_rows(bool append, const scap_kv4 *cache, const void *k, int64_t ldk, const void *v, int64_t ldv, const int *row_start, int rows, scap_dtype dt, scap_stream_t stream) {
@@ -343,10 +346,14 @@ static scap_status kv_rows(bool append, const scap_kv4 *cache, const void *k, in
     r.per_block = kv_per_block(rows, cache->heads);
     cudaStream_t st = reinterpret_cast<cudaStream_t>(stream);
     const bool bf16 = dt == SCAP_BF16;
-    switch (cache->head_dim) {
-        case 64: return cuda_status(kv_launch<64>(append, bf16, c, r, cache->group, st));
-        case 128: return cuda_status(kv_launch<128>(append, bf16, c, r, cache->group, st));
-        default: return cuda_status(kv_launch<256>(append, bf16, c, r, cache->group, st));
+    switch (cache->head_dim + cache->group) {
+        case 64 + 32: return cuda_status(kv_launch<64, 32>(append, bf16, c, r, st));
+        case 64 + 64: return cuda_status(kv_launch<64, 64>(append, bf16, c, r, st));
+        case 128 + 32: return cuda_status(kv_launch<128, 32>(append, bf16, c, r, st));
+        case 128 + 64: return cuda_status(kv_launch<128, 64>(append, bf16, c, r, st));
+        case 128 + 128: return cuda_status(kv_launch<128, 128>(append, bf16, c, r, st));
+        case 256 + 64: return cuda_status(kv_launch<256, 64>(append, bf16, c, r, st));
+        default: return cuda_status(kv_launch<256, 128>(append, bf16, c, r, st));
     }
 }
 
