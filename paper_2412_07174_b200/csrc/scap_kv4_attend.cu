@@ -54,9 +54,8 @@ struct AtArgs {
     int *status;
 };
 
-// Tiles that the new tokens of sequence b can see: first one and number.
-__device__ __forceinline__ int at_tiles(const AtArgs &a, int b, int &first) {
-    const int len = __ldcg(a.c.lens + b);
+// Tiles that the new tokens of a sequence of `len` tokens can see: first one and number.
+__device__ __forceinline__ int at_tiles_of(const AtArgs &a, int len, int &first) {
     first = 0;
     if (len <= 0) return 0;
     if (a.window > 0) {
@@ -76,6 +75,8 @@ __device__ __forceinline__ int at_ctas(const AtArgs &a, long long units, long lo
     const int most = units >= (long long)AT_TWO_WAVES * a.resident ? 2 * a.resident : a.resident;
     return n < most ? (int)n : most;
 }
+
+__device__ __forceinline__ int at_tiles(const AtArgs &a, int b, int &first) { return at_tiles_of(a, __ldcg(a.c.lens + b), first); }
 
 // Number of tiles of all sequences, and of the sequences that have any (the whole block takes part).
 __device__ __forceinline__ long long at_count(const AtArgs &a, long long *s, int &some) {
@@ -99,9 +100,9 @@ __device__ __forceinline__ long long at_count(const AtArgs &a, long long *s, int
     return all;
 }
 
-// This CTA's units [u, u1), the sequence that u belongs to and the first unit of that sequence (the whole block takes part); per = items
+// This CTA's units [u, u1), the sequence that u belongs to, its length and its first unit (the whole block takes part); per = items
 // per sequence.  False: there is nothing for this CTA.
-__device__ __forceinline__ bool at_begin(const AtArgs &a, int per, long long *s, long long &u, long long &u1, int &seq, long long &base) {
+__device__ __forceinline__ bool at_begin(const AtArgs &a, int per, long long *s, long long &u, long long &u1, int &seq, int &len, long long &base) {
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
     long long units = 0, before = 0;
     const bool one = a.c.n_seqs <= AT_THREADS;  // one look at the lengths gives the sum and the place
@@ -110,7 +111,8 @@ __device__ __forceinline__ bool at_begin(const AtArgs &a, int per, long long *s,
     for (int b0 = 0; b0 < a.c.n_seqs; b0 += AT_THREADS) {
         const int b = b0 + (int)threadIdx.x;
         int first;
-        const long long n = b < a.c.n_seqs ? (long long)at_tiles(a, b, first) * per : 0;
+        const int tokens = b < a.c.n_seqs ? __ldcg(a.c.lens + b) : 0;
+        const long long n = (long long)at_tiles_of(a, tokens, first) * per;
         long long incl = n;
 #pragma unroll
         for (int o = 1; o < 32; o *= 2) {
@@ -134,6 +136,7 @@ __device__ __forceinline__ bool at_begin(const AtArgs &a, int per, long long *s,
         if (n > 0 && off + incl - n <= u && u < off + incl) {
             s[AT_WARPS] = b;
             s[AT_WARPS + 1] = off + incl - n;
+            s[AT_WARPS + 2] = tokens;
         }
         before = all;
         __syncthreads();
@@ -141,6 +144,7 @@ __device__ __forceinline__ bool at_begin(const AtArgs &a, int per, long long *s,
     }
     seq = (int)s[AT_WARPS];
     base = s[AT_WARPS + 1];
+    len = (int)s[AT_WARPS + 2];
     return true;
 }
 
@@ -188,7 +192,7 @@ __global__ void __launch_bounds__(AT_THREADS, at_resident(D, G, RN)) kv4_attend_
     __shared__ uint32_t s_zq[QS ? RN : 1][G][32];
     __shared__ float s_f[RN];
     __shared__ unsigned long long s_full[AT_WARPS][ST];
-    __shared__ long long s_sum[AT_WARPS + 2];
+    __shared__ long long s_sum[AT_WARPS + 3];
     __shared__ float s_m[AT_WARPS][ROWS], s_l[AT_WARPS][ROWS];
 
     const int tid = threadIdx.x, warp = __shfl_sync(0xffffffffu, tid >> 5, 0), lane = tid & 31, qg = lane >> 2, qt = lane & 3;
@@ -201,19 +205,22 @@ __global__ void __launch_bounds__(AT_THREADS, at_resident(D, G, RN)) kv4_attend_
 
     const int per = a.c.heads * a.row_tiles;
     long long u, u1, base;
-    int seq;
-    if (!at_begin(a, per, s_sum, u, u1, seq, base)) return;
+    int seq, len;
+    if (!at_begin(a, per, s_sum, u, u1, seq, len, base)) return;
     int slot = 0, phase = 0;  // of this warp's ring, over all items
     bool dead = false;        // a wait of this warp ran out
 
     while (u < u1) {
         int first_tile;
-        const int tiles = at_tiles(a, seq, first_tile);
-        if (tiles == 0) { ++seq; continue; }  // (an empty sequence has no units; its rows are the second kernel's)
+        const int tiles = at_tiles_of(a, len, first_tile);
+        if (tiles == 0) {  // (an empty sequence has no units; its rows are the second kernel's)
+            len = __ldcg(a.c.lens + ++seq);
+            continue;
+        }
         const int item = (int)((u - base) / tiles), t0 = (int)(u - base - (long long)item * tiles);
         const int t1 = (int)min((long long)tiles, t0 + (u1 - u));
         const int rt = item / a.c.heads, h = item - rt * a.c.heads;
-        const int len = __ldcg(a.c.lens + seq), rows = min(ROWS, a.nq * a.g - rt * ROWS);
+        const int rows = min(ROWS, a.nq * a.g - rt * ROWS);
         const int count = !dead && t1 - t0 - warp > 0 ? (t1 - t0 - warp + AT_WARPS - 1) / AT_WARPS : 0;  // tiles t0 + warp, + 4, ... are this warp's
 
         // ---- addresses of the next 32 tiles of this warp, one per lane (0: no page), and the first copies
@@ -630,7 +637,7 @@ __global__ void __launch_bounds__(AT_THREADS, at_resident(D, G, RN)) kv4_attend_
         asm volatile("fence.proxy.async.shared::cta;" ::: "memory");  // the next copies may overwrite what was read and written here
         __syncthreads();
         u += t1 - t0;
-        if (u - base >= (long long)tiles * per) { base += (long long)tiles * per; ++seq; }
+        if (u - base >= (long long)tiles * per && u < u1) { base += (long long)tiles * per; len = __ldcg(a.c.lens + ++seq); }
     }
 }
 
