@@ -43,8 +43,8 @@ struct AtArgs {
     unsigned short *out;
     float *lse;
     long long ldq, ldo;   // elements between tokens
-    float *part;          // [4 resident][8 RN][D] weighted sums, then [4 resident][8 RN][2] reference and sum
-    int2 *where;          // [n_seqs][items]: first and last CTA of an item that was cut, equal where it was not
+    float *part, *ml;     // parts of items that were cut, two per worker: [8 RN][D] weighted sums, [8 RN][2] reference and sum
+    int2 *where;          // [n_seqs][items]: first and last worker of an item that was cut, equal where it was not
     int nq, g, row_tiles, window;
     float scale;          // times log2 e
     int tile_cap;         // tiles that a row of the table has room for
@@ -66,14 +66,19 @@ __device__ __forceinline__ int at_tiles_of(const AtArgs &a, int len, int &first)
     return max(0, min((int)(((long long)len + KV_TILE - 1) / KV_TILE), a.tile_cap) - first);
 }
 
-__device__ __forceinline__ long long at_cut(long long units, int i, int ctas) { return units * i / ctas; }
-// CTAs that share the units.  Where there is much to do twice as many as the device holds: the SMs favour the older ones of their CTAs, and
-// the younger ones of a second wave take over from those (83 units per resident CTA: 75 -> 71 us; 55 units: 42 -> 52).
+__device__ __forceinline__ long long at_cut(long long units, int i, int workers) { return units * i / workers; }
+// CTAs that share the units, and workers in them: the CTA, or (SOLO) each of its warps.  Where there is much to do there are twice as many CTAs as
+// the device holds: the SMs favour the older ones of their CTAs, and the younger ones of a second wave take over from those (83 units
+// per resident CTA: 75 -> 71 us; 55 units: 42 -> 52).
 constexpr int AT_TWO_WAVES = 64;
-__device__ __forceinline__ int at_ctas(const AtArgs &a, long long units, long long items) {
+template <bool SOLO>
+__device__ __forceinline__ int at_workers(const AtArgs &a, long long units, long long items, int &ctas) {
+    constexpr int PER = SOLO ? AT_WARPS : 1;
     const long long n = max((units + AT_MIN_UNITS - 1) / AT_MIN_UNITS, items);
     const int most = units >= (long long)AT_TWO_WAVES * a.resident ? 2 * a.resident : a.resident;
-    return n < most ? (int)n : most;
+    const int workers = n < (long long)PER * most ? (int)n : PER * most;
+    ctas = min(most, workers);  // (SOLO: worker w is warp w / ctas of CTA w % ctas, so that few of them lie in different CTAs)
+    return workers;
 }
 
 __device__ __forceinline__ int at_tiles(const AtArgs &a, int b, int &first) { return at_tiles_of(a, __ldcg(a.c.lens + b), first); }
@@ -100,13 +105,19 @@ __device__ __forceinline__ long long at_count(const AtArgs &a, long long *s, int
     return all;
 }
 
-// This CTA's units [u, u1), the sequence that u belongs to, its length and its first unit (the whole block takes part); per = items
-// per sequence.  False: there is nothing for this CTA.
-__device__ __forceinline__ bool at_begin(const AtArgs &a, int per, long long *s, long long &u, long long &u1, int &seq, int &len, long long &base) {
+// The units of a worker, the number of the worker, the sequence that its first unit belongs to, that sequence's length and first unit.
+struct AtPlace {
+    long long u, u1, base;
+    int id, seq, len;
+};
+// This worker's place (the whole block takes part); per = items per sequence.  False: there is nothing for this CTA.
+template <bool SOLO>
+__device__ __forceinline__ bool at_begin(const AtArgs &a, int per, long long *s, AtPlace &p) {
+    constexpr int PER = SOLO ? AT_WARPS : 1;
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
     long long units = 0, before = 0;
     const bool one = a.c.n_seqs <= AT_THREADS;  // one look at the lengths gives the sum and the place
-    int some = 0;
+    int some = 0, ctas = 0, workers = 0;
     if (!one) units = at_count(a, s, some) * per;
     for (int b0 = 0; b0 < a.c.n_seqs; b0 += AT_THREADS) {
         const int b = b0 + (int)threadIdx.x;
@@ -129,22 +140,37 @@ __device__ __forceinline__ bool at_begin(const AtArgs &a, int per, long long *s,
             all += s[w];
         }
         if (one) units = all;
-        const int ctas = at_ctas(a, units, (long long)some * per);
+        workers = at_workers<SOLO>(a, units, (long long)some * per, ctas);
         if ((int)blockIdx.x >= ctas) return false;
-        u = at_cut(units, blockIdx.x, ctas);
-        u1 = at_cut(units, blockIdx.x + 1, ctas);
-        if (n > 0 && off + incl - n <= u && u < off + incl) {
-            s[AT_WARPS] = b;
-            s[AT_WARPS + 1] = off + incl - n;
-            s[AT_WARPS + 2] = tokens;
+        long long last = 0;
+#pragma unroll
+        for (int w = 0; w < PER; ++w) {
+            const int id = (int)blockIdx.x + w * ctas;
+            if (id >= workers) break;
+            const long long u = at_cut(units, id, workers);
+            if (n > 0 && off + incl - n <= u && u < off + incl) {
+                s[AT_WARPS + 3 * w] = b;
+                s[AT_WARPS + 3 * w + 1] = off + incl - n;
+                s[AT_WARPS + 3 * w + 2] = tokens;
+            }
+            last = u;
         }
         before = all;
         __syncthreads();
-        if (u < before) break;
+        if (last < before) break;
     }
-    seq = (int)s[AT_WARPS];
-    base = s[AT_WARPS + 1];
-    len = (int)s[AT_WARPS + 2];
+    const int w = SOLO ? warp : 0;
+    p.id = (int)blockIdx.x + w * ctas;
+    p.u = p.u1 = 0;
+    p.seq = p.len = 0;
+    p.base = 0;
+    if (p.id < workers) {
+        p.u = at_cut(units, p.id, workers);
+        p.u1 = at_cut(units, p.id + 1, workers);
+        p.seq = (int)s[AT_WARPS + 3 * w];
+        p.base = s[AT_WARPS + 3 * w + 1];
+        p.len = (int)s[AT_WARPS + 3 * w + 2];
+    }
     return true;
 }
 
@@ -175,7 +201,7 @@ __device__ __forceinline__ void at_store(unsigned short *p, float v, bool bf16) 
 // 2^e for -126 <= e <= 127
 __device__ __forceinline__ float at_pow2(int e) { return __int_as_float((e + 127) << 23); }
 
-template <int D, int G, int RN>
+template <int D, int G, int RN, bool SOLO>
 __global__ void __launch_bounds__(AT_THREADS, at_resident(D, G, RN)) kv4_attend_kernel(const AtArgs a) {
     constexpr int W = D / 32;            // words of a K row per lane
     constexpr int TILE = kv_tile_bytes(D, G);
@@ -187,12 +213,14 @@ __global__ void __launch_bounds__(AT_THREADS, at_resident(D, G, RN)) kv4_attend_
     static_assert(ST * TILE >= ROWS * PITCH * 4, "a warp's part of the join goes where its ring was");
     // Sixteen rows: the queries are B operands in shared memory, one 16-byte load for two MMAs, where their registers would spill.
     constexpr bool QS = RN == 2;
+    static_assert(!(SOLO && QS), "a warp on its own has its queries in registers");
+    constexpr int STEP = SOLO ? 1 : AT_WARPS;  // the tiles of an item go round so many warps
     extern __shared__ __align__(128) unsigned char at_raw[];
     uint4 *s_q = reinterpret_cast<uint4 *>(at_raw + AT_WARPS * ST * TILE);  // [RN][W][32 lanes]
     __shared__ uint32_t s_zq[QS ? RN : 1][G][32];
     __shared__ float s_f[RN];
     __shared__ unsigned long long s_full[AT_WARPS][ST];
-    __shared__ long long s_sum[AT_WARPS + 3];
+    __shared__ long long s_sum[AT_WARPS + 3 * (SOLO ? AT_WARPS : 1)];
     __shared__ float s_m[AT_WARPS][ROWS], s_l[AT_WARPS][ROWS];
 
     const int tid = threadIdx.x, warp = __shfl_sync(0xffffffffu, tid >> 5, 0), lane = tid & 31, qg = lane >> 2, qt = lane & 3;
@@ -204,9 +232,12 @@ __global__ void __launch_bounds__(AT_THREADS, at_resident(D, G, RN)) kv4_attend_
     griddep_launch_dependents();  // (after the wait: the second kernel may rely on all work before this one)
 
     const int per = a.c.heads * a.row_tiles;
-    long long u, u1, base;
-    int seq, len;
-    if (!at_begin(a, per, s_sum, u, u1, seq, len, base)) return;
+    AtPlace place;
+    if (!at_begin<SOLO>(a, per, s_sum, place)) return;
+    long long u = place.u, base = place.base;
+    const long long u1 = place.u1;
+    int seq = place.seq, len = place.len;
+    const int own = SOLO ? 0 : warp;  // this warp's first tile of those that its worker has of an item
     int slot = 0, phase = 0;  // of this warp's ring, over all items
     bool dead = false;        // a wait of this warp ran out
 
@@ -221,13 +252,13 @@ __global__ void __launch_bounds__(AT_THREADS, at_resident(D, G, RN)) kv4_attend_
         const int t1 = (int)min((long long)tiles, t0 + (u1 - u));
         const int rt = item / a.c.heads, h = item - rt * a.c.heads;
         const int rows = min(ROWS, a.nq * a.g - rt * ROWS);
-        const int count = !dead && t1 - t0 - warp > 0 ? (t1 - t0 - warp + AT_WARPS - 1) / AT_WARPS : 0;  // tiles t0 + warp, + 4, ... are this warp's
+        const int count = !dead && t1 - t0 - own > 0 ? (t1 - t0 - own + STEP - 1) / STEP : 0;  // tiles t0 + own, + STEP, ... are this warp's
 
         // ---- addresses of the next 32 tiles of this warp, one per lane (0: no page), and the first copies
-        auto pos_of = [&](int i) { return (first_tile + t0 + warp + AT_WARPS * i) * KV_TILE; };
+        auto pos_of = [&](int i) { return (first_tile + t0 + own + STEP * i) * KV_TILE; };
         auto where = [&](int i) -> unsigned long long {
             if (i >= count) return 0ull;
-            const int per_page = a.c.page_tokens / KV_TILE, t = first_tile + t0 + warp + AT_WARPS * i, at = t / per_page;
+            const int per_page = a.c.page_tokens / KV_TILE, t = first_tile + t0 + own + STEP * i, at = t / per_page;
             if (at >= a.c.table_stride) return 0ull;
             const int page = __ldcg(a.c.table + (long long)seq * a.c.table_stride + at);
             if (page < 0 || page >= a.c.n_pages) return 0ull;
@@ -591,25 +622,27 @@ __global__ void __launch_bounds__(AT_THREADS, at_resident(D, G, RN)) kv4_attend_
                     part[row * PITCH + 16 * n + 8 + qg] = (o[rn][n][2 + k] - zz) * back1 * back2;
                 }
             }
-        __syncthreads();
+        if constexpr (SOLO) __syncwarp();
+        else __syncthreads();
         const bool whole = t0 == 0 && t1 == tiles;
-        if (tid == 0) {
+        if (SOLO ? lane == 0 : tid == 0) {
             int2 *at = a.where + (long long)seq * per + item;
             if (whole) *at = make_int2(-1, -1);
-            else if (t0 == 0) at->x = blockIdx.x;
-            else if (t1 == tiles) at->y = blockIdx.x;
+            else if (t0 == 0) at->x = place.id;
+            else if (t1 == tiles) at->y = place.id;
         }
-        const int slot_out = 2 * (int)blockIdx.x + (t0 == 0 ? 1 : 0);
-        float *sums = a.part + (size_t)slot_out * ROWS * D, *ml = a.part + (size_t)4 * a.resident * ROWS * D + (size_t)slot_out * ROWS * 2;
-        for (int row = warp; row < rows; row += AT_WARPS) {
-            float top = -INFINITY, wt[AT_WARPS], sum = 0.0f;
+        const int slot_out = 2 * place.id + (t0 == 0 ? 1 : 0);
+        float *sums = a.part + (size_t)slot_out * ROWS * D, *ml = a.ml + (size_t)slot_out * ROWS * 2;
+        constexpr int NW = SOLO ? 1 : AT_WARPS;
+        for (int row = own; row < rows; row += STEP) {
+            float top = -INFINITY, wt[NW], sum = 0.0f;
 #pragma unroll
-            for (int w = 0; w < AT_WARPS; ++w) top = fmaxf(top, s_m[w][row]);
+            for (int w = 0; w < NW; ++w) top = fmaxf(top, s_m[SOLO ? warp : w][row]);
             const float ref = top == -INFINITY ? 0.0f : top;
 #pragma unroll
-            for (int w = 0; w < AT_WARPS; ++w) {
-                wt[w] = at_ex2(s_m[w][row] - ref);
-                sum += wt[w] * s_l[w][row];
+            for (int w = 0; w < NW; ++w) {
+                wt[w] = at_ex2(s_m[SOLO ? warp : w][row] - ref);
+                sum += wt[w] * s_l[SOLO ? warp : w][row];
             }
             const float by = whole ? (sum > 0.0f || sum != sum ? 1.0f / sum : 0.0f) : 1.0f;
             const int in = rt * ROWS + row, tok = in / a.g, hd = in - tok * a.g;
@@ -618,8 +651,8 @@ __global__ void __launch_bounds__(AT_THREADS, at_resident(D, G, RN)) kv4_attend_
             for (int c = 0; c < D; c += 32) {
                 float v = 0.0f;
 #pragma unroll
-                for (int w = 0; w < AT_WARPS; ++w) {
-                    const float x = reinterpret_cast<const float *>(at_raw + w * ST * TILE)[row * PITCH + c + lane];
+                for (int w = 0; w < NW; ++w) {
+                    const float x = reinterpret_cast<const float *>(at_raw + (SOLO ? warp : w) * ST * TILE)[row * PITCH + c + lane];
                     v += wt[w] > 0.0f || x != x ? wt[w] * x : 0.0f;
                 }
                 if (whole) at_store(a.out + tokrow * a.ldo + (long long)(h * a.g + hd) * D + c + lane, v * by, a.bf16);
@@ -635,7 +668,8 @@ __global__ void __launch_bounds__(AT_THREADS, at_resident(D, G, RN)) kv4_attend_
             }
         }
         asm volatile("fence.proxy.async.shared::cta;" ::: "memory");  // the next copies may overwrite what was read and written here
-        __syncthreads();
+        if constexpr (SOLO) __syncwarp();
+        else __syncthreads();
         u += t1 - t0;
         if (u - base >= (long long)tiles * per && u < u1) { base += (long long)tiles * per; len = __ldcg(a.c.lens + ++seq); }
     }
@@ -651,7 +685,7 @@ __global__ void __launch_bounds__(AT_THREADS) kv4_join_kernel(const AtArgs a) {
     const long long tokrow = (long long)seq * a.nq + tok;
     unsigned short *out = a.out + tokrow * a.ldo + (long long)(h * a.g + hd) * D;
     float *lse = a.lse ? a.lse + tokrow * (a.c.heads * a.g) + h * a.g + hd : nullptr;
-    const float *ml = a.part + (size_t)4 * a.resident * ROWS * D;
+    const float *ml = a.ml;
     griddep_wait();
     griddep_launch_dependents();
     if (in >= a.nq * a.g) return;
@@ -724,11 +758,11 @@ __global__ void __launch_bounds__(AT_THREADS) kv4_join_kernel(const AtArgs a) {
     if (lse && tid == 0) *lse = any ? top * LN2 + logf(sum) : -INFINITY;
 }
 
-template <int D, int G, int RN>
+template <int D, int G, int RN, bool SOLO>
 static cudaError_t at_launch_rn(const AtArgs &a, int grid, cudaStream_t st) {
     static SmemOptIn opt_in;
     constexpr int SMEM = AT_WARPS * at_stages(D, G, RN) * kv_tile_bytes(D, G) + (RN == 2 ? RN * D / 32 * 32 * 16 : 0);
-    auto kern = kv4_attend_kernel<D, G, RN>;
+    auto kern = kv4_attend_kernel<D, G, RN, SOLO>;
     cudaError_t e = ensure_dynamic_smem(kern, SMEM, opt_in);
     if (e != cudaSuccess) return e;
     e = launch(kern, dim3(grid), dim3(AT_THREADS), SMEM, st, g_tune.pdl != 0, a);
@@ -736,13 +770,30 @@ static cudaError_t at_launch_rn(const AtArgs &a, int grid, cudaStream_t st) {
     const int rows = a.nq * a.g < 8 * RN ? a.nq * a.g : 8 * RN;
     return launch(kv4_join_kernel<D, 8 * RN>, dim3(a.c.n_seqs, a.c.heads * a.row_tiles, rows), dim3(AT_THREADS), 0, st, g_tune.pdl != 0, a);
 }
-template <int D, int G>
-static cudaError_t at_launch(const AtArgs &a, int rn, int grid, cudaStream_t st) {
-    return rn == 1 ? at_launch_rn<D, G, 1>(a, grid, st) : at_launch_rn<D, G, 2>(a, grid, st);
+
+// How the rows and items of a call are taken.  Eight rows at a time where a head has no more than that, else sixteen: the cache is then
+// read (and unpacked) half as often.  Warps work on their own (SOLO) where there are two items and more for every CTA that the device
+// holds: an item then costs no barriers, its queries are prepared once, and its tiles need not be a multiple of four.
+struct AtPlan {
+    int rn, items, resident;
+    bool solo;
+    size_t parts() const { return (size_t)2 * (solo ? AT_WARPS : 1) * 2 * resident; }  // two waves, two parts per worker
+};
+static AtPlan at_plan(int n_seqs, int nq, int q_heads, int heads, int D, int G) {
+    AtPlan p;
+    const int rows = nq * (q_heads / heads);
+    p.rn = rows <= 8 ? 1 : 2;
+    p.items = heads * ((rows + 8 * p.rn - 1) / (8 * p.rn));  // per sequence
+    p.resident = sm_count() * at_resident(D, G, p.rn);
+    p.solo = p.rn == 1 && (long long)n_seqs * p.items >= 2LL * p.resident;
+    return p;
 }
 
-// Eight rows at a time where a head has no more than that, else sixteen: the cache is then read (and unpacked) half as often.
-static int at_row_groups(int rows) { return rows <= 8 ? 1 : 2; }
+template <int D, int G>
+static cudaError_t at_launch(const AtArgs &a, const AtPlan &p, int grid, cudaStream_t st) {
+    if (p.solo) return at_launch_rn<D, G, 1, true>(a, grid, st);
+    return p.rn == 1 ? at_launch_rn<D, G, 1, false>(a, grid, st) : at_launch_rn<D, G, 2, false>(a, grid, st);
+}
 
 }  // namespace scap
 
@@ -751,10 +802,13 @@ using namespace scap;
 extern "C" size_t scap_kv4_attend_workspace(int n_seqs, int nq, int q_heads, int heads, int head_dim) {
     if (n_seqs < 1 || n_seqs > SCAP_MAX_SEQS || nq < 1 || nq > SCAP_MAX_BATCH || heads < 1 || heads > 1024 || q_heads < heads || q_heads % heads || q_heads > 1024) return 0;
     if (head_dim != 64 && head_dim != 128 && head_dim != 256) return 0;
-    const int rn = at_row_groups(nq * (q_heads / heads));
-    const int items = heads * ((nq * (q_heads / heads) + 8 * rn - 1) / (8 * rn));
-    return (size_t)4 * sm_count() * at_resident(head_dim, 1, rn) * 8 * rn * (head_dim + 2) * sizeof(float)  // (G = 1: the most CTAs)
-           + (size_t)n_seqs * items * sizeof(int2);
+    size_t most = 0;
+    for (int G = 1; G <= 4; G *= 2) {  // (the number of groups decides how many CTAs the device holds)
+        const AtPlan p = at_plan(n_seqs, nq, q_heads, heads, head_dim, G);
+        const size_t bytes = p.parts() * 8 * p.rn * (head_dim + 2) * sizeof(float) + (size_t)n_seqs * p.items * sizeof(int2);
+        most = bytes > most ? bytes : most;
+    }
+    return most;
 }
 
 extern "C" scap_status scap_kv4_attend(const scap_kv4 *cache, const void *q, int64_t ldq, void *out, int64_t ldo, float *lse, int nq, int q_heads, double scale, int window,
@@ -778,11 +832,11 @@ extern "C" scap_status scap_kv4_attend(const scap_kv4 *cache, const void *q, int
     a.lse = lse; a.ldq = ldq; a.ldo = ldo;
     a.part = reinterpret_cast<float *>(ws);
     a.nq = nq; a.g = q_heads / cache->heads;
-    const int rn = at_row_groups(nq * a.g);
-    a.row_tiles = (nq * a.g + 8 * rn - 1) / (8 * rn);
+    const AtPlan p = at_plan(cache->n_seqs, nq, q_heads, cache->heads, cache->head_dim, a.c.groups);
+    a.row_tiles = p.items / cache->heads;
     a.window = window;
     a.scale = (float)(scale * 1.4426950408889634);
-    a.resident = sm_count() * at_resident(cache->head_dim, a.c.groups, rn);
+    a.resident = p.resident;
     // What the tables have room for bounds the work: no more CTAs than that takes.
     const long long cap = (long long)cache->table_stride * (cache->page_tokens / KV_TILE), seen = window > 0 ? ((long long)window + nq) / KV_TILE + 2 : cap;
     a.tile_cap = (int)(cap < (1ll << 30) ? cap : (1ll << 30));
@@ -790,18 +844,19 @@ extern "C" scap_status scap_kv4_attend(const scap_kv4 *cache, const void *q, int
     const long long few = (units + AT_MIN_UNITS - 1) / AT_MIN_UNITS > items ? (units + AT_MIN_UNITS - 1) / AT_MIN_UNITS : items;
     const int most = units >= (long long)AT_TWO_WAVES * a.resident ? 2 * a.resident : a.resident;
     const int grid = few < most ? (int)few : most;
-    a.where = reinterpret_cast<int2 *>(a.part + (size_t)4 * a.resident * 8 * rn * (cache->head_dim + 2));
+    a.ml = a.part + p.parts() * 8 * p.rn * cache->head_dim;
+    a.where = reinterpret_cast<int2 *>(a.ml + p.parts() * 8 * p.rn * 2);
     a.bf16 = dt == SCAP_BF16;
     a.limit = g_tune.tc_spin ? (uint32_t)g_tune.tc_spin : TRIES;
     a.status = tc_status_ptr();
     cudaStream_t st = reinterpret_cast<cudaStream_t>(stream);
     switch (cache->head_dim * 8 + a.c.groups) {
-        case 64 * 8 + 1: return cuda_status(at_launch<64, 1>(a, rn, grid, st));
-        case 64 * 8 + 2: return cuda_status(at_launch<64, 2>(a, rn, grid, st));
-        case 128 * 8 + 1: return cuda_status(at_launch<128, 1>(a, rn, grid, st));
-        case 128 * 8 + 2: return cuda_status(at_launch<128, 2>(a, rn, grid, st));
-        case 128 * 8 + 4: return cuda_status(at_launch<128, 4>(a, rn, grid, st));
-        case 256 * 8 + 2: return cuda_status(at_launch<256, 2>(a, rn, grid, st));
-        default: return cuda_status(at_launch<256, 4>(a, rn, grid, st));
+        case 64 * 8 + 1: return cuda_status(at_launch<64, 1>(a, p, grid, st));
+        case 64 * 8 + 2: return cuda_status(at_launch<64, 2>(a, p, grid, st));
+        case 128 * 8 + 1: return cuda_status(at_launch<128, 1>(a, p, grid, st));
+        case 128 * 8 + 2: return cuda_status(at_launch<128, 2>(a, p, grid, st));
+        case 128 * 8 + 4: return cuda_status(at_launch<128, 4>(a, p, grid, st));
+        case 256 * 8 + 2: return cuda_status(at_launch<256, 2>(a, p, grid, st));
+        default: return cuda_status(at_launch<256, 4>(a, p, grid, st));
     }
 }

@@ -141,6 +141,22 @@ def test_many_and_long(B, most):
 
 
 @pytest.mark.gpu
+@pytest.mark.parametrize("D,group,heads,B,most,nq,g,window", [(64, 32, 8, 200, 90, 1, 3, 0), (128, 128, 16, 90, 300, 2, 4, 0), (128, 32, 6, 260, 60, 1, 8, 25),
+                                                              (256, 128, 4, 240, 50, 1, 2, 0), (64, 64, 40, 41, 2500, 1, 1, 700)])
+def test_a_warp_for_every_item(D, group, heads, B, most, nq, g, window):
+    """So many sequences and heads that each warp works on its own, lengths from none to a few that are cut."""
+    rng = np.random.default_rng(B)
+    lens = (most * rng.random(B) ** 3).astype(int).tolist()
+    lens[B // 2] = 4 * most
+    c = filled(lens, heads, D, group, page=32, seed=B, fill=255)
+    q = queries(B, nq, g * heads, D, BF)
+    out, lse = attend(c, q, D ** -0.5, window)
+    check(c, q, out, lse, lens, nq, D ** -0.5, window)
+    again, lse2 = attend(c, q, D ** -0.5, window)
+    assert torch.equal(out, again) and torch.equal(lse, lse2)
+
+
+@pytest.mark.gpu
 def test_peaked_and_large_scores():
     lens = [700, 64]
     for scale in (3.0, -0.5, 0.0, 50.0):
