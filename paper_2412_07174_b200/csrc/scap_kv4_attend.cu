@@ -48,7 +48,7 @@ struct AtArgs {
     int nq, g, row_tiles, window;
     float scale;          // times log2 e
     int tile_cap;         // tiles that a row of the table has room for
-    int resident;         // CTAs that the device holds at once
+    int resident, waves;  // CTAs that the device holds at once, and how many times that there may be
     bool bf16;
     uint32_t limit;
     int *status;
@@ -75,7 +75,7 @@ template <bool SOLO>
 __device__ __forceinline__ int at_workers(const AtArgs &a, long long units, long long items, int &ctas) {
     constexpr int PER = SOLO ? AT_WARPS : 1;
     const long long n = max((units + AT_MIN_UNITS - 1) / AT_MIN_UNITS, items);
-    const int most = units >= (long long)AT_TWO_WAVES * a.resident ? 2 * a.resident : a.resident;
+    const int most = units >= (long long)AT_TWO_WAVES * a.resident ? a.waves * a.resident : a.resident;
     const int workers = n < (long long)PER * most ? (int)n : PER * most;
     ctas = min(most, workers);  // (SOLO: worker w is warp w / ctas of CTA w % ctas, so that few of them lie in different CTAs)
     return workers;
@@ -142,19 +142,31 @@ __device__ __forceinline__ bool at_begin(const AtArgs &a, int per, long long *s,
         if (one) units = all;
         workers = at_workers<SOLO>(a, units, (long long)some * per, ctas);
         if ((int)blockIdx.x >= ctas) return false;
+        // (SOLO: a cut is moved to a border between items that lies within half a share of it, so that short items stay whole)
+        const long long near = SOLO ? units / workers / 2 : 0, tiles = per > 0 ? n / per : 0;
         long long last = 0;
 #pragma unroll
-        for (int w = 0; w < PER; ++w) {
-            const int id = (int)blockIdx.x + w * ctas;
-            if (id >= workers) break;
-            const long long u = at_cut(units, id, workers);
-            if (n > 0 && off + incl - n <= u && u < off + incl) {
-                s[AT_WARPS + 3 * w] = b;
-                s[AT_WARPS + 3 * w + 1] = off + incl - n;
-                s[AT_WARPS + 3 * w + 2] = tokens;
+        for (int w = 0; w < PER; ++w)
+#pragma unroll
+            for (int e = 0; e < (SOLO ? 2 : 1); ++e) {
+                const int id = (int)blockIdx.x + w * ctas + e;
+                if (id >= workers) break;
+                const long long u = at_cut(units, id, workers);
+                if (n > 0 && off + incl - n <= u && u < off + incl) {
+                    long long moved = u;
+                    if (SOLO) {
+                        const long long over = (u - (off + incl - n)) % tiles;
+                        moved = over <= near ? u - over : (tiles - over <= near ? u + tiles - over : u);
+                    }
+                    if (e == 0) {
+                        s[AT_WARPS + 5 * w] = b;
+                        s[AT_WARPS + 5 * w + 1] = off + incl - n;
+                        s[AT_WARPS + 5 * w + 2] = tokens;
+                    }
+                    s[AT_WARPS + 5 * w + 3 + e] = moved;
+                }
+                last = u;
             }
-            last = u;
-        }
         before = all;
         __syncthreads();
         if (last < before) break;
@@ -165,11 +177,11 @@ __device__ __forceinline__ bool at_begin(const AtArgs &a, int per, long long *s,
     p.seq = p.len = 0;
     p.base = 0;
     if (p.id < workers) {
-        p.u = at_cut(units, p.id, workers);
-        p.u1 = at_cut(units, p.id + 1, workers);
-        p.seq = (int)s[AT_WARPS + 3 * w];
-        p.base = s[AT_WARPS + 3 * w + 1];
-        p.len = (int)s[AT_WARPS + 3 * w + 2];
+        p.u = s[AT_WARPS + 5 * w + 3];
+        p.u1 = p.id + 1 == workers ? units : (SOLO ? s[AT_WARPS + 5 * w + 4] : at_cut(units, p.id + 1, workers));
+        p.seq = (int)s[AT_WARPS + 5 * w];
+        p.base = s[AT_WARPS + 5 * w + 1];
+        p.len = (int)s[AT_WARPS + 5 * w + 2];
     }
     return true;
 }
@@ -220,7 +232,7 @@ __global__ void __launch_bounds__(AT_THREADS, at_resident(D, G, RN)) kv4_attend_
     __shared__ uint32_t s_zq[QS ? RN : 1][G][32];
     __shared__ float s_f[RN];
     __shared__ unsigned long long s_full[AT_WARPS][ST];
-    __shared__ long long s_sum[AT_WARPS + 3 * (SOLO ? AT_WARPS : 1)];
+    __shared__ long long s_sum[AT_WARPS + 5 * (SOLO ? AT_WARPS : 1)];
     __shared__ float s_m[AT_WARPS][ROWS], s_l[AT_WARPS][ROWS];
 
     const int tid = threadIdx.x, warp = __shfl_sync(0xffffffffu, tid >> 5, 0), lane = tid & 31, qg = lane >> 2, qt = lane & 3;
@@ -244,7 +256,8 @@ __global__ void __launch_bounds__(AT_THREADS, at_resident(D, G, RN)) kv4_attend_
     while (u < u1) {
         int first_tile;
         const int tiles = at_tiles_of(a, len, first_tile);
-        if (tiles == 0) {  // (an empty sequence has no units; its rows are the second kernel's)
+        if (u - base >= (long long)tiles * per) {  // the next sequence (an empty one has no units; its rows are the second kernel's)
+            base += (long long)tiles * per;
             len = __ldcg(a.c.lens + ++seq);
             continue;
         }
@@ -671,48 +684,28 @@ __global__ void __launch_bounds__(AT_THREADS, at_resident(D, G, RN)) kv4_attend_
         if constexpr (SOLO) __syncwarp();
         else __syncthreads();
         u += t1 - t0;
-        if (u - base >= (long long)tiles * per && u < u1) { base += (long long)tiles * per; len = __ldcg(a.c.lens + ++seq); }
     }
 }
 
-// Joins the parts of the items that were cut, and writes the rows of sequences without tokens.  One block per row of an item.
+// A row of an item that was cut, from its parts i0 .. i1: `warps` warps (this one being number w of them) take every warps-th part, several
+// under way at a time, a lane D/32 neighbouring channels.  top, sum, v: reference, sum of weights and weighted sums of these parts.
 template <int D, int ROWS>
-__global__ void __launch_bounds__(AT_THREADS) kv4_join_kernel(const AtArgs a) {
-    constexpr float LN2 = 0.69314718055994531f;
-    __shared__ float s_w[AT_WARPS], s_top[AT_WARPS], s_v[AT_WARPS][D];
-    const int seq = blockIdx.x, item = blockIdx.y, rt = item / a.c.heads, h = item - rt * a.c.heads, row = blockIdx.z, tid = threadIdx.x;
-    const int in = rt * ROWS + row, per = a.c.heads * a.row_tiles, tok = in / a.g, hd = in - tok * a.g;
-    const long long tokrow = (long long)seq * a.nq + tok;
-    unsigned short *out = a.out + tokrow * a.ldo + (long long)(h * a.g + hd) * D;
-    float *lse = a.lse ? a.lse + tokrow * (a.c.heads * a.g) + h * a.g + hd : nullptr;
-    const float *ml = a.ml;
-    griddep_wait();
-    griddep_launch_dependents();
-    if (in >= a.nq * a.g) return;
-    const int2 range = __ldcg(a.where + (long long)seq * per + item);
-    int first;
-    if (at_tiles(a, seq, first) == 0) {
-        for (int c = tid; c < D; c += AT_THREADS) at_store(out + c, 0.0f, a.bf16);
-        if (lse && tid == 0) *lse = -INFINITY;
-        return;
-    }
-    const int i0 = range.x, i1 = range.y;
-    if (i0 == i1) return;  // finished by its CTA
-    auto slot_of = [&](int i) { return 2 * i + (i == i0 ? 1 : 0); };
-    // Each warp takes every fourth part, a lane D/32 neighbouring channels of them, several parts under way at a time.
+__device__ __forceinline__ void at_parts(const AtArgs &a, int i0, int i1, int row, int w, int warps, float &top, float &sum, float (&v)[D / 32]) {
     constexpr int CPL = D / 32, AHEAD = 8;
-    const int warp = tid >> 5, lane = tid & 31, parts = i1 - i0 + 1;
-    float top = -INFINITY, sum = 0.0f, v[CPL];
+    const int lane = threadIdx.x & 31, parts = i1 - i0 + 1;
+    top = -INFINITY;
+    sum = 0.0f;
 #pragma unroll
     for (int k = 0; k < CPL; ++k) v[k] = 0.0f;
-    for (int i = warp; i < parts; i += AT_WARPS * AHEAD) {
+    for (int i = w; i < parts; i += warps * AHEAD) {
         float2 p[AHEAD];
         float x[AHEAD][CPL];
 #pragma unroll
         for (int k = 0; k < AHEAD; ++k) {
-            const int at = slot_of(i0 + min(i + k * AT_WARPS, parts - 1));
-            p[k] = __ldcg(reinterpret_cast<const float2 *>(ml + ((size_t)at * ROWS + row) * 2));
-            const float *src = a.part + ((size_t)at * ROWS + row) * D + lane * CPL;
+            const int part = i0 + min(i + k * warps, parts - 1);
+            const size_t at = ((size_t)2 * part + (part == i0 ? 1 : 0)) * ROWS + row;
+            p[k] = __ldcg(reinterpret_cast<const float2 *>(a.ml + at * 2));
+            const float *src = a.part + at * D + lane * CPL;
 #pragma unroll
             for (int c = 0; c < CPL; c += 2) {
                 const float2 y = __ldcg(reinterpret_cast<const float2 *>(src + c));
@@ -722,7 +715,7 @@ __global__ void __launch_bounds__(AT_THREADS) kv4_join_kernel(const AtArgs a) {
         }
         float t = top;
 #pragma unroll
-        for (int k = 0; k < AHEAD; ++k) t = i + k * AT_WARPS < parts ? fmaxf(t, p[k].x) : t;
+        for (int k = 0; k < AHEAD; ++k) t = i + k * warps < parts ? fmaxf(t, p[k].x) : t;
         const float ref = t == -INFINITY ? 0.0f : t, down = at_ex2(top - ref);
         top = t;
         sum *= down;
@@ -730,32 +723,67 @@ __global__ void __launch_bounds__(AT_THREADS) kv4_join_kernel(const AtArgs a) {
         for (int c = 0; c < CPL; ++c) v[c] *= down;
 #pragma unroll
         for (int k = 0; k < AHEAD; ++k)
-            if (i + k * AT_WARPS < parts) {
-                const float w = at_ex2(p[k].x - ref);
-                sum += w * p[k].y;
+            if (i + k * warps < parts) {
+                const float wt = at_ex2(p[k].x - ref);
+                sum += wt * p[k].y;
 #pragma unroll
-                for (int c = 0; c < CPL; ++c) v[c] += w > 0.0f || x[k][c] != x[k][c] ? w * x[k][c] : 0.0f;
+                for (int c = 0; c < CPL; ++c) v[c] += wt > 0.0f || x[k][c] != x[k][c] ? wt * x[k][c] : 0.0f;
             }
     }
-    if (lane == 0) s_top[warp] = top;
-    __syncthreads();
-    float mine = top;
+}
+
+// Joins the parts of the items that were cut, and writes the rows of sequences without tokens.  A block has a row of an item, its four
+// warps a quarter of the parts each; SOLO, where there are many items and few parts of any, it has an item and a warp every fourth row.
+template <int D, int ROWS, bool SOLO>
+__global__ void __launch_bounds__(AT_THREADS) kv4_join_kernel(const AtArgs a) {
+    constexpr float LN2 = 0.69314718055994531f;
+    constexpr int CPL = D / 32;
+    __shared__ float s_w[AT_WARPS], s_top[AT_WARPS], s_v[SOLO ? 1 : AT_WARPS][D];
+    const int seq = blockIdx.x, item = blockIdx.y, rt = item / a.c.heads, h = item - rt * a.c.heads, tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+    const int per = a.c.heads * a.row_tiles, rows = min(ROWS, a.nq * a.g - rt * ROWS), q_heads = a.c.heads * a.g;
+    griddep_wait();
+    griddep_launch_dependents();
+    const int2 range = __ldcg(a.where + (long long)seq * per + item);
+    int first;
+    const bool empty = at_tiles(a, seq, first) == 0;
+    const int i0 = range.x, i1 = range.y;
+    if (!empty && i0 == i1) return;  // finished by its worker
+    for (int row = SOLO ? warp : (int)blockIdx.z; row < rows; row += SOLO ? AT_WARPS : ROWS) {
+        const int in = rt * ROWS + row, tok = in / a.g, hd = in - tok * a.g;
+        const long long tokrow = (long long)seq * a.nq + tok;
+        unsigned short *out = a.out + tokrow * a.ldo + (long long)(h * a.g + hd) * D;
+        float *lse = a.lse ? a.lse + tokrow * q_heads + h * a.g + hd : nullptr;
+        if (empty) {
+            for (int c = SOLO ? lane : tid; c < D; c += SOLO ? 32 : AT_THREADS) at_store(out + c, 0.0f, a.bf16);
+            if (lse && (SOLO ? lane : tid) == 0) *lse = -INFINITY;
+            continue;
+        }
+        float top, sum, v[CPL];
+        at_parts<D, ROWS>(a, i0, i1, row, SOLO ? 0 : warp, SOLO ? 1 : AT_WARPS, top, sum, v);
+        if constexpr (SOLO) {
+            const bool any = sum > 0.0f || sum != sum;
+            const float by = any ? 1.0f / sum : 0.0f;
 #pragma unroll
-    for (int w = 0; w < AT_WARPS; ++w) top = fmaxf(top, s_top[w]);
-    mine = at_ex2(mine - (top == -INFINITY ? 0.0f : top));
-    sum *= mine;
+            for (int c = 0; c < CPL; ++c) at_store(out + lane * CPL + c, v[c] * by, a.bf16);
+            if (lse && lane == 0) *lse = any ? top * LN2 + logf(sum) : -INFINITY;
+        } else {
+            if (lane == 0) s_top[warp] = top;
+            __syncthreads();
+            float own = top;
 #pragma unroll
-    for (int c = 0; c < CPL; ++c) v[c] *= mine;
-    // the four warps in order
+            for (int w = 0; w < AT_WARPS; ++w) top = fmaxf(top, s_top[w]);
+            own = at_ex2(own - (top == -INFINITY ? 0.0f : top));
 #pragma unroll
-    for (int c = 0; c < CPL; ++c) s_v[warp][lane * CPL + c] = v[c];
-    if (lane == 0) s_w[warp] = sum;
-    __syncthreads();
-    sum = ((s_w[0] + s_w[1]) + s_w[2]) + s_w[3];
-    const bool any = sum > 0.0f || sum != sum;
-    const float by = any ? 1.0f / sum : 0.0f;
-    for (int c = tid; c < D; c += AT_THREADS) at_store(out + c, (((s_v[0][c] + s_v[1][c]) + s_v[2][c]) + s_v[3][c]) * by, a.bf16);
-    if (lse && tid == 0) *lse = any ? top * LN2 + logf(sum) : -INFINITY;
+            for (int c = 0; c < CPL; ++c) s_v[warp][lane * CPL + c] = v[c] * own;
+            if (lane == 0) s_w[warp] = sum * own;
+            __syncthreads();
+            sum = ((s_w[0] + s_w[1]) + s_w[2]) + s_w[3];  // the four warps in order
+            const bool any = sum > 0.0f || sum != sum;
+            const float by = any ? 1.0f / sum : 0.0f;
+            for (int c = tid; c < D; c += AT_THREADS) at_store(out + c, (((s_v[0][c] + s_v[1][c]) + s_v[2][c]) + s_v[3][c]) * by, a.bf16);
+            if (lse && tid == 0) *lse = any ? top * LN2 + logf(sum) : -INFINITY;
+        }
+    }
 }
 
 template <int D, int G, int RN, bool SOLO>
@@ -768,7 +796,7 @@ static cudaError_t at_launch_rn(const AtArgs &a, int grid, cudaStream_t st) {
     e = launch(kern, dim3(grid), dim3(AT_THREADS), SMEM, st, g_tune.pdl != 0, a);
     if (e != cudaSuccess) return e;
     const int rows = a.nq * a.g < 8 * RN ? a.nq * a.g : 8 * RN;
-    return launch(kv4_join_kernel<D, 8 * RN>, dim3(a.c.n_seqs, a.c.heads * a.row_tiles, rows), dim3(AT_THREADS), 0, st, g_tune.pdl != 0, a);
+    return launch(kv4_join_kernel<D, 8 * RN, SOLO>, dim3(a.c.n_seqs, a.c.heads * a.row_tiles, SOLO ? 1 : rows), dim3(AT_THREADS), 0, st, g_tune.pdl != 0, a);
 }
 
 // How the rows and items of a call are taken.  Eight rows at a time where a head has no more than that, else sixteen: the cache is then
@@ -777,7 +805,9 @@ static cudaError_t at_launch_rn(const AtArgs &a, int grid, cudaStream_t st) {
 struct AtPlan {
     int rn, items, resident;
     bool solo;
-    size_t parts() const { return (size_t)2 * (solo ? AT_WARPS : 1) * 2 * resident; }  // two waves, two parts per worker
+    int waves() const { return solo ? 1 : 2; }
+    size_t workers() const { return (size_t)(solo ? AT_WARPS : 1) * waves() * resident; }  // at most; two parts for each
+    size_t bytes(int n_seqs, int D) const { return workers() * 2 * 8 * rn * (D + 2) * sizeof(float) + (size_t)n_seqs * items * sizeof(int2); }
 };
 static AtPlan at_plan(int n_seqs, int nq, int q_heads, int heads, int D, int G) {
     AtPlan p;
@@ -805,7 +835,7 @@ extern "C" size_t scap_kv4_attend_workspace(int n_seqs, int nq, int q_heads, int
     size_t most = 0;
     for (int G = 1; G <= 4; G *= 2) {  // (the number of groups decides how many CTAs the device holds)
         const AtPlan p = at_plan(n_seqs, nq, q_heads, heads, head_dim, G);
-        const size_t bytes = p.parts() * 8 * p.rn * (head_dim + 2) * sizeof(float) + (size_t)n_seqs * p.items * sizeof(int2);
+        const size_t bytes = p.bytes(n_seqs, head_dim);
         most = bytes > most ? bytes : most;
     }
     return most;
@@ -837,15 +867,16 @@ extern "C" scap_status scap_kv4_attend(const scap_kv4 *cache, const void *q, int
     a.window = window;
     a.scale = (float)(scale * 1.4426950408889634);
     a.resident = p.resident;
+    a.waves = p.waves();
     // What the tables have room for bounds the work: no more CTAs than that takes.
     const long long cap = (long long)cache->table_stride * (cache->page_tokens / KV_TILE), seen = window > 0 ? ((long long)window + nq) / KV_TILE + 2 : cap;
     a.tile_cap = (int)(cap < (1ll << 30) ? cap : (1ll << 30));
     const long long items = (long long)cache->n_seqs * cache->heads * a.row_tiles, units = (cap < seen ? cap : seen) * items;
     const long long few = (units + AT_MIN_UNITS - 1) / AT_MIN_UNITS > items ? (units + AT_MIN_UNITS - 1) / AT_MIN_UNITS : items;
-    const int most = units >= (long long)AT_TWO_WAVES * a.resident ? 2 * a.resident : a.resident;
+    const int most = units >= (long long)AT_TWO_WAVES * a.resident ? a.waves * a.resident : a.resident;
     const int grid = few < most ? (int)few : most;
-    a.ml = a.part + p.parts() * 8 * p.rn * cache->head_dim;
-    a.where = reinterpret_cast<int2 *>(a.ml + p.parts() * 8 * p.rn * 2);
+    a.ml = a.part + 2 * p.workers() * 8 * p.rn * cache->head_dim;
+    a.where = reinterpret_cast<int2 *>(a.ml + 2 * p.workers() * 8 * p.rn * 2);
     a.bf16 = dt == SCAP_BF16;
     a.limit = g_tune.tc_spin ? (uint32_t)g_tune.tc_spin : TRIES;
     a.status = tc_status_ptr();
