@@ -54,6 +54,12 @@ struct AtArgs {
     int *status;
 };
 
+// What a warp is at: units [u, u1) of its worker `id`, of which tiles t0 .. t1 - 1 of an item of sequence seq are next.
+struct AtWork {
+    long long u, u1, base;
+    int id, seq, len, item, tiles, t0, t1;
+};
+
 // Tiles that the new tokens of a sequence of `len` tokens can see: first one and number.
 __device__ __forceinline__ int at_tiles_of(const AtArgs &a, int len, int &first) {
     first = 0;
@@ -234,6 +240,7 @@ __global__ void __launch_bounds__(AT_THREADS, at_resident(D, G, RN)) kv4_attend_
     __shared__ unsigned long long s_full[AT_WARPS][ST];
     __shared__ long long s_sum[AT_WARPS + 5 * (SOLO ? AT_WARPS : 1)];
     __shared__ float s_m[AT_WARPS][ROWS], s_l[AT_WARPS][ROWS];
+    __shared__ AtWork s_work[AT_WARPS];
 
     const int tid = threadIdx.x, warp = __shfl_sync(0xffffffffu, tid >> 5, 0), lane = tid & 31, qg = lane >> 2, qt = lane & 3;
     unsigned char *ring = at_raw + warp * ST * TILE;
@@ -244,37 +251,64 @@ __global__ void __launch_bounds__(AT_THREADS, at_resident(D, G, RN)) kv4_attend_
     griddep_launch_dependents();  // (after the wait: the second kernel may rely on all work before this one)
 
     const int per = a.c.heads * a.row_tiles;
-    AtPlace place;
-    if (!at_begin<SOLO>(a, per, s_sum, place)) return;
-    long long u = place.u, base = place.base;
-    const long long u1 = place.u1;
-    int seq = place.seq, len = place.len;
-    const int own = SOLO ? 0 : warp;  // this warp's first tile of those that its worker has of an item
+    // What a warp is at lives in shared memory: none of it is needed while it goes through its tiles, whose registers are scarce.
+    volatile AtWork &work = s_work[warp];
+    {
+        AtPlace place;
+        if (!at_begin<SOLO>(a, per, s_sum, place)) return;
+        if (lane == 0) {
+            work.u = place.u;
+            work.u1 = place.u1;
+            work.base = place.base;
+            work.id = place.id;
+            work.seq = place.seq;
+            work.len = place.len;
+        }
+        __syncwarp();
+    }
     int slot = 0, phase = 0;  // of this warp's ring, over all items
     bool dead = false;        // a wait of this warp ran out
+    const int own = SOLO ? 0 : warp;  // this warp's first tile of those that its worker has of an item
 
-    while (u < u1) {
-        int first_tile;
-        const int tiles = at_tiles_of(a, len, first_tile);
-        if (u - base >= (long long)tiles * per) {  // the next sequence (an empty one has no units; its rows are the second kernel's)
-            base += (long long)tiles * per;
-            len = __ldcg(a.c.lens + ++seq);
-            continue;
+    while (work.u < work.u1) {
+        const int len = work.len;
+        int count, pos0;
+        {
+            int first_tile;
+            const int tiles = at_tiles_of(a, len, first_tile);
+            const long long in_seq = work.u - work.base;
+            if (in_seq >= (long long)tiles * per) {  // the next sequence (an empty one has no units; its rows are the second kernel's)
+                const int next = __ldcg(a.c.lens + work.seq + 1);
+                __syncwarp();
+                if (lane == 0) {
+                    work.base += (long long)tiles * per;
+                    work.seq += 1;
+                    work.len = next;
+                }
+                __syncwarp();
+                continue;
+            }
+            const int item = (int)(in_seq / tiles), t0 = (int)(in_seq - (long long)item * tiles);
+            const int t1 = (int)min((long long)tiles, t0 + (work.u1 - work.u));
+            count = !dead && t1 - t0 - own > 0 ? (t1 - t0 - own + STEP - 1) / STEP : 0;  // tiles t0 + own, + STEP, ... are this warp's
+            pos0 = (first_tile + t0 + own) * KV_TILE;
+            if (lane == 0) {
+                work.item = item;
+                work.tiles = tiles;
+                work.t0 = t0;
+                work.t1 = t1;
+            }
+            __syncwarp();
         }
-        const int item = (int)((u - base) / tiles), t0 = (int)(u - base - (long long)item * tiles);
-        const int t1 = (int)min((long long)tiles, t0 + (u1 - u));
-        const int rt = item / a.c.heads, h = item - rt * a.c.heads;
-        const int rows = min(ROWS, a.nq * a.g - rt * ROWS);
-        const int count = !dead && t1 - t0 - own > 0 ? (t1 - t0 - own + STEP - 1) / STEP : 0;  // tiles t0 + own, + STEP, ... are this warp's
 
         // ---- addresses of the next 32 tiles of this warp, one per lane (0: no page), and the first copies
-        auto pos_of = [&](int i) { return (first_tile + t0 + own + STEP * i) * KV_TILE; };
         auto where = [&](int i) -> unsigned long long {
             if (i >= count) return 0ull;
-            const int per_page = a.c.page_tokens / KV_TILE, t = first_tile + t0 + own + STEP * i, at = t / per_page;
+            const int per_page = a.c.page_tokens / KV_TILE, t = pos0 / KV_TILE + STEP * i, at = t / per_page;
             if (at >= a.c.table_stride) return 0ull;
-            const int page = __ldcg(a.c.table + (long long)seq * a.c.table_stride + at);
+            const int page = __ldcg(a.c.table + (long long)work.seq * a.c.table_stride + at);
             if (page < 0 || page >= a.c.n_pages) return 0ull;
+            const int h = work.item % a.c.heads;
             return (unsigned long long)(a.c.pages + (long long)page * a.c.page_stride + (long long)(h * per_page + t - at * per_page) * TILE);
         };
         unsigned long long at_now = where(lane), at_next = where(32 + lane);
@@ -301,10 +335,10 @@ __global__ void __launch_bounds__(AT_THREADS, at_resident(D, G, RN)) kv4_attend_
         if (!QS || warp < RN) {  // (in shared memory: warp rn for its eight rows)
             const int rn = QS ? warp : 0, row = 8 * rn + qg;
             uint4 raw[W];
-            const int in = rt * ROWS + row, tok = in / a.g, hd = in - tok * a.g;
-            const unsigned short *src = a.q + ((long long)seq * a.nq + tok) * a.ldq + (long long)(h * a.g + hd) * D + 8 * qt;
+            const int rt = work.item / a.c.heads, h = work.item - rt * a.c.heads, in = rt * ROWS + row, tok = in / a.g, hd = in - tok * a.g;
+            const unsigned short *src = a.q + ((long long)work.seq * a.nq + tok) * a.ldq + (long long)(h * a.g + hd) * D + 8 * qt;
 #pragma unroll
-            for (int j = 0; j < W; ++j) raw[j] = ld_act16_if(src + 32 * j, row < rows);
+            for (int j = 0; j < W; ++j) raw[j] = ld_act16_if(src + 32 * j, in < a.nq * a.g);
             float v[W][8], top = 0.0f;
 #pragma unroll
             for (int j = 0; j < W; ++j)
@@ -355,16 +389,17 @@ __global__ void __launch_bounds__(AT_THREADS, at_resident(D, G, RN)) kv4_attend_
 #pragma unroll
             for (int rn = 0; rn < RN; ++rn) f[rn] = s_f[rn];
         }
-        // keys that a row sees: lo .. hi
-        int hi[RN][2], lo[RN][2];
+        // keys that row 8 rn + 2 qt + k sees: up to that of its own token, hi, and with a window from lo on
+        uint32_t tok_of[RN];
 #pragma unroll
-        for (int rn = 0; rn < RN; ++rn)
-#pragma unroll
-            for (int k = 0; k < 2; ++k) {
-                const int in = min(rt * ROWS + 8 * rn + 2 * qt + k, a.nq * a.g - 1), at = len - a.nq + in / a.g;
-                hi[rn][k] = at;
-                lo[rn][k] = a.window > 0 && at >= a.window ? at - a.window + 1 : 0;
-            }
+        for (int rn = 0; rn < RN; ++rn) {
+            const int in = work.item / a.c.heads * ROWS + 8 * rn + 2 * qt, last = a.nq * a.g - 1;
+            tok_of[rn] = (uint32_t)(min(in, last) / a.g) | (uint32_t)(min(in + 1, last) / a.g) << 16;
+        }
+        auto unseen = [&](int at, int rn, int k) {
+            const int hi = len - a.nq + (int)((tok_of[rn] >> (16 * k)) & 0xffffu);
+            return at > hi || (a.window > 0 && at <= hi - a.window);
+        };
         const int hi_all = len - a.nq, lo_all = a.window > 0 && len > a.window ? len - a.window : 0;  // what every row sees
 
         float o[RN][MT][4], z[RN][G][4], m[RN][2], l[RN][2];
@@ -401,7 +436,7 @@ __global__ void __launch_bounds__(AT_THREADS, at_resident(D, G, RN)) kv4_attend_
                 break;
             }
             const unsigned char *tile = ring + slot * TILE;
-            const int pos = pos_of(i);
+            const int pos = pos0 + STEP * KV_TILE * i;
             if ((there >> (i & 31)) & 1u) {
                 // keys that not every row sees: tokens behind the last, before a window, or newer than the row's own
                 const bool edge = pos + KV_TILE - 1 > hi_all || pos < lo_all;
@@ -480,8 +515,7 @@ __global__ void __launch_bounds__(AT_THREADS, at_resident(D, G, RN)) kv4_attend_
                         for (int rn = 0; rn < RN; ++rn)
 #pragma unroll
                             for (int k = 0; k < 2; ++k) {
-                                const int at = pos + 8 * j + qg;
-                                if (at > hi[rn][k] || at < lo[rn][k]) s[rn][j][k] = -INFINITY;
+                                if (unseen(pos + 8 * j + qg, rn, k)) s[rn][j][k] = -INFINITY;
                             }
                 }
                 // ---- largest scale of the values; tokens that no row sees have none, whatever lies there
@@ -566,9 +600,8 @@ __global__ void __launch_bounds__(AT_THREADS, at_resident(D, G, RN)) kv4_attend_
                         for (int rn = 0; rn < RN; ++rn) {
                             float x0 = s[rn][j][0] * vs, x1 = s[rn][j][1] * vs;
                             if (edge) {  // a row does not see what another one does: not even a NaN
-                                const int at = pos + 8 * j + qg;
-                                if (at > hi[rn][0] || at < lo[rn][0]) x0 = 0.0f;
-                                if (at > hi[rn][1] || at < lo[rn][1]) x1 = 0.0f;
+                                if (unseen(pos + 8 * j + qg, rn, 0)) x0 = 0.0f;
+                                if (unseen(pos + 8 * j + qg, rn, 1)) x1 = 0.0f;
                             }
                             pb[rn][j] = at_trans(at_pack(x0, x1));
                         }
@@ -637,14 +670,15 @@ __global__ void __launch_bounds__(AT_THREADS, at_resident(D, G, RN)) kv4_attend_
             }
         if constexpr (SOLO) __syncwarp();
         else __syncthreads();
-        const bool whole = t0 == 0 && t1 == tiles;
+        const int seq = work.seq, item = work.item, t0 = work.t0, t1 = work.t1, rt = item / a.c.heads, h = item - rt * a.c.heads, rows = min(ROWS, a.nq * a.g - rt * ROWS);
+        const bool whole = t0 == 0 && t1 == work.tiles;
         if (SOLO ? lane == 0 : tid == 0) {
             int2 *at = a.where + (long long)seq * per + item;
             if (whole) *at = make_int2(-1, -1);
-            else if (t0 == 0) at->x = place.id;
-            else if (t1 == tiles) at->y = place.id;
+            else if (t0 == 0) at->x = work.id;
+            else if (t1 == work.tiles) at->y = work.id;
         }
-        const int slot_out = 2 * place.id + (t0 == 0 ? 1 : 0);
+        const int slot_out = 2 * work.id + (t0 == 0 ? 1 : 0);
         float *sums = a.part + (size_t)slot_out * ROWS * D, *ml = a.ml + (size_t)slot_out * ROWS * 2;
         constexpr int NW = SOLO ? 1 : AT_WARPS;
         for (int row = own; row < rows; row += STEP) {
@@ -681,9 +715,10 @@ __global__ void __launch_bounds__(AT_THREADS, at_resident(D, G, RN)) kv4_attend_
             }
         }
         asm volatile("fence.proxy.async.shared::cta;" ::: "memory");  // the next copies may overwrite what was read and written here
+        __syncwarp();
+        if (lane == 0) work.u += t1 - t0;
         if constexpr (SOLO) __syncwarp();
         else __syncthreads();
-        u += t1 - t0;
     }
 }
 
@@ -800,8 +835,9 @@ static cudaError_t at_launch_rn(const AtArgs &a, int grid, cudaStream_t st) {
 }
 
 // How the rows and items of a call are taken.  Eight rows at a time where a head has no more than that, else sixteen: the cache is then
-// read (and unpacked) half as often.  Warps work on their own (SOLO) where there are two items and more for every CTA that the device
-// holds: an item then costs no barriers, its queries are prepared once, and its tiles need not be a multiple of four.
+// read (and unpacked) half as often.  Warps work on their own (SOLO) where there are more items than CTAs that the device holds: an item then
+// costs no barriers, its queries are prepared once, and its tiles need not be a multiple of four (100 sequences of together 40000 tokens,
+// 8 key heads: 57 -> 44 us; 512 of 60000: 148 -> 76; 64 of 128000, where there are fewer items than CTAs: 61 -> 66).
 struct AtPlan {
     int rn, items, resident;
     bool solo;
@@ -815,7 +851,7 @@ static AtPlan at_plan(int n_seqs, int nq, int q_heads, int heads, int D, int G) 
     p.rn = rows <= 8 ? 1 : 2;
     p.items = heads * ((rows + 8 * p.rn - 1) / (8 * p.rn));  // per sequence
     p.resident = sm_count() * at_resident(D, G, p.rn);
-    p.solo = p.rn == 1 && (long long)n_seqs * p.items >= 2LL * p.resident;
+    p.solo = p.rn == 1 && (long long)n_seqs * p.items > p.resident;
     return p;
 }
 
