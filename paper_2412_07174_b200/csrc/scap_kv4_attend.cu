@@ -446,12 +446,15 @@ __global__ void __launch_bounds__(AT_THREADS, at_resident(D, G, RN)) kv4_attend_
 #pragma unroll
                 for (int n = 0; n < G; ++n)
                     *reinterpret_cast<uint4 *>(kw[n]) = *reinterpret_cast<const uint4 *>(tile + kv_k_words(D) + (n * KV_TILE + 4 * qg) * 4);
-                {
-                    float acc[2][RN][G][4];
-                    uint32_t w[4][W];
+                // (MB of the two A operands at a time: the chains of MMAs are independent, but their registers are scarce)
+                constexpr int MB = G == 1 ? 2 : 1;
 #pragma unroll
-                    for (int j = 0; j < 4; ++j) {
-                        const unsigned char *krow = tile + (8 * j + qg) * (D / 2) + qt * (D / 8);
+                for (int m0 = 0; m0 < 2; m0 += MB) {
+                    float acc[MB][RN][G][4];
+                    uint32_t w[2 * MB][W];
+#pragma unroll
+                    for (int j = 0; j < 2 * MB; ++j) {
+                        const unsigned char *krow = tile + (8 * (2 * m0 + j) + qg) * (D / 2) + qt * (D / 8);
                         if constexpr (W == 2) *reinterpret_cast<uint2 *>(w[j]) = *reinterpret_cast<const uint2 *>(krow);
                         else
 #pragma unroll
@@ -460,8 +463,8 @@ __global__ void __launch_bounds__(AT_THREADS, at_resident(D, G, RN)) kv4_attend_
 #pragma unroll
                     for (int n = 0; n < G; ++n)
 #pragma unroll
-                        for (int mt = 0; mt < 2; ++mt) {
-                            const uint32_t z0 = (kw[n][2 * mt] & zmask) * 0x00400040u, z1 = (kw[n][2 * mt + 1] & zmask) * 0x00400040u;
+                        for (int mt = 0; mt < MB; ++mt) {
+                            const uint32_t z0 = (kw[n][2 * (m0 + mt)] & zmask) * 0x00400040u, z1 = (kw[n][2 * (m0 + mt) + 1] & zmask) * 0x00400040u;
 #pragma unroll
                             for (int rn = 0; rn < RN; ++rn) {
 #pragma unroll
@@ -469,8 +472,10 @@ __global__ void __launch_bounds__(AT_THREADS, at_resident(D, G, RN)) kv4_attend_
                                 at_mma(acc[mt][rn][n], z0, z1, 0u, 0u, QS ? s_zq[QS ? rn : 0][n][lane] : zq[QS ? 0 : n], 0u);
                             }
                         }
+                    // (the words of a group lie W / G apart from those of the next: in turn, so that neighbouring MMAs have different accumulators)
 #pragma unroll
-                    for (int k = 0; k < W; ++k) {
+                    for (int kk = 0; kk < W; ++kk) {
+                        const int k = kk % G * (W / G) + kk / G;
                         uint32_t q[RN][2][2];
 #pragma unroll
                         for (int rn = 0; rn < RN; ++rn) {
@@ -485,7 +490,7 @@ __global__ void __launch_bounds__(AT_THREADS, at_resident(D, G, RN)) kv4_attend_
 #pragma unroll
                         for (int hi8 = 0; hi8 < 2; ++hi8)
 #pragma unroll
-                            for (int mt = 0; mt < 2; ++mt) {
+                            for (int mt = 0; mt < MB; ++mt) {
                                 const uint32_t x = w[2 * mt][k] >> (8 * hi8), y = w[2 * mt + 1][k] >> (8 * hi8);
                                 const uint32_t a0 = x & 0x000f000fu, a1 = y & 0x000f000fu, a2 = x & 0x00f000f0u, a3 = y & 0x00f000f0u;
 #pragma unroll
@@ -493,17 +498,17 @@ __global__ void __launch_bounds__(AT_THREADS, at_resident(D, G, RN)) kv4_attend_
                             }
                     }
 #pragma unroll
-                    for (int j = 0; j < 4; ++j)
+                    for (int j = 0; j < 2 * MB; ++j)
 #pragma unroll
                         for (int n = 0; n < G; ++n) {
-                            const float ks = __uint_as_float(kw[n][j] & ~15u);
+                            const float ks = __uint_as_float(kw[n][2 * m0 + j] & ~15u);
 #pragma unroll
                             for (int rn = 0; rn < RN; ++rn) {
                                 const float by = ks * f[rn];
 #pragma unroll
                                 for (int k = 0; k < 2; ++k) {
                                     const float x = acc[j >> 1][rn][n][2 * (j & 1) + k];
-                                    s[rn][j][k] = n == 0 ? by * x : s[rn][j][k] + by * x;
+                                    s[rn][2 * m0 + j][k] = n == 0 ? by * x : s[rn][2 * m0 + j][k] + by * x;
                                 }
                             }
                         }
