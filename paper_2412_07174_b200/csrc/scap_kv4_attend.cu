@@ -513,36 +513,38 @@ __global__ void __launch_bounds__(AT_THREADS, at_resident(D, G, RN)) kv4_attend_
                             }
                         }
                 }
+                uint32_t vw[G][4];
+#pragma unroll
+                for (int n = 0; n < G; ++n) *reinterpret_cast<uint4 *>(vw[n]) = *reinterpret_cast<const uint4 *>(tile + kv_v_words(D, G) + (n * KV_TILE + 4 * qg) * 4);
                 if (edge) {
 #pragma unroll
-                    for (int j = 0; j < 4; ++j)
+                    for (int j = 0; j < 4; ++j) {
+                        const int at = pos + 8 * j + qg;
 #pragma unroll
                         for (int rn = 0; rn < RN; ++rn)
 #pragma unroll
-                            for (int k = 0; k < 2; ++k) {
-                                if (unseen(pos + 8 * j + qg, rn, k)) s[rn][j][k] = -INFINITY;
-                            }
-                }
-                // ---- largest scale of the values; tokens that no row sees have none, whatever lies there
-                uint32_t vw[G][4], big = 0;
+                            for (int k = 0; k < 2; ++k)
+                                if (unseen(at, rn, k)) s[rn][j][k] = -INFINITY;
+                        if (at >= len || at <= lo_all - a.nq) {  // tokens that no row sees have no scale, whatever lies there
 #pragma unroll
-                for (int n = 0; n < G; ++n) {
-                    *reinterpret_cast<uint4 *>(vw[n]) = *reinterpret_cast<const uint4 *>(tile + kv_v_words(D, G) + (n * KV_TILE + 4 * qg) * 4);
-                    if (edge) {
-#pragma unroll
-                        for (int j = 0; j < 4; ++j)
-                            if (pos + 8 * j + qg >= len || pos + 8 * j + qg <= lo_all - a.nq) vw[n][j] = 0;
+                            for (int n = 0; n < G; ++n) vw[n][j] = 0;
+                        }
                     }
-                    big = max(max(big, max(vw[n][0], vw[n][1])), max(vw[n][2], vw[n][3]));
                 }
-                if (__any_sync(0xffffffffu, big >= 0x7f800000u)) {  // a NaN has no say
+                // ---- largest scale of the values
+                uint32_t big = 0;
+#pragma unroll
+                for (int n = 0; n < G; ++n) big = max(max(big, max(vw[n][0], vw[n][1])), max(vw[n][2], vw[n][3]));
+                uint32_t most = __reduce_max_sync(0xffffffffu, big);
+                if (most >= 0x7f800000u) {  // a NaN has no say
                     big = 0;
 #pragma unroll
                     for (int n = 0; n < G; ++n)
 #pragma unroll
                         for (int j = 0; j < 4; ++j) big = max(big, vw[n][j] < 0x7f800000u ? vw[n][j] : 0u);
+                    most = __reduce_max_sync(0xffffffffu, big);
                 }
-                const int e = (int)(__reduce_max_sync(0xffffffffu, big) >> 23);
+                const int e = (int)(most >> 23);
                 // ---- reference of the weights: the largest score, but left as it is while weights stay below 2^8, so that the
                 // accumulators are rarely rescaled
                 float t[RN][2];
@@ -595,22 +597,32 @@ __global__ void __launch_bounds__(AT_THREADS, at_resident(D, G, RN)) kv4_attend_
                     }
                 // ---- weighted values: p vs as B operands (a block of eight tokens x eight rows is transposed in registers)
                 const float up = at_pow2(AT_UP - top_e), up16 = up * 0.0625f;
+                uint32_t pb[G][RN][4];
 #pragma unroll
-                for (int n = 0; n < G; ++n) {
-                    uint32_t pb[RN][4];
+                for (int n = 0; n < G; ++n)
 #pragma unroll
                     for (int j = 0; j < 4; ++j) {
                         const float vs = __uint_as_float(vw[n][j] & ~15u) * (j & 1 ? up16 : up);
 #pragma unroll
-                        for (int rn = 0; rn < RN; ++rn) {
-                            float x0 = s[rn][j][0] * vs, x1 = s[rn][j][1] * vs;
-                            if (edge) {  // a row does not see what another one does: not even a NaN
-                                if (unseen(pos + 8 * j + qg, rn, 0)) x0 = 0.0f;
-                                if (unseen(pos + 8 * j + qg, rn, 1)) x1 = 0.0f;
-                            }
-                            pb[rn][j] = at_trans(at_pack(x0, x1));
-                        }
+                        for (int rn = 0; rn < RN; ++rn) pb[n][rn][j] = at_pack(s[rn][j][0] * vs, s[rn][j][1] * vs);
                     }
+                if (edge) {  // a row does not see what another one does: not even a NaN
+#pragma unroll
+                    for (int j = 0; j < 4; ++j)
+#pragma unroll
+                        for (int rn = 0; rn < RN; ++rn) {
+                            const int at = pos + 8 * j + qg;
+                            const uint32_t seen = (unseen(at, rn, 0) ? 0u : 0xffffu) | (unseen(at, rn, 1) ? 0u : 0xffff0000u);
+#pragma unroll
+                            for (int n = 0; n < G; ++n) pb[n][rn][j] &= seen;
+                        }
+                }
+#pragma unroll
+                for (int n = 0; n < G; ++n) {
+#pragma unroll
+                    for (int rn = 0; rn < RN; ++rn)
+#pragma unroll
+                        for (int j = 0; j < 4; ++j) pb[n][rn][j] = at_trans(pb[n][rn][j]);
                     uint32_t w0[4], w1[4];  // tokens 8 j + 2 qt and the next
                     *reinterpret_cast<uint4 *>(w0) = *reinterpret_cast<const uint4 *>(tile + kv_v_words(D, G) + (n * KV_TILE + 8 * qt) * 4);
                     *reinterpret_cast<uint4 *>(w1) = *reinterpret_cast<const uint4 *>(tile + kv_v_words(D, G) + (n * KV_TILE + 8 * qt + 4) * 4);
@@ -618,7 +630,7 @@ __global__ void __launch_bounds__(AT_THREADS, at_resident(D, G, RN)) kv4_attend_
                     for (int ks = 0; ks < 2; ++ks) {
                         const uint32_t z0 = __byte_perm(w0[2 * ks], w1[2 * ks], 0x5410) & 0x000f000fu, z1 = (__byte_perm(w0[2 * ks + 1], w1[2 * ks + 1], 0x5410) & 0x000f000fu) << 4;
 #pragma unroll
-                        for (int rn = 0; rn < RN; ++rn) at_mma(z[rn][n], z0, z0, z1, z1, pb[rn][2 * ks], pb[rn][2 * ks + 1]);
+                        for (int rn = 0; rn < RN; ++rn) at_mma(z[rn][n], z0, z0, z1, z1, pb[n][rn][2 * ks], pb[n][rn][2 * ks + 1]);
                     }
 #pragma unroll
                     for (int b4 = n * W / G; b4 < (n + 1) * W / G; ++b4) {
@@ -631,7 +643,7 @@ __global__ void __launch_bounds__(AT_THREADS, at_resident(D, G, RN)) kv4_attend_
                                 const uint32_t x = w[2 * half] >> (8 * ks), y = w[2 * half + 1] >> (8 * ks);
                                 const uint32_t a0 = x & 0x000f000fu, a1 = y & 0x000f000fu, a2 = x & 0x00f000f0u, a3 = y & 0x00f000f0u;
 #pragma unroll
-                                for (int rn = 0; rn < RN; ++rn) at_mma(o[rn][2 * b4 + half], a0, a1, a2, a3, pb[rn][2 * ks], pb[rn][2 * ks + 1]);
+                                for (int rn = 0; rn < RN; ++rn) at_mma(o[rn][2 * b4 + half], a0, a1, a2, a3, pb[n][rn][2 * ks], pb[n][rn][2 * ks + 1]);
                             }
                     }
                 }
