@@ -447,7 +447,7 @@ __global__ void __launch_bounds__(AT_THREADS, at_resident(D, G, RN)) kv4_attend_
                 for (int n = 0; n < G; ++n)
                     *reinterpret_cast<uint4 *>(kw[n]) = *reinterpret_cast<const uint4 *>(tile + kv_k_words(D) + (n * KV_TILE + 4 * qg) * 4);
                 // (MB of the two A operands at a time: the chains of MMAs are independent, but their registers are scarce)
-                constexpr int MB = G == 1 ? 2 : 1;
+                constexpr int MB = G <= 2 ? 2 : 1;
 #pragma unroll
                 for (int m0 = 0; m0 < 2; m0 += MB) {
                     float acc[MB][RN][G][4];
