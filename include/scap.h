@@ -24,7 +24,8 @@
  *     synchronisation, so they may be recorded into a CUDA graph.  Two calls that share a
  *     workspace must be ordered on one stream.
  *   - Data pointers must be 16-byte aligned and N (and F, D for the FFN calls) a multiple of 8,
- *     else SCAP_ERR_ALIGN.  B outside 1..16, K < 1, K > 1048576 or N < 1 give SCAP_ERR_SHAPE.  A
+ *     else SCAP_ERR_ALIGN.  B outside 1..16 (scap_fc_act and the calls on a cache have limits of their own), K < 1, K > 1048576 or N < 1
+ *     give SCAP_ERR_SHAPE.  A
  *     NULL required pointer gives SCAP_ERR_INVALID_ARG, a workspace smaller than the matching
  *     *_workspace() query SCAP_ERR_WORKSPACE, an unknown dtype SCAP_ERR_DTYPE, a failed launch
  *     SCAP_ERR_CUDA, a device that is not compute capability 10.x SCAP_ERR_UNSUPPORTED_ARCH.
@@ -37,7 +38,7 @@
  *     is the exception: it is a constant of the layer and must be complete in device memory when the call is
  *     ISSUED (not written by work still pending on the stream), because kernels that know their first weight rows
  *     without looking at the activations (the batch 5..16 kernel, also on the rows of a grouped call; the tensor-core
- *     kernel of 8- and 4-bit weights at any batch; the dense calls, a sparse call with "head_rows" set) request them
+ *     kernel of 8- and 4-bit weights at any batch; the dense calls, scap_fc_act, a sparse call with "head_rows" set) request them
  *     before that wait, so that the memory system does not idle between consecutive calls.  Consecutive calls overlap where they can: a kernel may
  *     become resident and set up its shared memory while its predecessor drains (programmatic dependent launch,
  *     "pdl" below).
@@ -102,7 +103,7 @@ int scap_version(void);
  *              kernel wherever it can run.
  *              Grouped calls: 0 = always one gather per group (better when the rows of a group keep the very same
  *              channels, and less than about a fifth of them); else see scap_sparse_fc_grouped
- *   "tc_spin"  tcgen05 kernels: how often a wait on one of its shared-memory barriers polls before it gives up
+ *   "tc_spin"  tcgen05 kernels and scap_kv4_attend: how often a wait on one of its shared-memory barriers polls before it gives up
  *              (0 = the built-in limits, the default: about a million polls, tens of milliseconds, or, where the wait
  *              sleeps, 65536 tries of 4 us).  A limit of 1 makes the waits of
  *              the next call run out at once, which is how the error path of scap_device_status() is exercised
@@ -409,7 +410,9 @@ size_t scap_kv4_page_bytes(int page_tokens, int heads, int head_dim, int group);
  * apart (a multiple of 8: slices of a fused QKV result will do).  Sequence b has the rows row_start[b] .. row_start[b+1] - 1
  * (row_start[n_seqs + 1], ascending; rows before the first and behind the last are not touched), which become its last tokens: the
  * positions lens[b] - n .. lens[b] - 1.  row_start NULL: row b is the last token of sequence b, for the first `rows` sequences.
- * scap_kv4_read is the way back: the same rows, their values as the cache holds them (rounded to dt).  0 <= rows <= SCAP_MAX_ROWS. */
+ * scap_kv4_read is the way back: the same rows, their values as the cache holds them (rounded to dt).  0 <= rows <= SCAP_MAX_ROWS.
+ * No page may appear twice among the places that a call writes (full pages may be shared, see scap_kv4_fork; a page that tokens are
+ * still added to may not). */
 scap_status scap_kv4_append(const scap_kv4 *cache, const void *k, int64_t ldk, const void *v, int64_t ldv, const int *row_start, int rows,
                             scap_dtype dt, scap_stream_t stream);
 scap_status scap_kv4_read(const scap_kv4 *cache, void *k, int64_t ldk, void *v, int64_t ldv, const int *row_start, int rows, scap_dtype dt,
@@ -418,12 +421,14 @@ scap_status scap_kv4_read(const scap_kv4 *cache, void *k, int64_t ldk, void *v, 
 /* Attention over the cache: for each sequence the last nq (1..16) of its lens[b] tokens are queries,
  *   out[b,i,h] = sum_t p_t v_t / sum_t p_t,  p_t = exp(scale q[b,i,h] . k_t)  over the tokens t <= lens[b] - nq + i, and with window > 0
  *   only the last `window` of these.
- * q[n_seqs, nq, q_heads, head_dim] (dtype dt), tokens ldq elements apart (a multiple of 8); out likewise with ldo, rounded to dt;
+ * q[n_seqs, nq, q_heads, head_dim] (dtype dt), tokens ldq elements apart (a multiple of 8); out likewise with ldo, rounded to dt, and
+ * may not overlap q;
  * q_heads a multiple of cache->heads up to 1024, query head h reads key head h / (q_heads / heads).  lse[n_seqs, nq, q_heads] fp32 or
  * NULL: log of the sum of the exp(...), for joining with attention over tokens that are not in the cache.  A row that sees nothing (an
  * empty sequence, or nq > lens[b]) gives 0 and -inf.  A NaN or an infinity in a query, or in a key or value that it sees, makes
  * its row non-finite, no other one.  Scores, sums and accumulators are fp32; a weight times the scale of its value is rounded to
- * fp16 once, relative to the largest scale seen so far, so values below 2^-20 of the largest ones seen lose precision.
+ * fp16 once, relative to the largest scale seen so far, so values below 2^-20 of the largest ones seen lose precision; queries are exact
+ * down to 2^-22 of the largest of the eight rows that are taken together.
  * Bitwise reproducible on one device.  Workspace: scap_kv4_attend_workspace() bytes.                                             */
 size_t scap_kv4_attend_workspace(int n_seqs, int nq, int q_heads, int heads, int head_dim);
 scap_status scap_kv4_attend(const scap_kv4 *cache, const void *q, int64_t ldq, void *out, int64_t ldo, float *lse, int nq, int q_heads,

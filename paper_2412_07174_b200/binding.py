@@ -181,7 +181,10 @@ def _invoke_real(name: str, x: float, at: int, *args) -> None:
     """The same for an entry point that has one double, `x`, before its argument number `at`."""
     if _lib is None:
         lib()
-    code = _call_real(_entry[name], x, *args) if _call is not _ctypes_call else _call(_entry[name], *args[:at], C.c_double(x), *args[at:])
+    if _call_real is not None and _call is not _ctypes_call:
+        code = _call_real(_entry[name], x, *args)
+    else:
+        code = _ctypes_call(getattr(_lib, name), *args[:at], C.c_double(x), *args[at:])
     if code != 0:
         raise ScapError(code, name)
 

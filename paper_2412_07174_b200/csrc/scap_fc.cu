@@ -298,7 +298,7 @@ const char *scap_status_string(scap_status st) {
     return "SCAP_ERR_UNKNOWN";
 }
 
-int scap_version(void) { return 1002; }
+int scap_version(void) { return 1003; }
 
 scap_status scap_device_status(void) {
     const int v = tc_take_status();

@@ -6,18 +6,23 @@
 //   scores  s_t = ks_t (sum_c q_c code_tc - zero_t sum_c q_c), the second sum by one more MMA with the zero points as codes
 //   output  o_c = sum_t (p_t vs_t) code_tc - sum_t (p_t vs_t) zero_t, likewise.
 // p vs is rounded to fp16 (11 bits) once and used in both sums, so the rounding acts on the value v, not on its code part; the queries
-// are scaled by a power of two per row and are exact.  Scores, maxima, sums and accumulators are fp32.
+// are scaled by one power of two per eight rows and are exact.  Scores, maxima, sums and accumulators are fp32.
 // (With the rows as the M rows of the MMA a head with eight or fewer of them pays for sixteen: twice the MMAs, accumulators and
-// exponentials; 131001 tokens, 8 key heads, 8 rows: 56 us.)
+// exponentials; 131001 tokens, 8 key heads, 8 rows: 57 us against 45 at that time.)
 //
-// What bounds it: the bytes of the cache, D/2 + 4 groups per token, head and side - if the instructions keep up: per tile of 32 tokens a
-// warp issues 36 MMAs (D = 128, RN = 1), 160 mask and shift instructions and about 100 for the softmax.
+// What bounds it: the instructions.  The bytes of the cache are D/2 + 4 groups per token, head and side; per tile of 32 tokens (D = 128,
+// RN = 1, one group) a warp issues 36 MMAs, 160 mask and shift instructions - five for eight codes, and the pipe that runs them takes two cycles
+// each - and about 150 others.  48 sequences of together 196608 tokens, 8 key heads, groups of 64: 67 us at 228 MB = 3.4 TB/s, issue slots
+// 56 % busy, the mask pipe 47 %, tensor pipe 22 %, DRAM 43 %; 131001 tokens of one sequence, groups of 128: 38 us at 143 MB = 3.7 TB/s.  With
+// the copies alone, no arithmetic, these took 48 and 33 us: 4 to 6 us until the first tiles of all warps have come, then 5.7 TB/s.
 //
 // Work is cut into equal parts, whatever the lengths: a unit is one tile of 32 tokens of one (sequence, 8 RN rows, head), all units are
-// numbered, and CTA i of C takes the units [U i / C, U (i + 1) / C).  Inside a CTA the tiles of an item go round the four warps, each
-// of which has its own ring of tiles, filled by cp.async.bulk (one copy per tile, 4.3 KB at D = 128), its own running maximum and sum, and no barrier with
-// the others until the item ends.  An item that lies in one CTA is finished there; the parts of one that is cut go to the
-// workspace, and a second kernel joins them in order.  No atomics: the same bits each time.
+// numbered, and worker i of w takes the units [U i / w, U (i + 1) / w).  A worker is a CTA: the tiles of an item go round its four warps,
+// each of which has its own ring of tiles, filled by cp.async.bulk (one copy per tile, 4.3 KB at D = 128), its own running maximum and sum, and no
+// barrier with the others until the item ends.  Or (SOLO), with many items, a warp.  An item that lies in one worker is finished there; the
+// parts of one that is cut go to the workspace, and a second kernel joins them in order.  No atomics: the same bits each time.
+// (Tried and slower: the first tiles of the next item asked for while the last ones of the present one are worked on: 77 -> 85 us, the loop
+// over tiles pays for it; a fifth CTA per SM: the same; the shifts as multiplications on the idle pipe: 77 -> 82.)
 //
 // Every wait is bounded; one that runs out sets the status word and leaves its tile out.
 #include "scap_kv4.cuh"

@@ -190,6 +190,17 @@ def test_sizes_of_queries_and_values():
 
 
 @pytest.mark.gpu
+def test_rows_of_different_size():
+    """Eight rows share a power of two: those 2^-14 as large as the largest keep all of their bits."""
+    lens = [150, 33]
+    c = filled(lens, 2, 128, 64, seed=17)
+    q = queries(2, 2, 8, 128, HF)
+    q = (q * torch.tensor([1.0, 2.0 ** -14, 4.0, 2.0 ** -7, 2.0 ** -3, 0.0, 1.0, 2.0 ** -14], device="cuda")[:, None].half()).to(HF)
+    out, lse = attend(c, q, 128 ** -0.5)
+    check(c, q, out, lse, lens, 2, 128 ** -0.5, 0)
+
+
+@pytest.mark.gpu
 def test_non_finite_values_stay_with_the_rows_that_see_them():
     lens, D, nq = [100, 100], 64, 4
     c = Cache(lens, heads=2, D=D, group=64)
