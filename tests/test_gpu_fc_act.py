@@ -99,6 +99,26 @@ def test_many_tiles(M, K, N):
 
 
 @pytest.mark.gpu
+@pytest.mark.parametrize("M,K,N", [(1 << 20, 8, 8), (300001, 72, 16), (1, 1 << 20, 8), (20, 300001, 16), (3, 64, 1 << 18), (130, 24, 65544)])
+def test_long_sides(M, K, N):
+    run_case(M, K, N, BF, BF, act="silu", seed=7)
+    run_case(M, K, N, HF, F32, bias=False, res=True, seed=8)
+
+
+@pytest.mark.gpu
+def test_slices_of_wider_matrices():
+    import paper_2412_07174_b200 as scap
+    wide = torch.randn(70, 400, device="cuda").to(BF)
+    W = (0.05 * torch.randn(128, 64, device="cuda")).to(BF)
+    ws = torch.empty(16, dtype=torch.uint8, device="cuda")
+    out = torch.zeros(70, 400, device="cuda")
+    scap.scap_fc_act(wide[:, 8:136], W, None, out[:, 104:168], ws)
+    want = wide[:, 8:136].double() @ W.double()
+    assert torch.allclose(out[:, 104:168].double(), want, atol=1e-4)
+    assert bool((out[:, :104] == 0).all()) and bool((out[:, 168:] == 0).all())
+
+
+@pytest.mark.gpu
 @pytest.mark.parametrize("M,K,N,ldx,ldy", [(5, 100, 64, 136, 64), (40, 100, 64, 101, 80), (300, 511, 520, 511, 521), (130, 256, 264, 300, 1000)])
 def test_strides(M, K, N, ldx, ldy):
     run_case(M, K, N, BF, BF, act="relu", res=True, ldx=ldx, ldy=ldy, seed=ldx)

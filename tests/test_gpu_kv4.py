@@ -75,6 +75,22 @@ def test_random_lengths_and_rows_left_alone():
 
 
 @pytest.mark.gpu
+@pytest.mark.parametrize("B,page", [(33, 4096), (1000, 32), (4096, 32)])
+def test_many_sequences(B, page):
+    rng = np.random.default_rng(B)
+    new = rng.integers(0, 4, B)
+    new[rng.random(B) < 0.5] = 0
+    new[:3], new[-3:] = 0, 0     # empty ones at both ends
+    past = rng.integers(0, 30, B)
+    c = Cache((past + new).tolist(), page=page, heads=1, D=64, group=64, seed=B, room=40)
+    n = int(new.sum())
+    k, v = tokens(n, 1, 64, BF, 1), tokens(n, 1, 64, BF, 2)
+    c.scap.scap_kv4_append(c.cache, k, v, starts(new))
+    ko, vo = read_back(c, n, new)
+    assert same(ko, stored64(k, 64)) and same(vo, stored64(v, 64)) and c.guards_intact()
+
+
+@pytest.mark.gpu
 @pytest.mark.parametrize("dt", [BF, HF])
 def test_values_at_the_borders(dt):
     D, group = 128, 64

@@ -276,6 +276,41 @@ def test_slices_graph_and_stream():
 
 
 @pytest.mark.gpu
+@pytest.mark.parametrize("B,heads,tokens,nq,g,window", [(1, 32, 215000, 1, 2, 0), (2, 16, 180000, 2, 8, 0), (110, 8, 4200, 1, 2, 0), (100, 8, 6000, 2, 1, 4000)])
+def test_more_than_32_tiles_per_warp(B, heads, tokens, nq, g, window):
+    """The addresses of a warp's tiles come 32 at a time.  Some heads of some sequences against 64 bits."""
+    import paper_2412_07174_b200 as scap
+    D, page, dev = 64, 128, "cuda"
+    rng = np.random.default_rng(tokens)
+    lens = [tokens - int(rng.integers(0, 200)) for _ in range(B)]
+    width = -(-tokens // page)
+    table = torch.tensor(rng.permutation(B * width).reshape(B, width), dtype=torch.int32, device=dev)
+    n = torch.tensor(lens, dtype=torch.int32, device=dev)
+    pool = torch.zeros(B * width, scap.scap_kv4_page_bytes(page, heads, D, 64), dtype=torch.uint8, device=dev)
+    cache = scap.ScapKv4(pool, page, heads, D, 64, table, n)
+    gen = torch.Generator(device=dev).manual_seed(3)
+    k = torch.empty(sum(lens), heads, D, dtype=BF, device=dev).normal_(generator=gen)
+    v = torch.empty(sum(lens), heads, D, dtype=BF, device=dev).normal_(generator=gen)
+    at = starts(lens)
+    scap.scap_kv4_append(cache, k, v, at)
+    q = queries(B, nq, g * heads, D, BF)
+    out, lse = torch.empty_like(q), torch.empty(B, nq, g * heads, device=dev)
+    ws = torch.empty(scap.scap_kv4_attend_workspace(B, nq, g * heads, heads, D), dtype=torch.uint8, device=dev)
+    scap.scap_kv4_attend(cache, q, out, 0.125, ws, window=window, lse=lse)
+    torch.cuda.synchronize()
+    scap.scap_device_status()
+
+    class One:  # one head of one sequence, as a cache of its own
+        pass
+    for b, h in {(0, 0), (B - 1, heads - 1), (B // 2, 3)}:
+        c = One()
+        c.heads, c.group = 1, 64
+        rows = slice(int(at[b]), int(at[b + 1]))
+        c.kv = (k[rows, h:h + 1], v[rows, h:h + 1])
+        check(c, q[b:b + 1, :, h * g:(h + 1) * g], out[b:b + 1, :, h * g:(h + 1) * g], lse[b:b + 1, :, h * g:(h + 1) * g], lens[b:b + 1], nq, 0.125, window)
+
+
+@pytest.mark.gpu
 def test_offsets_beyond_32_bits():
     import paper_2412_07174_b200 as scap
     n, stride = 40, 1 << 27   # 5.4 GB
