@@ -26,6 +26,7 @@
 #include <math.h>
 #include <string.h>
 
+#include <atomic>
 #include <type_traits>
 
 #include "scap_tc.cuh"
@@ -150,6 +151,52 @@ __device__ __noinline__ float4 fa_act4(float4 v, int act) {
     return make_float4(u[0], u[1], u[2], u[3]);
 }
 
+__device__ __forceinline__ float fa_exp2(float x) {
+    float r;
+    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(x));
+    return r;
+}
+__device__ __forceinline__ float fa_rcp(float x) {  // 0 of an infinity
+    float r;
+    asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(x));
+    return r;
+}
+// (1 - erf(u / sqrt 2)) / 2 of u >= 0, as e^(-u^2 / 2) times a polynomial in t = 1 / (1 + p u) whose coefficients are a fit, by reweighted least
+// squares, with the smallest relative error over u = 0 .. 14: 1e-7, and 9e-7 with the roundings of the exponential up to u = 4, 3e-6 up to 8.
+__device__ __forceinline__ float fa_upper_tail(float u) {
+    const float t = fa_rcp(fmaf(u, 0.23334524f, 1.0f));
+    float s = -0.0676725209f;
+    s = fmaf(s, t, 0.230117321f);
+    s = fmaf(s, t, -0.175572917f);
+    s = fmaf(s, t, 0.204248384f);
+    s = fmaf(s, t, 0.0236110892f);
+    s = fmaf(s, t, 0.100611739f);
+    s = fmaf(s, t, 0.0914779976f);
+    s = fmaf(s, t, 0.0931788981f);
+    return s * t * fa_exp2(u * u * -0.72134752f);
+}
+
+// Activations of sixteen values that a rounding to 16 bits follows: in line, in about 5 to 18 instructions each (the calls of fa_act4 took 2.8 us of
+// 13.6 with relu and 8.4 us of 19.2 with gelu, at 832 x 1280 x 3328).
+__device__ __forceinline__ void fa_act16(float (&u)[16], int act) {
+    if (act == SCAP_ACT_RELU) {
+#pragma unroll
+        for (int j = 0; j < 16; ++j) u[j] = u[j] < 0.0f ? 0.0f : u[j];
+    } else if (act == SCAP_ACT_SILU) {
+#pragma unroll
+        for (int j = 0; j < 16; ++j) u[j] *= fa_rcp(1.0f + fa_exp2(-1.44269504f * u[j]));
+    } else if (act == SCAP_ACT_GELU) {
+#pragma unroll
+        for (int j = 0; j < 16; ++j) {
+            const float q = fa_upper_tail(fabsf(u[j]));
+            u[j] *= u[j] < 0.0f ? q : 1.0f - q;
+        }
+    } else if (act == SCAP_ACT_GELU_TANH) {  // (1 + tanh a) / 2 = 1 / (1 + e^(-2a))
+#pragma unroll
+        for (int j = 0; j < 16; ++j) u[j] *= fa_rcp(1.0f + fa_exp2(u[j] * fmaf(u[j] * u[j], -0.10294324f, -2.3022082f)));
+    }
+}
+
 // Elements of y and r: fp32, or 16 bits of the type of x.  A load gives the bits, 0 where it is off (no branch, and nothing that
 // waits for them, so that a batch of loads is under way together); fa_widen makes the number of them.
 template <bool F32>
@@ -167,6 +214,19 @@ __device__ __forceinline__ void fa_store(void *p, long long i, float v) {
     if constexpr (F32) reinterpret_cast<float *>(p)[i] = v;
     else if constexpr (BF16) reinterpret_cast<__nv_bfloat16 *>(p)[i] = __float2bfloat16_rn(v);
     else reinterpret_cast<__half *>(p)[i] = __float2half_rn(v);
+}
+// Two rows of a lane's channel against one row of a pair of channels: lanes 2i and 2i+1 hold channels c and c+1, each with row a in the lower and
+// row a+1 in the upper half.  Lane 2i gets row a, lane 2i+1 row a+1, of both channels.  The same step again undoes it.
+__device__ __forceinline__ uint32_t fa_swap(uint32_t v, uint32_t sel) { return __byte_perm(v, __shfl_xor_sync(0xffffffffu, v, 1), sel); }
+template <bool BF16>
+__device__ __forceinline__ uint32_t fa_pack(float lo, float hi) {
+    if constexpr (BF16) {
+        const __nv_bfloat162 v = __floats2bfloat162_rn(lo, hi);
+        return *reinterpret_cast<const uint32_t *>(&v);
+    } else {
+        const __half2 v = __floats2half2_rn(lo, hi);
+        return *reinterpret_cast<const uint32_t *>(&v);
+    }
 }
 
 // Tile number -> channel tile and row tile.  Row tiles are walked in groups: the tiles that run at the same time then share both
@@ -334,10 +394,27 @@ __global__ void __launch_bounds__(FA_THREADS, 1) fc_act_kernel(const FaArgs a, c
             const float bias = on && a.b ? ld_act(a.b + col) : 0.0f;
             const int m0 = tm * a.BN, rows = min(a.BN, a.M - m0);
             // The residual of 16 rows is asked for ahead of their accumulators: while the MMAs run, and while the 16 rows before are worked on.
-            uint32_t r[16];
+            // 16-bit rows move four bytes per lane: a pair of channels, of even rows in even lanes and of odd rows in odd ones.  (A lane with one
+            // channel and two bytes per store took 45 cycles per row of a tile, 11.2 us in place of 13.3 at 832 x 1280 x 3328.)
+            uint32_t r[F32 ? 16 : 8];
+            const uint32_t sel = lane & 1 ? 0x3276u : 0x5410u;
+            const int colp = col & ~1;
             auto ask_r = [&](int c) {
+                if constexpr (F32) {
 #pragma unroll
-                for (int j = 0; j < 16; ++j) r[j] = fa_load<F32>(a.r, (long long)(m0 + c + j) * a.ldr + col, on && c + j < rows);
+                    for (int j = 0; j < 16; ++j) r[j] = fa_load<F32>(a.r, (long long)(m0 + c + j) * a.ldr + col, on && c + j < rows);
+                } else {
+                    const int left = on ? rows - c - (lane & 1) : 0;
+                    const unsigned short *p = reinterpret_cast<const unsigned short *>(a.r) + (long long)(m0 + c + (lane & 1)) * a.ldr + colp;
+                    if (a.ldr & 1) {  // (rows that begin between two words)
+#pragma unroll
+                        for (int j = 0; j < 8; ++j)
+                            r[j] = ld_act_if_u16(p + 2 * j * a.ldr, 2 * j < left) | (uint32_t)ld_act_if_u16(p + 2 * j * a.ldr + 1, 2 * j < left) << 16;
+                    } else {
+#pragma unroll
+                        for (int j = 0; j < 8; ++j) r[j] = __float_as_uint(ld_act_if(reinterpret_cast<const float *>(p + 2 * j * a.ldr), 2 * j < left));
+                    }
+                }
             };
             if (S == 1 && a.r) ask_r(half * 16);
             bool ok = true;
@@ -368,21 +445,48 @@ __global__ void __launch_bounds__(FA_THREADS, 1) fc_act_kernel(const FaArgs a, c
                 float u[16];
 #pragma unroll
                 for (int j = 0; j < 16; ++j) u[j] = v[j] + bias;
-                if (a.act != SCAP_ACT_NONE) {
+                if constexpr (!F32) fa_act16(u, a.act);
+                else if (a.act != SCAP_ACT_NONE) {
 #pragma unroll
                     for (int j = 0; j < 16; j += 4) {
                         const float4 w = fa_act4(make_float4(u[j], u[j + 1], u[j + 2], u[j + 3]), a.act);
                         u[j] = w.x; u[j + 1] = w.y; u[j + 2] = w.z; u[j + 3] = w.w;
                     }
                 }
-                if (a.r) {
+                if constexpr (F32) {
+                    if (a.r) {
 #pragma unroll
-                    for (int j = 0; j < 16; ++j) u[j] += fa_widen<BF16, F32>(r[j]);
-                    ask_r(c + 32);
+                        for (int j = 0; j < 16; ++j) u[j] += fa_widen<BF16, F32>(r[j]);
+                        ask_r(c + 32);
+                    }
+#pragma unroll
+                    for (int j = 0; j < 16; ++j)
+                        if (on && c + j < rows) fa_store<BF16, F32>(a.y, (long long)(m0 + c + j) * a.ldy + col, u[j]);
+                } else {
+                    if (a.r) {
+#pragma unroll
+                        for (int j = 0; j < 8; ++j) {
+                            const uint32_t w = fa_swap(r[j], sel);
+                            u[2 * j] += widen_bits<BF16>((unsigned short)w);
+                            u[2 * j + 1] += widen_bits<BF16>((unsigned short)(w >> 16));
+                        }
+                        ask_r(c + 32);
+                    }
+                    uint32_t w[8];
+#pragma unroll
+                    for (int j = 0; j < 8; ++j) w[j] = fa_swap(fa_pack<BF16>(u[2 * j], u[2 * j + 1]), sel);
+                    const int left = on ? rows - c - (lane & 1) : 0;
+                    unsigned short *p = reinterpret_cast<unsigned short *>(a.y) + (long long)(m0 + c + (lane & 1)) * a.ldy + colp;
+                    if (a.ldy & 1) {
+#pragma unroll
+                        for (int j = 0; j < 8; ++j)
+                            if (2 * j < left) { p[2 * j * a.ldy] = (unsigned short)w[j]; p[2 * j * a.ldy + 1] = (unsigned short)(w[j] >> 16); }
+                    } else {
+#pragma unroll
+                        for (int j = 0; j < 8; ++j)
+                            if (2 * j < left) *reinterpret_cast<uint32_t *>(p + 2 * j * a.ldy) = w[j];
+                    }
                 }
-#pragma unroll
-                for (int j = 0; j < 16; ++j)
-                    if (on && c + j < rows) fa_store<BF16, F32>(a.y, (long long)(m0 + c + j) * a.ldy + col, u[j]);
             };
             if constexpr (F32) {
                 constexpr int NC = FA_MAX_BN_F32 / 32;
@@ -527,6 +631,7 @@ __global__ void __launch_bounds__(FA_THREADS, 1) fc_act_kernel(const FaArgs a, c
 // Rows of x whose stride TMA cannot take (not a multiple of 16 bytes), copied to rows that it can.
 __global__ void fc_act_repack_kernel(const unsigned short *x, long long ldx, unsigned short *out, int ldo, int M, int K) {
     griddep_wait();
+    griddep_launch_dependents();  // (the product asks for its first weights meanwhile, and waits for this kernel before it looks at x)
     const long long n = (long long)M * ldo;
     for (long long i = (long long)blockIdx.x * blockDim.x + threadIdx.x; i < n; i += (long long)gridDim.x * blockDim.x) {
         const long long m = i / ldo;
@@ -545,22 +650,61 @@ static int fa_stages(int cg, int BN) {
     return n < FA_MAX_STAGES ? n : FA_MAX_STAGES;
 }
 
+// Clusters of S CTAs that the device holds at once.  A CTA takes a whole SM, and a cluster needs S free SMs of one group of SMs, so the larger
+// sizes leave SMs over: of 148, 9 clusters of 8 would be only 72, yet a tenth of a size that does not fit waits for a whole turn of the others.
+static int fa_clusters(int S) {
+    static std::atomic<int> cached_by_dev[64][MAX_CLUSTER + 1];
+    if (S == 1) return sm_count();
+    int dev = 0;
+    if (cudaGetDevice(&dev) != cudaSuccess) { cudaGetLastError(); dev = -1; }
+    if (dev >= 0 && dev < 64) {
+        const int hit = cached_by_dev[dev][S].load(std::memory_order_relaxed);
+        if (hit) return hit;
+    }
+    int n = sm_count() / S;
+    static SmemOptIn opt_in;
+    auto kern = fc_act_kernel<true, 1, false>;
+    if (ensure_dynamic_smem(kern, FA_SMEM, opt_in) == cudaSuccess) {
+        cudaLaunchConfig_t cfg = {};
+        cfg.gridDim = dim3(1, S);
+        cfg.blockDim = dim3(FA_THREADS);
+        cfg.dynamicSmemBytes = FA_SMEM;
+        cudaLaunchAttribute attr[1];
+        attr[0].id = cudaLaunchAttributeClusterDimension;
+        attr[0].val.clusterDim.x = 1;
+        attr[0].val.clusterDim.y = S;
+        attr[0].val.clusterDim.z = 1;
+        cfg.attrs = attr;
+        cfg.numAttrs = 1;
+        int found = 0;
+        if (cudaOccupancyMaxActiveClusters(&found, kern, &cfg) == cudaSuccess && found > 0) n = found;
+        else cudaGetLastError();
+    } else {
+        cudaGetLastError();
+    }
+    if (dev >= 0 && dev < 64) cached_by_dev[dev][S].store(n, std::memory_order_relaxed);
+    return n;
+}
+
 // The form with the shortest estimate, in cycles: waves of tiles x blocks of 128 channels x the slower of a block's MMAs and its loads (60
 // bytes per cycle and SM, from L2), W at the rate of the memory, and what the epilogue and the sum over ranks cost.
 static FaPlan fa_plan(int M, int K, int N, bool f32) {
-    const int sms = sm_count(), nkb = (K + FA_BK - 1) / FA_BK;
+    const int nkb = (K + FA_BK - 1) / FA_BK;
     FaPlan best = {1, 16, 1, 0};
     const double floor = 0.3 * K * (double)N * 2 / 1000.0;  // W at the rate of the memory, in cycles
     double best_t = 1e300;
+    int slots_of[MAX_CLUSTER + 1];
+    for (int S = 1; S <= MAX_CLUSTER; ++S) slots_of[S] = fa_clusters(S);
     for (int cg = 1; cg <= 2; ++cg)
         for (int BN = 16 * cg; BN <= (f32 ? FA_MAX_BN_F32 : 256); BN += 16 * cg) {
             if (BN >= M + 16 * cg) break;
             const long long tiles = (long long)((N + FA_TN * cg - 1) / (FA_TN * cg)) * ((M + BN - 1) / BN);
             const int most = cg == 1 ? MAX_CLUSTER : 1;
             for (int S = 1; S <= most; ++S) {
-                if (S > 1 && (S > nkb || tiles * S > sms)) break;
-                const double slots = cg == 2 ? sms / 2 : sms;
-                const double waves = (double)((long long)((tiles * S + slots - 1) / slots));
+                if (S > nkb) break;
+                const int slots = slots_of[cg == 2 ? 2 : S];
+                if (S > 1 && tiles > slots) continue;
+                const double waves = (double)((tiles + slots - 1) / slots);
                 const double mma = 8.0 * (BN / 2 < 46 ? 46 : BN / 2), load = (FA_ABYTES + BN / cg * FA_BK * 2) / 60.0;
                 double t = waves * ((nkb + S - 1) / S) * (mma > load ? mma : load);
                 t = sqrt(t * t + floor * floor);  // the closer to the memory's rate, the slower each SM's share
@@ -592,7 +736,7 @@ static cudaError_t fa_launch_y(const FaArgs &a, const CUtensorMap &wmap, const C
     const int tiles = a.tiles_n * a.tiles_m;
     cudaLaunchConfig_t cfg = {};
     if (CG == 2) {
-        const int pairs = sm_count() / 2;
+        const int pairs = fa_clusters(2);
         cfg.gridDim = dim3(2 * (tiles < pairs ? tiles : pairs));
     } else {
         cfg.gridDim = a.S > 1 ? dim3(tiles, a.S) : dim3(tiles < sm_count() ? tiles : sm_count());
