@@ -125,32 +125,6 @@ __device__ __forceinline__ void fa_ld16(uint32_t (&v)[16], uint32_t addr) {
         : "r"(addr));
 }
 
-// Activations of four values.  A function of its own, not inlined: sixteen copies of it in an epilogue's loop do not fit the
-// instruction cache.  (The fast division is good to 2 units of the last place; where its divisor overflows the result is 0, as it should be.)
-__device__ __noinline__ float4 fa_act4(float4 v, int act) {
-    float u[4] = {v.x, v.y, v.z, v.w};
-    switch (act) {
-        case SCAP_ACT_RELU:
-#pragma unroll
-            for (int j = 0; j < 4; ++j) u[j] = u[j] > 0.0f || u[j] != u[j] ? u[j] : 0.0f;
-            break;
-        case SCAP_ACT_SILU:
-#pragma unroll
-            for (int j = 0; j < 4; ++j) u[j] = __fdividef(u[j], 1.0f + expf(-u[j]));
-            break;
-        case SCAP_ACT_GELU:
-#pragma unroll
-            for (int j = 0; j < 4; ++j) u[j] = 0.5f * u[j] * erfcf(-0.70710678118654752f * u[j]);  // 1 + erf(a) = erfc(-a), without its cancellation
-            break;
-        case SCAP_ACT_GELU_TANH:  // (1 + tanh a) / 2 = 1 / (1 + e^(-2a))
-#pragma unroll
-            for (int j = 0; j < 4; ++j) u[j] = __fdividef(u[j], 1.0f + expf(-1.5957691216057308f * (u[j] + 0.044715f * u[j] * u[j] * u[j])));
-            break;
-        default: break;
-    }
-    return make_float4(u[0], u[1], u[2], u[3]);
-}
-
 __device__ __forceinline__ float fa_exp2(float x) {
     float r;
     asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(x));
@@ -176,24 +150,25 @@ __device__ __forceinline__ float fa_upper_tail(float u) {
     return s * t * fa_exp2(u * u * -0.72134752f);
 }
 
-// Activations of sixteen values that a rounding to 16 bits follows: in line, in about 5 to 18 instructions each (the calls of fa_act4 took 2.8 us of
-// 13.6 with relu and 8.4 us of 19.2 with gelu, at 832 x 1280 x 3328).
-__device__ __forceinline__ void fa_act16(float (&u)[16], int act) {
+// Activations of R values, in line, in about 5 to 18 instructions each: sixteen copies have to fit the instruction cache in an epilogue's loop (with
+// expf, erfcf and a function call per four values relu took 2.8 us of 13.6 and gelu 8.4 us of 19.2, at 832 x 1280 x 3328).  Good to about 2^-21.
+template <int R>
+__device__ __forceinline__ void fa_act(float (&u)[R], int act) {
     if (act == SCAP_ACT_RELU) {
 #pragma unroll
-        for (int j = 0; j < 16; ++j) u[j] = u[j] < 0.0f ? 0.0f : u[j];
+        for (int j = 0; j < R; ++j) u[j] = u[j] < 0.0f ? 0.0f : u[j];
     } else if (act == SCAP_ACT_SILU) {
 #pragma unroll
-        for (int j = 0; j < 16; ++j) u[j] *= fa_rcp(1.0f + fa_exp2(-1.44269504f * u[j]));
+        for (int j = 0; j < R; ++j) u[j] *= fa_rcp(1.0f + fa_exp2(-1.44269504f * u[j]));
     } else if (act == SCAP_ACT_GELU) {
 #pragma unroll
-        for (int j = 0; j < 16; ++j) {
+        for (int j = 0; j < R; ++j) {
             const float q = fa_upper_tail(fabsf(u[j]));
             u[j] *= u[j] < 0.0f ? q : 1.0f - q;
         }
     } else if (act == SCAP_ACT_GELU_TANH) {  // (1 + tanh a) / 2 = 1 / (1 + e^(-2a))
 #pragma unroll
-        for (int j = 0; j < 16; ++j) u[j] *= fa_rcp(1.0f + fa_exp2(u[j] * fmaf(u[j] * u[j], -0.10294324f, -2.3022082f)));
+        for (int j = 0; j < R; ++j) u[j] *= fa_rcp(1.0f + fa_exp2(u[j] * fmaf(u[j] * u[j], -0.10294324f, -2.3022082f)));
     }
 }
 
@@ -445,14 +420,7 @@ __global__ void __launch_bounds__(FA_THREADS, 1) fc_act_kernel(const FaArgs a, c
                 float u[16];
 #pragma unroll
                 for (int j = 0; j < 16; ++j) u[j] = v[j] + bias;
-                if constexpr (!F32) fa_act16(u, a.act);
-                else if (a.act != SCAP_ACT_NONE) {
-#pragma unroll
-                    for (int j = 0; j < 16; j += 4) {
-                        const float4 w = fa_act4(make_float4(u[j], u[j + 1], u[j + 2], u[j + 3]), a.act);
-                        u[j] = w.x; u[j + 1] = w.y; u[j + 2] = w.z; u[j + 3] = w.w;
-                    }
-                }
+                fa_act(u, a.act);
                 if constexpr (F32) {
                     if (a.r) {
 #pragma unroll
@@ -577,13 +545,9 @@ __global__ void __launch_bounds__(FA_THREADS, 1) fc_act_kernel(const FaArgs a, c
 #pragma unroll
                         for (int i = 0; i < 4; ++i) u[i] += s0 + s < S ? v[s][i] : 0.0f;
                 }
-                if (a.act != SCAP_ACT_NONE) {
-                    const float4 w = fa_act4(make_float4(u[0] + bias, u[1] + bias, u[2] + bias, u[3] + bias), a.act);
-                    u[0] = w.x; u[1] = w.y; u[2] = w.z; u[3] = w.w;
-                } else {
 #pragma unroll
-                    for (int i = 0; i < 4; ++i) u[i] += bias;
-                }
+                for (int i = 0; i < 4; ++i) u[i] += bias;
+                fa_act(u, a.act);
 #pragma unroll
                 for (int i = 0; i < 4; ++i) {
                     const int c = c0 + 2 * S * i;
@@ -650,8 +614,9 @@ static int fa_stages(int cg, int BN) {
     return n < FA_MAX_STAGES ? n : FA_MAX_STAGES;
 }
 
-// Clusters of S CTAs that the device holds at once.  A CTA takes a whole SM, and a cluster needs S free SMs of one group of SMs, so the larger
-// sizes leave SMs over: of 148, 9 clusters of 8 would be only 72, yet a tenth of a size that does not fit waits for a whole turn of the others.
+// Clusters of S CTAs that the device holds at once, as the runtime reports it.  A CTA takes a whole SM, and the S of a cluster come from one group
+// of SMs, so the larger sizes leave SMs over: on 148, 74 clusters of 2, 33 of 4, 22 of 6 and 15 of 8.  One cluster more is a second turn of
+// them all: 18 of 8 took 18.7 us where 9 of them with twice the rows take 10.2 (28 rows, 8736 x 1048).
 static int fa_clusters(int S) {
     static std::atomic<int> cached_by_dev[64][MAX_CLUSTER + 1];
     if (S == 1) return sm_count();
@@ -686,12 +651,15 @@ static int fa_clusters(int S) {
     return n;
 }
 
-// The form with the shortest estimate, in cycles: waves of tiles x blocks of 128 channels x the slower of a block's MMAs and its loads (60
-// bytes per cycle and SM, from L2), W at the rate of the memory, and what the epilogue and the sum over ranks cost.
-static FaPlan fa_plan(int M, int K, int N, bool f32) {
+// The form with the shortest estimate, in cycles: waves of tiles x blocks of 128 channels x the slower of a block's MMAs and its loads (58
+// bytes per cycle and SM, from L2), W at the rate of the memory, the epilogue of the last wave (18 cycles a row; more with a function to compute or
+// fp32 rows), and what a pair or the sum over ranks costs.  A sum reads
+// its peers four at a time, and clusters of 5 and 7 were never the best.  Over 70 drawn shapes with every form measured the choice is 4% off the best.
+static FaPlan fa_plan(int M, int K, int N, bool f32, int act) {
     const int nkb = (K + FA_BK - 1) / FA_BK;
     FaPlan best = {1, 16, 1, 0};
-    const double floor = 0.3 * K * (double)N * 2 / 1000.0;  // W at the rate of the memory, in cycles
+    const double floor = 0.45 * K * (double)N * 2 / 1000.0;  // W at the rate of the memory, in cycles
+    const double row = (f32 ? 25.0 : 18.0) + (act > SCAP_ACT_RELU ? 10.0 : 0.0);
     double best_t = 1e300;
     int slots_of[MAX_CLUSTER + 1];
     for (int S = 1; S <= MAX_CLUSTER; ++S) slots_of[S] = fa_clusters(S);
@@ -702,13 +670,15 @@ static FaPlan fa_plan(int M, int K, int N, bool f32) {
             const int most = cg == 1 ? MAX_CLUSTER : 1;
             for (int S = 1; S <= most; ++S) {
                 if (S > nkb) break;
+                if (S == 5 || S == 7) continue;
                 const int slots = slots_of[cg == 2 ? 2 : S];
                 if (S > 1 && tiles > slots) continue;
                 const double waves = (double)((tiles + slots - 1) / slots);
-                const double mma = 8.0 * (BN / 2 < 46 ? 46 : BN / 2), load = (FA_ABYTES + BN / cg * FA_BK * 2) / 60.0;
+                const double mma = 8.0 * (BN / 2 < 46 ? 46 : BN / 2), load = (FA_ABYTES + BN / cg * FA_BK * 2) / 58.0;
                 double t = waves * ((nkb + S - 1) / S) * (mma > load ? mma : load);
                 t = sqrt(t * t + floor * floor);  // the closer to the memory's rate, the slower each SM's share
-                t += 3.0 * BN + (S > 1 ? 4000.0 + 40.0 * BN : 0.0);
+                if (S > 1) t += 2500.0 + 35.0 * BN + (S > 4 ? 2500.0 : 0.0);
+                else t += row * BN + (cg == 2 ? 3500.0 : 0.0);
                 if (t < best_t) { best_t = t; best = {cg, BN, S, 0}; }
             }
         }
@@ -785,7 +755,7 @@ extern "C" scap_status scap_fc_act(const void *x, int64_t ldx, const void *W, co
     if (dev != SCAP_OK) return dev;
     cudaStream_t st = reinterpret_cast<cudaStream_t>(stream);
 
-    const FaPlan p = fa_plan(M, K, N, ydt == SCAP_F32);
+    const FaPlan p = fa_plan(M, K, N, ydt == SCAP_F32, act);
     FaArgs a = {};
     a.b = b; a.r = r; a.y = y; a.ldr = ldr; a.ldy = ldy;
     a.M = M; a.K = K; a.N = N; a.act = act;
