@@ -343,6 +343,8 @@ __global__ void __launch_bounds__(PG_THREADS) kv4_compact_kernel(const PgCache c
 
 // ---- host --------------------------------------------------------------------------------------------------------------------------------
 
+static bool aligned4(const int *p) { return (reinterpret_cast<uintptr_t>(p) & 3u) == 0; }  // (one number: any int will do)
+
 static scap_status pg_check(const scap_kv4 *c, bool rows) {
     if (!c || !c->pages) return SCAP_ERR_INVALID_ARG;
     if (rows && (!c->table || !c->lens || !c->refs)) return SCAP_ERR_INVALID_ARG;
@@ -412,7 +414,7 @@ extern "C" scap_status scap_kv4_fork(const scap_kv4 *cache, const int *src, cons
     if (n < 0 || n > cache->n_seqs) return SCAP_ERR_SHAPE;
     if (n == 0) return SCAP_OK;
     if (!src || !dst || !ws) return SCAP_ERR_INVALID_ARG;
-    if (!aligned16(src) || !aligned16(dst) || !aligned16(ws)) return SCAP_ERR_ALIGN;
+    if (!aligned16(src) || !aligned16(dst) || !aligned16(ws) || !aligned4(fail_out)) return SCAP_ERR_ALIGN;
     if (ws_bytes < scap_kv4_pages_workspace(cache->n_pages, n)) return SCAP_ERR_WORKSPACE;
     s = check_device();
     if (s != SCAP_OK) return s;
@@ -441,7 +443,7 @@ extern "C" scap_status scap_kv4_reserve(const scap_kv4 *cache, const int *add, i
     scap_status s = pg_check(cache, true);
     if (s != SCAP_OK) return s;
     if (!add || !ws) return SCAP_ERR_INVALID_ARG;
-    if (!aligned16(add) || !aligned16(ws)) return SCAP_ERR_ALIGN;
+    if (!aligned16(add) || !aligned16(ws) || !aligned4(fail_out)) return SCAP_ERR_ALIGN;
     if (ws_bytes < scap_kv4_pages_workspace(cache->n_pages, 1)) return SCAP_ERR_WORKSPACE;
     s = check_device();
     if (s != SCAP_OK) return s;
@@ -453,7 +455,7 @@ extern "C" scap_status scap_kv4_compact(const scap_kv4 *cache, int *used_out, vo
     scap_status s = pg_check(cache, true);
     if (s != SCAP_OK) return s;
     if (!ws) return SCAP_ERR_INVALID_ARG;
-    if (!aligned16(ws)) return SCAP_ERR_ALIGN;
+    if (!aligned16(ws) || !aligned4(used_out)) return SCAP_ERR_ALIGN;
     if (ws_bytes < scap_kv4_pages_workspace(cache->n_pages, 1)) return SCAP_ERR_WORKSPACE;
     s = check_device();
     if (s != SCAP_OK) return s;

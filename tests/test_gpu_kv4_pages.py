@@ -370,3 +370,15 @@ def test_refusals():
     for f, args in ((L.scap_kv4_fork, (P, P, 0, P, P, big, None)), (L.scap_kv4_free, (P, 0, None)), (L.scap_kv4_copy, (P, P, 0, None))):
         assert both(f, *args) == 0
     assert L.scap_kv4_pages_workspace(0, 1) == 0 and L.scap_kv4_pages_workspace(8, 4097) == 0
+
+
+def test_counts_that_lie_between_two_ints_are_refused():
+    from paper_2412_07174_b200 import binding, build
+    build.build()
+    L = binding.lib()
+    P, big = 0x10000, 1 << 30
+    c = fake_cache(binding, heads=0, head_dim=0, group=0)
+    for off in (1, 2, 3):
+        assert L.scap_kv4_fork(C.addressof(c), P, P, 2, P + off, P, big, None) == 4
+        assert L.scap_kv4_reserve(C.addressof(c), P, P + off, P, big, None) == 4
+        assert L.scap_kv4_compact(C.addressof(c), P + off, P, big, None) == 4
