@@ -2,8 +2,8 @@
 //
 // Both kernels take their rows in runs: the rows of one sequence that fall into one 32-token tile.  A block has a run and one head: a
 // word of V codes holds the eight tokens 8 j + 2 t + o, and whoever writes one of them has to write back the other seven, so warp t of
-// four has those.  A lane has D/32 neighbouring channels.  Bound by instruction issue (prompts: about 100 instructions per token, head and
-// side, 524000 of these for 8191 tokens of 32 heads) or by the latency of a few dependent loads (single tokens).
+// four has those.  A lane has D/32 neighbouring channels.  Bound by instruction issue (prompts: about 170 instructions of a warp per token,
+// head and side, 524000 of these for 8191 tokens of 32 heads) or by the latency of a few dependent loads (single tokens).
 //
 // Quantisation is decided exactly as its definition in real numbers: (hi - lo) / 15 in binary64 and rounded to 20 bits there, and
 // x / s in binary32 unless it comes near a tie, which is then decided in binary64.

@@ -208,3 +208,47 @@ def test_refusals():
     assert call(M=0, x=None) == 0
     assert L.scap_fc_act_workspace(4, 64, 64, 63) == 0 and L.scap_fc_act_workspace(-1, 64, 64, 64) == 0
     assert L.scap_fc_act_workspace(4, 61, 64, 61) == 4 * 64 * 2
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("M,K,N,ldy", [(1, 64, 24, 25), (2, 40, 8, 9), (31, 130, 136, 137), (300, 256, 520, 523), (1000, 128, 2056, 2059), (33, 2048, 264, 267)])
+@pytest.mark.parametrize("dt", [BF, HF])
+def test_rows_that_begin_between_two_words(M, K, N, ldy, dt):
+    run_case(M, K, N, dt, dt, act="gelu", in_place=True, ldy=ldy, seed=M)       # y and the residual at odd strides
+    run_case(M, K, N, dt, dt, act="relu", in_place=True, ldy=ldy + 1, seed=M)   # at even ones that are no multiple of eight
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("act", list(ACTS))
+@pytest.mark.parametrize("dt,ydt", [(BF, BF), (HF, HF), (BF, F32), (HF, F32)])
+@pytest.mark.parametrize("K", [8, 8192])  # (8192 of a few rows: a sum over ranks)
+def test_activations_over_the_range_of_numbers(act, dt, ydt, K):
+    """u = x[m, 0] alone, exactly: what is left is the activation and one rounding."""
+    import paper_2412_07174_b200 as scap
+    big = 3e38 if dt is BF else 6e4
+    vals = [0.0, -0.0, 1e-7, -1e-7, 1e-3, -1e-3, 300.0, -300.0, big / 2, -big / 2, big, -big, float("inf"), float("nan")]
+    vals += torch.linspace(-16, 16, 601).tolist()
+    x = torch.zeros(len(vals), K, device="cuda").to(dt)
+    x[:, 0] = torch.tensor(vals, device="cuda").to(dt)
+    W = torch.zeros(K, 16, device="cuda").to(dt)
+    W[0] = 1.0
+    for rows in (slice(0, 10), slice(10, 21), slice(None)):  # few rows and many take different forms
+        xs = x[rows].contiguous()
+        y = torch.full((xs.shape[0], 16), 5.0, device="cuda").to(ydt)
+        scap.scap_fc_act(xs, W, None, y, torch.empty(16, dtype=torch.uint8, device="cuda"), act=ACTS[act])
+        u = xs[:, :1].double().expand(-1, 16)
+        ref = act64(u, act)
+        nan, inf = u.isnan(), u.isinf()
+        assert bool(y[nan].isnan().all()) and bool((y[inf] == float("inf")).all())
+        fine = ~(nan | inf)
+        # The argument z of the exponential has at most four roundings, each 2^-24 of it, which make it wrong by so much of itself; the exponential,
+        # the reciprocal and the polynomial add fewer than 16 units of 2^-24.  Then the rounding to the type of y, and what lies below its smallest
+        # numbers (an exponential below 2^-126 is 0).
+        z = {"silu": u.abs(), "gelu": u * u / 2, "gelu_tanh": 1.6 * (u.abs() + 0.045 * u.abs() ** 3)}.get(act, u * 0)
+        rel = (4 * z + 16) * 2.0 ** -24 + torch.finfo(ydt).eps / 2
+        least = {F32: 1e-36, BF: 1e-36, HF: 2.0 ** -25}[ydt]
+        limit = torch.finfo(ydt).max
+        want = torch.where(ref.abs() > limit, ref.sign() * float("inf"), ref)
+        err = torch.where(want.isinf(), (y.double() != want).double(), (y.double() - ref).abs())
+        bound = torch.where(ref.abs() > 0, ref.abs() * rel.clamp(max=4.0), 0.0) + least
+        assert bool((err[fine] <= bound[fine]).all()), float((err / bound)[fine].max())
