@@ -2,7 +2,7 @@
 //
 // Both kernels take their rows in runs: the rows of one sequence that fall into one 32-token tile.  A block has a run and one head: a
 // word of V codes holds the eight tokens 8 j + 2 t + o, and whoever writes one of them has to write back the other seven, so warp t of
-// four has those.  A lane has D/32 neighbouring channels.  Bound by instruction issue (prompts: about 170 instructions of a warp per token,
+// four has those.  A lane has eight neighbouring channels of a token (append) or D/32 of every token (read).  Bound by instruction issue (prompts: about 170 instructions of a warp per token,
 // head and side, 524000 of these for 8191 tokens of 32 heads) or by the latency of a few dependent loads (single tokens).
 //
 // Quantisation is decided exactly as its definition in real numbers: (hi - lo) / 15 in binary64 and rounded to 20 bits there, and
@@ -109,75 +109,78 @@ __device__ __forceinline__ KvVec<CPL> kv_load(const void *p, long long i, bool o
     return r;
 }
 
-// Codes of a lane's channels (nibble i = channel i) and the word of its group.  All lanes of the warp take part.
+// Codes of a lane's channels (nibble i = channel i) and the word of its group.  All lanes of the warp take part.  True where they
+// come too near a tie, and kv_quantise_near has to look.
 template <int CPL, int GL, bool BF16>
-__device__ __forceinline__ uint32_t kv_quantise(const KvVec<CPL> &v, uint32_t &word) {
+__device__ __forceinline__ bool kv_quantise(const KvVec<CPL> &v, uint32_t &codes, uint32_t &word, float &lo, float &s) {
     // smallest value and smallest negative in one register, per group of lanes
-    uint32_t m = 0;  // (0, 0): the range always holds zero
+    uint32_t m2 = 0;  // (0, 0): the range always holds zero
 #pragma unroll
     for (int k = 0; k < CPL / 2; ++k) {
         const uint32_t a = v.w[k];
-        m = kv_min2<BF16>(m, __byte_perm(a, a ^ 0x80008000u, 0x5410));  // (x0, -x0)
-        m = kv_min2<BF16>(m, __byte_perm(a, a ^ 0x80008000u, 0x7632));  // (x1, -x1)
+        m2 = kv_min2<BF16>(m2, __byte_perm(a, a ^ 0x80008000u, 0x5410));  // (x0, -x0)
+        m2 = kv_min2<BF16>(m2, __byte_perm(a, a ^ 0x80008000u, 0x7632));  // (x1, -x1)
     }
 #pragma unroll
-    for (int o = 1; o < GL; o *= 2) m = kv_min2<BF16>(m, __shfl_xor_sync(0xffffffffu, m, o));
-    float lo, hi;
-    widen2<BF16>(m, lo, hi);
+    for (int o = 1; o < GL; o *= 2) m2 = kv_min2<BF16>(m2, __shfl_xor_sync(0xffffffffu, m2, o));
+    float hi;
+    widen2<BF16>(m2, lo, hi);
     hi = -hi;
-    if (!(fabsf(lo) < __int_as_float(0x7f800000) && fabsf(hi) < __int_as_float(0x7f800000))) {  // an infinity or a NaN: the group reads as NaN
-        word = 0x7fc00000u;
-        return 0;
-    }
-    const float s = kv_scale(lo, hi);
-    if (s == 0.0f) {
-        word = 0;
-        return 0;
-    }
-    // round(x / s), ties to even, as in real numbers: by the product with 1 / s (good to 2^-23), which is at most a little over 15, so
-    // it is off by less than 3e-6 - right unless it comes that near a tie; rounded by adding 1.5 2^23, whose last bit is one.
+    const float inf = __int_as_float(0x7f800000);
+    const bool bad = !(fabsf(lo) < inf && fabsf(hi) < inf);  // an infinity or a NaN: the group reads as NaN
+    s = kv_scale(lo, hi);
+    // round(x / s) + zero, ties to even, as in real numbers: by the product with 1 / s (good to 2^-23) added to 1.5 2^23 + zero, whose last bit is
+    // one.  The product is at most a little over 15, so it is off by less than 2e-6 - right unless it comes that near a tie, which is seen from
+    // what the rounding took off.  Codes lie at or above 0 by themselves: x >= lo, so round(x / s) >= round(lo / s) = -zero.
     constexpr float BIG = 12582912.0f;
-    const float inv = kv_rcp(s);
-    float x[CPL];
-#pragma unroll
-    for (int k = 0; k < CPL / 2; ++k) widen2<BF16>(v.w[k], x[2 * k], x[2 * k + 1]);
-    const float tz = -lo * inv, nz = (tz + BIG) - BIG;
-    bool near = fabsf(tz - nz) > 0.4999f || s < 0x1p-100f;  // (no use of 1 / s there)
-    int zero = (int)(__float_as_uint(tz + BIG) - __float_as_uint(BIG)), n[CPL];
+    const uint32_t big = __float_as_uint(BIG);
+    const float inv = kv_rcp(s), mz = fmaf(-lo, inv, BIG);
+    float off = fabsf(fmaf(-lo, inv, BIG - mz));
+    const float base = fminf(mz, BIG + 15.0f);
+    uint32_t sum = 0;
 #pragma unroll
     for (int k = 0; k < CPL; ++k) {
-        const float t = x[k] * inv, m = t + BIG;
-        n[k] = (int)(__float_as_uint(m) - __float_as_uint(BIG));
-        near = near || fabsf(t - (m - BIG)) > 0.4999f;
+        float x[2];
+        widen2<BF16>(v.w[k / 2], x[0], x[1]);
+        const float m = fmaf(x[k & 1], inv, base);
+        off = fmaxf(off, fabsf(fmaf(x[k & 1], inv, base - m)));
+        sum += min(__float_as_uint(m), big + 15u) << (4 * k);
     }
-    if (near) {
-        zero = (int)rint(-(double)lo / (double)s);
-#pragma unroll 1
-        for (int k = 0; k < CPL; ++k) {
-            const int q = (int)rint((double)x[0] / (double)s);
-#pragma unroll
-            for (int i = 0; i < CPL; ++i) n[i] = i == k ? q : n[i];
-#pragma unroll
-            for (int i = 0; i + 1 < CPL; ++i) x[i] = x[i + 1];  // (rolled: one copy of the division)
-        }
-    }
-    zero = min(15, max(0, zero));
+    const bool none = bad || s == 0.0f;
+    codes = none ? 0u : sum - big * (0x11111111u >> (32 - 4 * CPL));
+    word = bad ? 0x7fc00000u : (none ? 0u : __float_as_uint(s) | (__float_as_uint(base) - big));
+    return !none && (off > 0.49999f || s < 0x1p-100f);  // (no use of 1 / s below)
+}
+template <int CPL, bool BF16>
+__device__ __forceinline__ void kv_quantise_near(KvVec<CPL> v, uint32_t &codes, uint32_t &word, float lo, float s) {
+    const int zero = min(15, max(0, (int)rint(-(double)lo / (double)s)));
     word = __float_as_uint(s) | (uint32_t)zero;
-    uint32_t codes = 0;
+    codes = 0;
+#pragma unroll 1
+    for (int k = 0; k < CPL; ++k) {  // (rolled: one copy of the division)
+        float x, next;
+        widen2<BF16>(v.w[0], x, next);
+        codes |= (uint32_t)min(15, max(0, (int)rint((double)x / (double)s) + zero)) << (4 * k);
 #pragma unroll
-    for (int k = 0; k < CPL; ++k) codes |= (uint32_t)min(15, max(0, n[k] + zero)) << (4 * k);
-    return codes;
+        for (int i = 0; i < CPL / 2; ++i) v.w[i] = __funnelshift_r(v.w[i], i + 1 < CPL / 2 ? v.w[i + 1] : 0u, 16);
+    }
 }
 
 template <int D, int GROUP, bool BF16>
-__global__ void __launch_bounds__(KV_THREADS) kv4_append_kernel(const KvCache c, const KvRows r) {
-    constexpr int CPL = D / 32, GL = GROUP / CPL, GROUPS = D / GROUP;  // channels of a lane, lanes of a group
+__global__ void __launch_bounds__(KV_THREADS, 6) kv4_append_kernel(const KvCache c, const KvRows r) {
+    // Eight channels of a lane, so what a group costs whatever its size (its range over the lanes, its scale, its zero point) is shared by as many as
+    // fit one load: a warp takes 256 / D tokens at a time.
+    constexpr int CPL = 8, LPT = D / CPL, TPW = 32 / LPT, GL = GROUP / CPL, GROUPS = D / GROUP;  // lanes of a token, tokens of a warp, lanes of a group
+    constexpr int OUT = CPL / TPW;                                                              // words of V codes that a lane stores
     griddep_wait();
     griddep_launch_dependents();
-    const int lane = threadIdx.x & 31, t = threadIdx.x >> 5, h = blockIdx.y;
+    const int lane = threadIdx.x & 31, t = threadIdx.x >> 5, h = blockIdx.y, sub = lane / LPT;
     constexpr int tile_bytes = kv_tile_bytes(D, GROUPS);
-    const int ch = lane * CPL, g = ch / GROUP;
+    const int ch = lane % LPT * CPL, g = ch / GROUP;
     const bool writes = lane % GL == 0;
+    int out = 0;  // first of its channels whose word of V codes this lane stores
+#pragma unroll
+    for (int d = LPT, have = CPL / 2; d < 32; d *= 2, have /= 2) out += lane & d ? have : 0;
     const int row0 = blockIdx.x * r.per_block, row1 = min(row0 + r.per_block, r.rows);
     for (int row = row0; row < row1;) {
         const KvRun run = kv_run(c, r, row, lane);
@@ -192,14 +195,6 @@ __global__ void __launch_bounds__(KV_THREADS) kv4_append_kernel(const KvCache c,
             if (n >= 0 && n < run.n) mask |= 15u << (4 * ((i >> 1) + 4 * (i & 1)));
         }
         if (mask == 0) continue;
-        const int page = kv_page(c, run.seq, run.pos);
-        if (page < 0) continue;
-        unsigned char *tile = kv_tile(c, page, h, run.pos, tile_bytes);
-        uint32_t *kw = reinterpret_cast<uint32_t *>(tile + kv_k_words(D)) + g * KV_TILE, *vw = reinterpret_cast<uint32_t *>(tile + kv_v_words(D, GROUPS)) + g * KV_TILE;
-        uint32_t *vcodes = reinterpret_cast<uint32_t *>(tile + kv_v_codes(D));
-        uint32_t vcode[CPL];
-#pragma unroll
-        for (int k = 0; k < CPL; ++k) vcode[k] = mask == 0xffffffffu ? 0u : __ldcg(vcodes + kv_v_word(ch + k, t)) & ~mask;
         // (rolled, with the next token's values under way: unrolled the code does not fit the instruction cache)
         auto tok_of = [&](int i) { return 8 * (i >> 1) + 2 * t + (i & 1); };
         auto ask = [&](int i, KvVec<CPL> &kx, KvVec<CPL> &vx) {
@@ -209,31 +204,53 @@ __global__ void __launch_bounds__(KV_THREADS) kv4_append_kernel(const KvCache c,
             vx = kv_load<CPL>(r.v, (long long)(first + n) * r.ldv + (long long)h * D + ch, on);
         };
         KvVec<CPL> kx[2], vx[2];
-        ask(0, kx[0], vx[0]);
-        ask(1, kx[1], vx[1]);
+        ask(sub, kx[0], vx[0]);
+        ask(sub + TPW, kx[1], vx[1]);
+        const int page = kv_page(c, run.seq, run.pos);
+        if (page < 0) continue;
+        unsigned char *tile = kv_tile(c, page, h, run.pos, tile_bytes);
+        uint32_t *kw = reinterpret_cast<uint32_t *>(tile + kv_k_words(D)) + g * KV_TILE, *vw = reinterpret_cast<uint32_t *>(tile + kv_v_words(D, GROUPS)) + g * KV_TILE;
+        uint32_t *vcodes = reinterpret_cast<uint32_t *>(tile + kv_v_codes(D));
+        uint32_t old[OUT], vcode[CPL];
+#pragma unroll
+        for (int k = 0; k < OUT; ++k) old[k] = mask == 0xffffffffu ? 0u : __ldcg(vcodes + kv_v_word(ch + out + k, t)) & ~mask;
+#pragma unroll
+        for (int k = 0; k < CPL; ++k) vcode[k] = 0;
 #pragma unroll 1
-        for (int i = 0; i < 8; ++i) {
+        for (int i = sub; i < 8; i += TPW) {  // (as often in all lanes)
             const KvVec<CPL> k0 = kx[0], v0 = vx[0];
             kx[0] = kx[1];
             vx[0] = vx[1];
-            ask(i + 2, kx[1], vx[1]);
+            ask(i + 2 * TPW, kx[1], vx[1]);
             const int tok = tok_of(i);
-            if (tok < tok0 || tok >= tok0 + run.n) continue;  // (the same for all lanes)
-            uint32_t word;
-            const uint32_t kc = kv_quantise<CPL, GL, BF16>(k0, word);
-            unsigned char *to = tile + tok * (D / 2) + kv_k_byte(D, ch);
-            if constexpr (CPL == 2) *to = (unsigned char)kc;
-            else if constexpr (CPL == 4) *reinterpret_cast<unsigned short *>(to) = (unsigned short)kc;
-            else *reinterpret_cast<uint32_t *>(to) = kc;
-            if (writes) kw[kv_word_at(tok)] = word;
-            const uint32_t vc = kv_quantise<CPL, GL, BF16>(v0, word);
-            if (writes) vw[kv_word_at(tok)] = word;
+            const bool on = tok >= tok0 && tok < tok0 + run.n;
+            if (!__any_sync(0xffffffffu, on)) continue;
+            // (nothing but zeros where there is no token)
+            uint32_t kc, vc, kword, vword;
+            float klo, ks, vlo, vs;
+            const bool knear = kv_quantise<CPL, GL, BF16>(k0, kc, kword, klo, ks), vnear = kv_quantise<CPL, GL, BF16>(v0, vc, vword, vlo, vs);
+            if (knear) kv_quantise_near<CPL, BF16>(k0, kc, kword, klo, ks);
+            if (vnear) kv_quantise_near<CPL, BF16>(v0, vc, vword, vlo, vs);
+            if (on) *reinterpret_cast<uint32_t *>(tile + tok * (D / 2) + kv_k_byte(D, ch)) = kc;
+            if (on && writes) {
+                kw[kv_word_at(tok)] = kword;
+                vw[kv_word_at(tok)] = vword;
+            }
             const int nib = 4 * ((i >> 1) + 4 * (i & 1));
 #pragma unroll
             for (int k = 0; k < CPL; ++k) vcode[k] |= ((vc >> (4 * k)) & 15u) << nib;
         }
+        // The tokens of a word from all lanes that have some; each keeps the words that it stores.
 #pragma unroll
-        for (int k = 0; k < CPL; ++k) vcodes[kv_v_word(ch + k, t)] = vcode[k];
+        for (int d = LPT, have = CPL / 2; d < 32; d *= 2, have /= 2)
+#pragma unroll
+            for (int k = 0; k < have; ++k) {
+                const bool upper = lane & d;
+                const uint32_t away = __shfl_xor_sync(0xffffffffu, upper ? vcode[k] : vcode[k + have], d);
+                vcode[k] = (upper ? vcode[k + have] : vcode[k]) | away;
+            }
+#pragma unroll
+        for (int k = 0; k < OUT; ++k) vcodes[kv_v_word(ch + out + k, t)] = vcode[k] | old[k];
     }
 }
 
