@@ -2,8 +2,9 @@
 //
 // Both kernels take their rows in runs: the rows of one sequence that fall into one 32-token tile.  A block has a run and one head: a
 // word of V codes holds the eight tokens 8 j + 2 t + o, and whoever writes one of them has to write back the other seven, so warp t of
-// four has those.  A lane has eight neighbouring channels of a token (append) or D/32 of every token (read).  Bound by instruction issue (prompts: about 170 instructions of a warp per token,
-// head and side, 524000 of these for 8191 tokens of 32 heads) or by the latency of a few dependent loads (single tokens).
+// four has those.  A lane has eight neighbouring channels of a token (append) or D/32 of every token (read).  Bound by instruction issue
+// (prompts: 8191 tokens of 32 heads take 88 us, 48 of them without the quantisation; the bytes alone are 26) or by the latency of a few
+// dependent loads (single tokens).
 //
 // Quantisation is decided exactly as its definition in real numbers: (hi - lo) / 15 in binary64 and rounded to 20 bits there, and
 // x / s in binary32 unless it comes near a tie, which is then decided in binary64.
@@ -166,12 +167,14 @@ __device__ __forceinline__ void kv_quantise_near(KvVec<CPL> v, uint32_t &codes, 
     }
 }
 
-template <int D, int GROUP, bool BF16>
-__global__ void __launch_bounds__(KV_THREADS, 6) kv4_append_kernel(const KvCache c, const KvRows r) {
-    // Eight channels of a lane, so what a group costs whatever its size (its range over the lanes, its scale, its zero point) is shared by as many as
-    // fit one load: a warp takes 256 / D tokens at a time.
-    constexpr int CPL = 8, LPT = D / CPL, TPW = 32 / LPT, GL = GROUP / CPL, GROUPS = D / GROUP;  // lanes of a token, tokens of a warp, lanes of a group
-    constexpr int OUT = CPL / TPW;                                                              // words of V codes that a lane stores
+template <int D, int GROUP, bool BF16, int CPL>
+__global__ void __launch_bounds__(KV_THREADS, CPL == D / 32 ? 7 : 6) kv4_append_kernel(const KvCache c, const KvRows r) {
+    // Many rows: eight channels of a lane, so what a group costs whatever its size (its range over the lanes, its scale, its zero point) is paid for
+    // several at once, as a warp takes 256 / D tokens at a time (one token of a warp: 111 us; six CTAs of an SM, 85 registers: 94 -> 88).
+    // Few rows, so that a block looks for one: all lanes for the one token that there is, a shorter way (64 tokens of 32 heads, with the read
+    // behind it: 12.0 -> 10.2 us; seven CTAs of an SM, or the 2048 of them take three waves).
+    constexpr int LPT = D / CPL, TPW = 32 / LPT, GL = GROUP / CPL, GROUPS = D / GROUP;  // lanes of a token, tokens of a warp, lanes of a group
+    constexpr int OUT = CPL / TPW;                                                      // words of V codes that a lane stores
     griddep_wait();
     griddep_launch_dependents();
     const int lane = threadIdx.x & 31, t = threadIdx.x >> 5, h = blockIdx.y, sub = lane / LPT;
@@ -231,7 +234,12 @@ __global__ void __launch_bounds__(KV_THREADS, 6) kv4_append_kernel(const KvCache
             const bool knear = kv_quantise<CPL, GL, BF16>(k0, kc, kword, klo, ks), vnear = kv_quantise<CPL, GL, BF16>(v0, vc, vword, vlo, vs);
             if (knear) kv_quantise_near<CPL, BF16>(k0, kc, kword, klo, ks);
             if (vnear) kv_quantise_near<CPL, BF16>(v0, vc, vword, vlo, vs);
-            if (on) *reinterpret_cast<uint32_t *>(tile + tok * (D / 2) + kv_k_byte(D, ch)) = kc;
+            if (on) {
+                unsigned char *to = tile + tok * (D / 2) + kv_k_byte(D, ch);
+                if constexpr (CPL == 2) *to = (unsigned char)kc;
+                else if constexpr (CPL == 4) *reinterpret_cast<unsigned short *>(to) = (unsigned short)kc;
+                else *reinterpret_cast<uint32_t *>(to) = kc;
+            }
             if (on && writes) {
                 kw[kv_word_at(tok)] = kword;
                 vw[kv_word_at(tok)] = vword;
@@ -341,7 +349,10 @@ template <int D, int GROUP>
 static cudaError_t kv_launch(bool append, bool bf16, const KvCache &c, const KvRows &r, cudaStream_t st) {
     const dim3 grid((r.rows + r.per_block - 1) / r.per_block, c.heads), block(KV_THREADS);
     const bool pdl = g_tune.pdl != 0;
-    if (append) return bf16 ? launch(kv4_append_kernel<D, GROUP, true>, grid, block, 0, st, pdl, c, r) : launch(kv4_append_kernel<D, GROUP, false>, grid, block, 0, st, pdl, c, r);
+    if (append && r.per_block > 1)
+        return bf16 ? launch(kv4_append_kernel<D, GROUP, true, 8>, grid, block, 0, st, pdl, c, r) : launch(kv4_append_kernel<D, GROUP, false, 8>, grid, block, 0, st, pdl, c, r);
+    if (append)
+        return bf16 ? launch(kv4_append_kernel<D, GROUP, true, D / 32>, grid, block, 0, st, pdl, c, r) : launch(kv4_append_kernel<D, GROUP, false, D / 32>, grid, block, 0, st, pdl, c, r);
     return bf16 ? launch(kv4_read_kernel<D, GROUP, true>, grid, block, 0, st, pdl, c, r) : launch(kv4_read_kernel<D, GROUP, false>, grid, block, 0, st, pdl, c, r);
 }
 
