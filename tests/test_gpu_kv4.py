@@ -244,3 +244,49 @@ def test_refusals():
         assert call(f, rows=0) == 0
     assert L.scap_kv4_page_bytes(64, 8, 128, 64) == 8 * 2 * (32 * 128 + 2 * 2 * 128)
     assert L.scap_kv4_page_bytes(63, 8, 128, 64) == 0 and L.scap_kv4_page_bytes(64, 8, 100, 64) == 0
+
+
+# Many rows times heads take the form with eight channels of a lane, from 16 rows and heads per multiprocessor on (2368 on 148 of them).
+@pytest.mark.gpu
+@pytest.mark.parametrize("D,group", SHAPES)
+@pytest.mark.parametrize("dt", [BF, HF])
+def test_long_prompts_in_pieces(D, group, dt):
+    pieces = [[45, 0, 3, 77, 31], [50, 33, 1, 90, 60], [7, 64, 32, 0, 29]]
+    heads = 24
+    total = np.sum(pieces, 0).tolist()
+    c = Cache(total, page=64, heads=heads, D=D, group=group, dt=dt, seed=D + group)
+    c.lens.zero_()
+    k = [[] for _ in total]
+    v = [[] for _ in total]
+    for i, counts in enumerate(pieces):
+        n = sum(counts)
+        assert n * heads >= 2368
+        kn, vn = tokens(n, heads, D, dt, 3 * i), tokens(n, heads, D, dt, 3 * i + 1)
+        c.lens += torch.tensor(counts, dtype=torch.int32, device="cuda")
+        c.scap.scap_kv4_append(c.cache, kn, vn, starts(counts))
+        at = np.concatenate(([0], np.cumsum(counts)))
+        for b in range(len(total)):
+            k[b].append(kn[at[b]:at[b + 1]])
+            v[b].append(vn[at[b]:at[b + 1]])
+    ko, vo = read_back(c, sum(total), total)
+    want = [torch.cat([torch.cat(x) for x in y]) for y in (k, v)]
+    assert same(ko, stored64(want[0], group)) and same(vo, stored64(want[1], group)) and c.guards_intact()
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("D,group", SHAPES)
+@pytest.mark.parametrize("dt", [BF, HF])
+def test_values_at_the_borders_of_many_heads(D, group, dt):
+    heads, r = 300, torch.arange(D).float()
+    rows = [torch.zeros(D), torch.full((D,), -3.0), (r % 16) - 7.5, ((r % 31) - 15) * 0.5, (r % 2) * 2.0 ** -24, torch.where(r == 5, float("nan"), r),
+            torch.where(r == D - 2, float("inf"), -r), torch.where(r == D - 2, -float("inf"), r), torch.where(r % 2 == 0, 65504.0, -65504.0), (r % 16) * 0.1, -(r % 16) / 3]
+    if dt is BF:
+        rows += [(r - D / 2) * 2.0 ** 118, (r - 64) * 2.0 ** -140, (r % 3) * 2.0 ** -133, torch.where(r % 2 == 0, 3.38e38, -3.38e38), (r % 15) * 2.0 ** -101, (r % 15 - 7) * 2.0 ** -99]
+    x = torch.stack(rows)[:, None, :].expand(-1, heads, -1).to(dt).to("cuda")
+    k, v = x.contiguous(), x.flip(0).contiguous()
+    n = x.shape[0]
+    assert n * heads >= 2368
+    c = Cache([n], page=32, heads=heads, D=D, group=group, dt=dt)
+    c.scap.scap_kv4_append(c.cache, k, v, starts([n]))
+    ko, vo = read_back(c, n, [n])
+    assert same(ko, stored64(k, group)) and same(vo, stored64(v, group)) and c.guards_intact()
