@@ -241,7 +241,9 @@ __global__ void __launch_bounds__(AT_THREADS, at_resident(D, G, RN)) kv4_attend_
     extern __shared__ __align__(128) unsigned char at_raw[];
     uint4 *s_q = reinterpret_cast<uint4 *>(at_raw + AT_WARPS * ST * TILE);  // [RN][W][32 lanes]
     __shared__ uint32_t s_zq[QS ? RN : 1][G][32];
-    __shared__ float s_f[RN];
+    // What turns an accumulator of a row into a score in units of log 2, by warp (QS: by eight rows).  Read once per tile: in registers, one more of them
+    // than before, the kernel for 256 channels spilled (300 sequences of together 30000 tokens, 8 key heads: 66 -> 82 us).
+    __shared__ __align__(8) float s_f[QS ? RN : AT_WARPS][8];
     __shared__ unsigned long long s_full[AT_WARPS][ST];
     __shared__ long long s_sum[AT_WARPS + 5 * (SOLO ? AT_WARPS : 1)];
     __shared__ float s_m[AT_WARPS][ROWS], s_l[AT_WARPS][ROWS];
@@ -331,12 +333,12 @@ __global__ void __launch_bounds__(AT_THREADS, at_resident(D, G, RN)) kv4_attend_
         // (the first tile alone: those of all warps of the device are then under way before anybody's second)
         if (lane == 0 && count > 0) ask(at_now, slot);
 
-        // ---- queries: rows 8 rn + qg as B operands, scaled by one power of two so that the largest lies just below 2^12 (what is lost of
-        // a row that is smaller by 2^x is 2^-36 of the largest scores); channels 32 j + 8 qt + i, the
-        // even and odd nibbles of a code word in the two k halves of an MMA, the odd ones 16 times smaller as their codes are larger.
+        // ---- queries: rows 8 rn + qg as B operands, each scaled by a power of two of its own so that its largest channel lies in 2^11 .. 2^12 (a
+        // row does not depend on those it is taken with); channels 32 j + 8 qt + i, the
+        // even and odd nibbles of a code word in the two k halves of an MMA, the odd ones 16 times smaller as their codes are larger: a channel is exact
+        // down to 2^-21 of the largest of its row, and off by 2^-32 of that below.
         // zq: minus the sum of a group, in two fp16 parts, against the zero points (times 2^6, as zero 2^-18 is the subnormal used)
         uint32_t qb[QS ? 1 : 2 * W][2], zq[QS ? 1 : G];
-        float f[RN];  // what turns an accumulator into a score in units of log 2
         if (!QS || warp < RN) {  // (in shared memory: warp rn for its eight rows)
             const int rn = QS ? warp : 0, row = 8 * rn + qg;
             uint4 raw[W];
@@ -353,24 +355,23 @@ __global__ void __launch_bounds__(AT_THREADS, at_resident(D, G, RN)) kv4_attend_
                     v[j][i] = at_widen((unsigned short)(i & 1 ? w >> 16 : w), a.bf16);
                     top = fmaxf(top, fabsf(v[j][i]));
                 }
-            if (!(top < INFINITY)) top = 0.0f;  // (a row that is not finite has no say)
-#pragma unroll
-            for (int k = 1; k < 32; k *= 2) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, k));
-            int e = top > 0.0f ? 11 - ((__float_as_int(top) >> 23) - 127) : 0;
-            e = e > 100 ? 100 : (e < -100 ? -100 : e);
-            const float up = at_pow2(e);
+            if (!(top < INFINITY)) top = 0.0f;  // (a row that is not finite stays so, whatever its scale)
+            top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 1));  // of the four lanes that have the row
+            top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 2));
+            const int e = top > 0.0f ? min(126, 11 - ((__float_as_int(top) >> 23) - 127)) : 0;  // at least -116
+            const float up = at_pow2(e), up16 = up * 0.0625f;
             float sum[G];
 #pragma unroll
             for (int n = 0; n < G; ++n) sum[n] = 0.0f;
 #pragma unroll
             for (int j = 0; j < W; ++j) {
 #pragma unroll
-                for (int i = 0; i < 8; ++i) sum[j * G / W] += v[j][i];
+                for (int i = 0; i < 8; ++i) sum[j * G / W] = fmaf(v[j][i], up, sum[j * G / W]);
                 uint32_t w[2][2];
 #pragma unroll
                 for (int hi = 0; hi < 2; ++hi) {
                     w[hi][0] = at_pack(v[j][2 * hi] * up, v[j][2 * hi + 4] * up);
-                    w[hi][1] = at_pack(v[j][2 * hi + 1] * (up * 0.0625f), v[j][2 * hi + 5] * (up * 0.0625f));
+                    w[hi][1] = at_pack(v[j][2 * hi + 1] * up16, v[j][2 * hi + 5] * up16);
                     if constexpr (!QS) { qb[2 * j + hi][0] = w[hi][0]; qb[2 * j + hi][1] = w[hi][1]; }
                 }
                 if constexpr (QS) s_q[(rn * W + j) * 32 + lane] = make_uint4(w[0][0], w[0][1], w[1][0], w[1][1]);
@@ -379,21 +380,16 @@ __global__ void __launch_bounds__(AT_THREADS, at_resident(D, G, RN)) kv4_attend_
             for (int n = 0; n < G; ++n) {
                 sum[n] += __shfl_xor_sync(0xffffffffu, sum[n], 1);
                 sum[n] += __shfl_xor_sync(0xffffffffu, sum[n], 2);
-                const float x = -sum[n] * up * 0.015625f, x_hi = __half2float(__float2half_rn(x));
+                const float x = -sum[n] * 0.015625f, x_hi = __half2float(__float2half_rn(x));
                 if constexpr (QS) s_zq[rn][n][lane] = at_pack(x_hi, x - x_hi);
                 else zq[n] = at_pack(x_hi, x - x_hi);
             }
-            f[0] = at_pow2(24 - e) * a.scale;
-            if constexpr (QS) {
-                if (lane == 0) s_f[rn] = f[0];
-            }
+            const float back = a.scale * at_pow2((24 - e) / 2) * at_pow2(24 - e - (24 - e) / 2);
+            if (qt == 0) s_f[warp][qg] = back;
+            __syncwarp();
         }
         if (lane > 0 && lane < ST && lane < count) ask(at_now, slot + lane < ST ? slot + lane : slot + lane - ST);
-        if constexpr (QS) {
-            __syncthreads();
-#pragma unroll
-            for (int rn = 0; rn < RN; ++rn) f[rn] = s_f[rn];
-        }
+        if constexpr (QS) __syncthreads();
         // keys that row 8 rn + 2 qt + k sees: up to that of its own token, hi, and with a window from lo on
         uint32_t tok_of[RN];
 #pragma unroll
@@ -508,15 +504,22 @@ __global__ void __launch_bounds__(AT_THREADS, at_resident(D, G, RN)) kv4_attend_
                         for (int n = 0; n < G; ++n) {
                             const float ks = __uint_as_float(kw[n][2 * m0 + j] & ~15u);
 #pragma unroll
-                            for (int rn = 0; rn < RN; ++rn) {
-                                const float by = ks * f[rn];
+                            for (int rn = 0; rn < RN; ++rn)
 #pragma unroll
                                 for (int k = 0; k < 2; ++k) {
                                     const float x = acc[j >> 1][rn][n][2 * (j & 1) + k];
-                                    s[rn][2 * m0 + j][k] = n == 0 ? by * x : s[rn][2 * m0 + j][k] + by * x;
+                                    s[rn][2 * m0 + j][k] = n == 0 ? ks * x : fmaf(ks, x, s[rn][2 * m0 + j][k]);
                                 }
-                            }
                         }
+                }
+#pragma unroll
+                for (int rn = 0; rn < RN; ++rn) {
+                    const float2 f = *reinterpret_cast<const float2 *>(&s_f[QS ? rn : warp][2 * qt]);
+#pragma unroll
+                    for (int j = 0; j < 4; ++j) {
+                        s[rn][j][0] *= f.x;
+                        s[rn][j][1] *= f.y;
+                    }
                 }
                 uint32_t vw[G][4];
 #pragma unroll
