@@ -5,8 +5,8 @@
 // mask: a code is an fp16 subnormal (see scap_kv4.cuh), and what belongs to a group of channels is applied once per token:
 //   scores  s_t = ks_t (sum_c q_c code_tc - zero_t sum_c q_c), the second sum by one more MMA with the zero points as codes
 //   output  o_c = sum_t (p_t vs_t) code_tc - sum_t (p_t vs_t) zero_t, likewise.
-// p vs is rounded to fp16 (11 bits) once and used in both sums, so the rounding acts on the value v, not on its code part; the queries
-// are scaled by one power of two per eight rows and are exact.  Scores, maxima, sums and accumulators are fp32.
+// p vs is rounded to fp16 (11 bits) once and used in both sums, so the rounding acts on the value v, not on its code part; its size is kept by a
+// reference per row (below).  The queries are scaled by a power of two per row and are exact.  Scores, references, sums and accumulators are fp32.
 // (With the rows as the M rows of the MMA a head with eight or fewer of them pays for sixteen: twice the MMAs, accumulators and
 // exponentials; 131001 tokens, 8 key heads, 8 rows: 57 us against 45 at that time.)
 //
@@ -32,7 +32,12 @@ namespace scap {
 constexpr int AT_WARPS = 4;
 constexpr int AT_THREADS = AT_WARPS * 32;
 constexpr int AT_MIN_UNITS = 4;  // tiles per CTA, one for each warp, unless the items are shorter: an item after another takes 4 us each
-constexpr int AT_UP = 133;       // a scale of exponent field e is below 2^(e - 126), a weight at most 2^8: their product below 2^15 as held
+// The reference m of a row is such that a weight p = 2^(s - m) times the scale of its value (exponent field e: 2^(e - 127) .. 2^(e - 126)) times 2^-24 is
+// 2^10 .. 2^11 for the largest product seen, s + e = m + AT_TOP, and it moves when one would reach 2^15, s + e > m + AT_MOST.  (With 2^-24 the weights of values
+// as large as binary32 holds are still 33 bits above 2^-126, where 2^x becomes 0.)  A scale below 2^-56 counts as 2^-56 here, so that weights stay below
+// 2^94 and the sum of any number of them is finite.
+constexpr float AT_TOP = 161.0f, AT_MOST = 165.0f, AT_DOWN = 0x1p-24f;
+constexpr uint32_t AT_LEAST = 71u << 23;
 
 // CTAs per SM and tiles in a warp's ring, as registers and shared memory allow (RN groups of eight rows, G groups of channels).
 __host__ __device__ constexpr int at_resident(int D, int G, int RN) {
@@ -216,6 +221,11 @@ __device__ __forceinline__ float at_ex2(float v) {  // 2^v; -inf gives 0
     float r;
     asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(v));
     return r;
+}
+// x 2^d for d <= 0, in two steps: 2^d alone is 0 below -126, where a sum of weights may have 94 bits to spare
+__device__ __forceinline__ float at_lower(float x, float d) {
+    const float h = at_ex2(0.5f * d);
+    return x * h * h;
 }
 __device__ __forceinline__ float at_widen(unsigned short u, bool bf16) { return bf16 ? widen_bits<true>(u) : widen_bits<false>(u); }
 __device__ __forceinline__ void at_store(unsigned short *p, float v, bool bf16) {
@@ -404,7 +414,6 @@ __global__ void __launch_bounds__(AT_THREADS, at_resident(D, G, RN)) kv4_attend_
         const int hi_all = len - a.nq, lo_all = a.window > 0 && len > a.window ? len - a.window : 0;  // what every row sees
 
         float o[RN][MT][4], z[RN][G][4], m[RN][2], l[RN][2];
-        int top_e = AT_UP - 126;  // exponent field of the largest scale of values so far (at least this): p vs is held as p vs 2^(AT_UP - top_e)
 #pragma unroll
         for (int rn = 0; rn < RN; ++rn) {
 #pragma unroll
@@ -539,48 +548,57 @@ __global__ void __launch_bounds__(AT_THREADS, at_resident(D, G, RN)) kv4_attend_
                         }
                     }
                 }
-                // ---- largest scale of the values
-                uint32_t big = 0;
+                // ---- reference of a row: by its largest product of a weight and a scale, so that a large value that has next to no weight takes no bits
+                // of the others.  It is left as it is while products stay below 2^15, so that the accumulators are rarely rescaled.
+                float top[RN][2];
+                auto largest = [&](const float (&e)[4]) {
 #pragma unroll
-                for (int n = 0; n < G; ++n) big = max(max(big, max(vw[n][0], vw[n][1])), max(vw[n][2], vw[n][3]));
-                uint32_t most = __reduce_max_sync(0xffffffffu, big);
-                if (most >= 0x7f800000u) {  // a NaN has no say
-                    big = 0;
+                    for (int rn = 0; rn < RN; ++rn)
 #pragma unroll
-                    for (int n = 0; n < G; ++n)
+                        for (int k = 0; k < 2; ++k)
+                            top[rn][k] = fmaxf(fmaxf(s[rn][0][k] + e[0], s[rn][1][k] + e[1]), fmaxf(s[rn][2][k] + e[2], s[rn][3][k] + e[3]));
+                };
+                float e[4];
+                bool fine = true;
 #pragma unroll
-                        for (int j = 0; j < 4; ++j) big = max(big, vw[n][j] < 0x7f800000u ? vw[n][j] : 0u);
-                    most = __reduce_max_sync(0xffffffffu, big);
+                for (int j = 0; j < 4; ++j) {
+                    uint32_t big = AT_LEAST;
+#pragma unroll
+                    for (int n = 0; n < G; ++n) big = max(big, vw[n][j]);
+                    fine = fine && big < 0x7f800000u;
+                    e[j] = (float)(big >> 23);
                 }
-                const int e = (int)(most >> 23);
-                // ---- reference of the weights: the largest score, but left as it is while weights stay below 2^8, so that the
-                // accumulators are rarely rescaled
-                float t[RN][2];
-                bool keep = e <= top_e;
+                largest(e);
+                bool keep = fine;
 #pragma unroll
                 for (int rn = 0; rn < RN; ++rn)
 #pragma unroll
-                    for (int k = 0; k < 2; ++k) {
-                        float x = fmaxf(fmaxf(s[rn][0][k], s[rn][1][k]), fmaxf(s[rn][2][k], s[rn][3][k]));
-                        x = fmaxf(x, __shfl_xor_sync(0xffffffffu, x, 4));
-                        x = fmaxf(x, __shfl_xor_sync(0xffffffffu, x, 8));
-                        x = fmaxf(x, __shfl_xor_sync(0xffffffffu, x, 16));
-                        t[rn][k] = x;
-                        keep = keep && !(x > m[rn][k] + 8.0f);
-                    }
+                    for (int k = 0; k < 2; ++k) keep = keep && !(top[rn][k] > m[rn][k] + AT_MOST);
                 if (!__all_sync(0xffffffffu, keep)) {
-                    const float by = e > top_e ? at_pow2(top_e - e < -126 ? -126 : top_e - e) : 1.0f;
-                    top_e = max(top_e, e);
+                    if (!__all_sync(0xffffffffu, fine)) {
+#pragma unroll
+                        for (int j = 0; j < 4; ++j) {  // (a scale that is NaN has no say)
+                            uint32_t big = AT_LEAST;
+#pragma unroll
+                            for (int n = 0; n < G; ++n) big = max(big, vw[n][j] < 0x7f800000u ? vw[n][j] : 0u);
+                            e[j] = (float)(big >> 23);
+                        }
+                        largest(e);
+                    }
 #pragma unroll
                     for (int rn = 0; rn < RN; ++rn) {
                         float down[2];
 #pragma unroll
                         for (int k = 0; k < 2; ++k) {
-                            const float ref = fmaxf(m[rn][k], t[rn][k]);
-                            down[k] = ref == -INFINITY ? 1.0f : at_ex2(m[rn][k] - ref);
-                            l[rn][k] *= down[k];
+                            float x = top[rn][k];
+                            x = fmaxf(x, __shfl_xor_sync(0xffffffffu, x, 4));
+                            x = fmaxf(x, __shfl_xor_sync(0xffffffffu, x, 8));
+                            x = fmaxf(x, __shfl_xor_sync(0xffffffffu, x, 16));
+                            const float ref = x > m[rn][k] + AT_MOST ? x - AT_TOP : m[rn][k];  // (every row by itself)
+                            const float by = ref == -INFINITY ? 0.0f : m[rn][k] - ref;
+                            l[rn][k] = at_lower(l[rn][k], by);
+                            down[k] = at_ex2(by);
                             m[rn][k] = ref;
-                            down[k] *= by;
                         }
 #pragma unroll
                         for (int n = 0; n < MT; ++n)
@@ -592,25 +610,25 @@ __global__ void __launch_bounds__(AT_THREADS, at_resident(D, G, RN)) kv4_attend_
                             for (int k = 0; k < 4; ++k) z[rn][n][k] *= down[k & 1];
                     }
                 }
+                // ---- weights, those of blocks whose codes are 16 times larger as held made 16 times smaller
 #pragma unroll
                 for (int rn = 0; rn < RN; ++rn)
 #pragma unroll
                     for (int k = 0; k < 2; ++k) {
-                        const float ref = m[rn][k] == -INFINITY ? 0.0f : m[rn][k];  // nothing seen so far: all weights are 0
+                        const float ref = m[rn][k] == -INFINITY ? 0.0f : m[rn][k], ref16 = ref + 4.0f;  // nothing seen so far: all weights are 0
 #pragma unroll
                         for (int j = 0; j < 4; ++j) {
-                            s[rn][j][k] = at_ex2(s[rn][j][k] - ref);
-                            l[rn][k] += s[rn][j][k];
+                            s[rn][j][k] = at_ex2(s[rn][j][k] - (j & 1 ? ref16 : ref));
+                            l[rn][k] = j & 1 ? fmaf(s[rn][j][k], 16.0f, l[rn][k]) : l[rn][k] + s[rn][j][k];
                         }
                     }
                 // ---- weighted values: p vs as B operands (a block of eight tokens x eight rows is transposed in registers)
-                const float up = at_pow2(AT_UP - top_e), up16 = up * 0.0625f;
                 uint32_t pb[G][RN][4];
 #pragma unroll
                 for (int n = 0; n < G; ++n)
 #pragma unroll
                     for (int j = 0; j < 4; ++j) {
-                        const float vs = __uint_as_float(vw[n][j] & ~15u) * (j & 1 ? up16 : up);
+                        const float vs = __uint_as_float(vw[n][j] & ~15u) * AT_DOWN;
 #pragma unroll
                         for (int rn = 0; rn < RN; ++rn) pb[n][rn][j] = at_pack(s[rn][j][0] * vs, s[rn][j][1] * vs);
                     }
@@ -670,8 +688,7 @@ __global__ void __launch_bounds__(AT_THREADS, at_resident(D, G, RN)) kv4_attend_
         }
 
         // ---- join of the four warps: each puts its sums where its ring was (all of its copies have landed)
-        const int es = top_e - AT_UP + 24, e1 = es / 2, e2 = es - e1;
-        const float back1 = at_pow2(e1), back2 = at_pow2(e2);
+        constexpr float BACK = 0x1p24f / AT_DOWN;  // codes are held times 2^-24
         float *part = reinterpret_cast<float *>(ring);
 #pragma unroll
         for (int rn = 0; rn < RN; ++rn)
@@ -689,8 +706,8 @@ __global__ void __launch_bounds__(AT_THREADS, at_resident(D, G, RN)) kv4_attend_
 #pragma unroll
                 for (int n = 0; n < MT; ++n) {
                     const float zz = z[rn][n * G / MT][k];
-                    part[row * PITCH + 16 * n + qg] = (o[rn][n][k] - zz) * back1 * back2;
-                    part[row * PITCH + 16 * n + 8 + qg] = (o[rn][n][2 + k] - zz) * back1 * back2;
+                    part[row * PITCH + 16 * n + qg] = (o[rn][n][k] - zz) * BACK;
+                    part[row * PITCH + 16 * n + 8 + qg] = (o[rn][n][2 + k] - zz) * BACK;
                 }
             }
         if constexpr (SOLO) __syncwarp();
@@ -713,8 +730,9 @@ __global__ void __launch_bounds__(AT_THREADS, at_resident(D, G, RN)) kv4_attend_
             const float ref = top == -INFINITY ? 0.0f : top;
 #pragma unroll
             for (int w = 0; w < NW; ++w) {
-                wt[w] = at_ex2(s_m[SOLO ? warp : w][row] - ref);
-                sum += wt[w] * s_l[SOLO ? warp : w][row];
+                const float by = s_m[SOLO ? warp : w][row] - ref;
+                wt[w] = at_ex2(by);
+                sum += at_lower(s_l[SOLO ? warp : w][row], by);
             }
             const float by = whole ? (sum > 0.0f || sum != sum ? 1.0f / sum : 0.0f) : 1.0f;
             const int in = rt * ROWS + row, tok = in / a.g, hd = in - tok * a.g;
@@ -777,15 +795,15 @@ __device__ __forceinline__ void at_parts(const AtArgs &a, int i0, int i1, int ro
 #pragma unroll
         for (int k = 0; k < AHEAD; ++k) t = i + k * warps < parts ? fmaxf(t, p[k].x) : t;
         const float ref = t == -INFINITY ? 0.0f : t, down = at_ex2(top - ref);
+        sum = at_lower(sum, top - ref);
         top = t;
-        sum *= down;
 #pragma unroll
         for (int c = 0; c < CPL; ++c) v[c] *= down;
 #pragma unroll
         for (int k = 0; k < AHEAD; ++k)
             if (i + k * warps < parts) {
                 const float wt = at_ex2(p[k].x - ref);
-                sum += wt * p[k].y;
+                sum += at_lower(p[k].y, p[k].x - ref);
 #pragma unroll
                 for (int c = 0; c < CPL; ++c) v[c] += wt > 0.0f || x[k][c] != x[k][c] ? wt * x[k][c] : 0.0f;
             }
@@ -832,10 +850,11 @@ __global__ void __launch_bounds__(AT_THREADS) kv4_join_kernel(const AtArgs a) {
             float own = top;
 #pragma unroll
             for (int w = 0; w < AT_WARPS; ++w) top = fmaxf(top, s_top[w]);
-            own = at_ex2(own - (top == -INFINITY ? 0.0f : top));
+            own -= top == -INFINITY ? 0.0f : top;
+            const float wt = at_ex2(own);
 #pragma unroll
-            for (int c = 0; c < CPL; ++c) s_v[warp][lane * CPL + c] = v[c] * own;
-            if (lane == 0) s_w[warp] = sum * own;
+            for (int c = 0; c < CPL; ++c) s_v[warp][lane * CPL + c] = v[c] * wt;
+            if (lane == 0) s_w[warp] = at_lower(sum, own);
             __syncthreads();
             sum = ((s_w[0] + s_w[1]) + s_w[2]) + s_w[3];  // the four warps in order
             const bool any = sum > 0.0f || sum != sum;

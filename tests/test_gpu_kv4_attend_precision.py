@@ -1,14 +1,17 @@
-"""scap_kv4_attend where rows differ much in size."""
+"""scap_kv4_attend where rows and tokens differ much in size: bounds that follow the products of a row, not its largest value."""
+import math
+
 import pytest
 import torch
 
-from test_gpu_kv4_attend import attend, check, filled, queries
+from kv4_testlib import Cache, starts
+from test_gpu_kv4_attend import attend, check, filled, queries, side64
 
-BF = torch.bfloat16
+BF, HF = torch.bfloat16, torch.float16
 
 
 @pytest.mark.gpu
-@pytest.mark.parametrize("nq,g,heads,B", [(1, 8, 2, 3), (4, 2, 1, 2), (5, 4, 1, 2)])  # eight rows of one token and of several, sixteen
+@pytest.mark.parametrize("nq,g,heads,B", [(1, 8, 2, 3), (4, 2, 1, 2), (5, 4, 1, 2), (1, 4, 8, 100)])  # eight rows, eight of several tokens, sixteen, a warp for an item
 @pytest.mark.parametrize("size", [2.0 ** 40, 2.0 ** 100, 2.0 ** 127, 2.0 ** -110])
 def test_a_row_does_not_depend_on_the_rows_beside_it(nq, g, heads, B, size):
     """One query head of a very different size (finite, as a padded or an outlier one): the others keep their bits, and are right."""
@@ -39,3 +42,87 @@ def test_queries_of_any_size(up):
     assert torch.equal(big.double() * 2.0 ** -up, q.double())
     out, lse2 = attend(c, big, 0.125 * 2.0 ** -up)
     assert torch.equal(out, want) and torch.equal(lse2, lse)
+
+
+def tight(c, q, out, lse, lens, nq, scale, run=512):
+    """Against attention in 64 bits, with a bound made of the products of a weight and a value that a row has.  run: additions into one accumulator."""
+    B, _, Hq, D = q.shape
+    g = Hq // c.heads
+    k64, kmag = side64(c.kv[0], c.group)
+    v64, vmag = side64(c.kv[1], c.group)
+    at = 0
+    for b, n in enumerate(lens):
+        for i in range(nq):
+            idx = slice(at, at + n - nq + i + 1)
+            for h in range(c.heads):
+                o, ls = out[b, i, h * g:(h + 1) * g].double(), lse[b, i, h * g:(h + 1) * g].double()
+                qq = q[b, i, h * g:(h + 1) * g].double()
+                s = scale * qq @ k64[idx, h].T
+                want_l = torch.logsumexp(s, -1)
+                p = torch.exp(s - want_l[:, None])
+                want = p @ v64[idx, h]
+                # A score: as in `check`, D / 8 + 16 additions and multiplications in fp32.  s - m is rounded once and below 2^8: 2^-17 of the weight.
+                es = scale * 2 * (qq.abs() @ kmag[idx, h].T) * (D / 8 + 16) * 2.0 ** -23 + 2.0 ** -17
+                # A weight times the scale of its value is rounded to fp16: 2^-11 of it, or half a step of the subnormal numbers, 2^-25, where the largest
+                # product of the row is 2^10 or more, 16 times more in half of the blocks: 2^-31 of the largest (a value is up to 15 scales).
+                err = (p * (2.0 ** -11 + 2 * es)) @ v64[idx, h].abs() + (p * 2 * es).sum(-1, keepdim=True) * want.abs()
+                err = err + (p[..., None] * vmag[idx, h]).amax((-2, -1))[:, None] * len(s[0]) * 2.0 ** -31
+                # code and zero-point parts are added up apart, two additions per tile
+                err = err + 2 * (p @ vmag[idx, h]) * (min(len(s[0]) / 16, run) + 32) * 2.0 ** -23
+                err = err + want.abs() * torch.finfo(out.dtype).eps / 2 * 1.001 + (2.0 ** -25 if out.dtype is HF else 2.0 ** -134)
+                assert bool(((o - want).abs() <= err).all()), (b, i, h, float(((o - want).abs() / err).max()))
+                el = es.amax(-1) + 2.0 ** -22 * (want_l.abs() + math.log(n) + 4)
+                assert bool(((ls - want_l).abs() <= el).all()), (b, i, h, float(((ls - want_l).abs() / el).max()))
+        at += n
+
+
+def spiked(lens, D, group, where, key, value, dt=BF, seed=31):
+    """Tokens of ordinary size, and in every sequence one at `where` (of its length): its key is `key` times the direction of the queries, its values `value`
+    times larger."""
+    c = Cache(lens, heads=1, D=D, group=group, dt=dt)
+    gen = torch.Generator(device="cuda").manual_seed(seed)
+    rand = lambda *s: torch.randn(*s, generator=gen, device="cuda", dtype=torch.float64)  # noqa: E731
+    base = rand(D)
+    k, v = 0.3 * rand(sum(lens), 1, D), rand(sum(lens), 1, D) + 0.5
+    at = 0
+    for n in lens:
+        t = at + int(where * (n - 1))
+        k[t, 0] = key * base
+        v[t, 0] *= value
+        at += n
+    c.kv = (k.to(dt), v.to(dt))
+    c.scap.scap_kv4_append(c.cache, *c.kv, starts(lens))
+    return c, (base + 0.05 * rand(len(lens), 1, 4, D)).to(dt)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("D,group", [(64, 64), (128, 64), (128, 32), (256, 128)])
+@pytest.mark.parametrize("where", [0.0, 0.4, 1.0])
+def test_a_large_value_of_next_to_no_weight(D, group, where):
+    """A token with a weight of about 2^-60 and values 2^30 times as large as the others' takes no bits from them."""
+    lens = [40, 300, 2500]
+    c, q = spiked(lens, D, group, where, -42 / D ** 0.5, 2.0 ** 30)
+    out, lse = attend(c, q, D ** -0.5)
+    tight(c, q, out, lse, lens, 1, D ** -0.5)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("where", [0.0, 0.5])
+@pytest.mark.parametrize("value", [0.0, 2.0 ** -20, 2.0 ** -40])
+def test_a_token_of_all_the_weight_and_small_values(where, value):
+    """An attention sink: nearly all of the weight, values of zero or nearly so.  What the other tokens add is still right."""
+    lens = [40, 300, 2500]
+    c, q = spiked(lens, 128, 128, where, 25 / 128 ** 0.5, value)
+    out, lse = attend(c, q, 128 ** -0.5)
+    tight(c, q, out, lse, lens, 1, 128 ** -0.5)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("up", [-70, -40, 40, 100, 123])
+def test_values_of_any_size(up):
+    lens, D = [200, 1000], 64
+    c, q = spiked(lens, D, 32, 0.5, 0.1, 2.0 ** -6)
+    c.kv = (c.kv[0], (c.kv[1].double().clamp(-7, 7) * 2.0 ** up).to(BF))
+    c.scap.scap_kv4_append(c.cache, *c.kv, starts(lens))
+    out, lse = attend(c, q, D ** -0.5)
+    tight(c, q, out, lse, lens, 1, D ** -0.5)
