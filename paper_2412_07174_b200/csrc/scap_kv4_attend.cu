@@ -64,10 +64,17 @@ struct AtArgs {
     int *status;
 };
 
-// What a warp is at: units [u, u1) of its worker `id`, of which tiles t0 .. t1 - 1 of an item of sequence seq are next.
+// Tiles that a warp adds up in its accumulators before it puts the sums where parts go and begins anew.  The tensor core truncates as it adds: a sum of n
+// numbers of one sign is off by up to n 2^-23 of itself, and code and zero-point part of an output are two such sums whose difference may be small (the mean of
+// 400000 values, a third of them in each warp, was off by 4.7 % of itself; with 256 tiles by 1.0e-3, with 128 by less than the two roundings to 11 bits allow).  Only warps with
+// so many tiles of one item pay for it: 120 sequences of 100000 tokens, 8 key heads: 3763 -> 3865 us (256 tiles: 3811, 64: 3961).
+constexpr int AT_RUN = 128;
+
+// What a warp is at: units [u, u1) of its worker `id`.  Tiles t0 .. t1 - 1 of an item of sequence seq are next, a stretch of the tiles i0 .. i1 - 1 that the
+// worker has of it.
 struct AtWork {
     long long u, u1, base;
-    int id, seq, len, item, tiles, t0, t1;
+    int id, seq, len, item, tiles, t0, t1, i0, i1;
 };
 
 // Tiles that the new tokens of a sequence of `len` tokens can see: first one and number.
@@ -234,6 +241,28 @@ __device__ __forceinline__ void at_store(unsigned short *p, float v, bool bf16) 
 // 2^e for -126 <= e <= 127
 __device__ __forceinline__ float at_pow2(int e) { return __int_as_float((e + 127) << 23); }
 
+// Adds the sums of the stretches before to those that a warp has put into shared memory, for the rows own, own + STEP, ... that this warp puts out (and put
+// where parts go, a channel the same lane).  Out of line: in line it costs the loop over tiles registers (four new tokens of 32 key heads: 80 -> 82 us).
+template <int D, int STEP, int PITCH>
+__device__ __noinline__ void at_fold(int own, int rows, int lane, float *part, float *s_m, float *s_l, const float *sums, const float *ml) {
+    __syncwarp();
+#pragma unroll 1
+    for (int row = own; row < rows; row += STEP) {
+        const float had = ml[2 * row], had_l = ml[2 * row + 1], now = s_m[row], now_l = s_l[row], top = fmaxf(now, had), ref = top == -INFINITY ? 0.0f : top;
+        const float w_now = at_ex2(now - ref), w_had = at_ex2(had - ref);
+#pragma unroll 1
+        for (int c = lane; c < D; c += 32) {
+            const float x = part[row * PITCH + c], y = sums[row * D + c];
+            part[row * PITCH + c] = (w_now > 0.0f || x != x ? w_now * x : 0.0f) + (w_had > 0.0f || y != y ? w_had * y : 0.0f);
+        }
+        __syncwarp();
+        if (lane == 0) {
+            s_m[row] = top;
+            s_l[row] = at_lower(now_l, now - ref) + at_lower(had_l, had - ref);
+        }
+    }
+}
+
 template <int D, int G, int RN, bool SOLO>
 __global__ void __launch_bounds__(AT_THREADS, at_resident(D, G, RN)) kv4_attend_kernel(const AtArgs a) {
     constexpr int W = D / 32;            // words of a K row per lane
@@ -278,6 +307,7 @@ __global__ void __launch_bounds__(AT_THREADS, at_resident(D, G, RN)) kv4_attend_
             work.u1 = place.u1;
             work.base = place.base;
             work.id = place.id;
+            work.t1 = work.i1 = 0;
             work.seq = place.seq;
             work.len = place.len;
         }
@@ -306,12 +336,14 @@ __global__ void __launch_bounds__(AT_THREADS, at_resident(D, G, RN)) kv4_attend_
                 continue;
             }
             const int item = (int)(in_seq / tiles), t0 = (int)(in_seq - (long long)item * tiles);
-            const int t1 = (int)min((long long)tiles, t0 + (work.u1 - work.u));
+            const int i1 = (int)min((long long)tiles, t0 + (work.u1 - work.u)), t1 = min(i1, t0 + AT_RUN * STEP);
             count = !dead && t1 - t0 - own > 0 ? (t1 - t0 - own + STEP - 1) / STEP : 0;  // tiles t0 + own, + STEP, ... are this warp's
             pos0 = (first_tile + t0 + own) * KV_TILE;
             if (lane == 0) {
                 work.item = item;
                 work.tiles = tiles;
+                if (work.t1 == work.i1) work.i0 = t0;  // (else the stretch before this one ended inside the item)
+                work.i1 = i1;
                 work.t0 = t0;
                 work.t1 = t1;
             }
@@ -710,18 +742,19 @@ __global__ void __launch_bounds__(AT_THREADS, at_resident(D, G, RN)) kv4_attend_
                     part[row * PITCH + 16 * n + 8 + qg] = (o[rn][n][2 + k] - zz) * BACK;
                 }
             }
+        const int seq = work.seq, item = work.item, i0 = work.i0, i1 = work.i1, rt = item / a.c.heads, h = item - rt * a.c.heads, rows = min(ROWS, a.nq * a.g - rt * ROWS);
+        const int slot_out = 2 * work.id + (i0 == 0 ? 1 : 0);
+        float *sums = a.part + (size_t)slot_out * ROWS * D, *ml = a.ml + (size_t)slot_out * ROWS * 2;
+        if (work.t0 != i0) at_fold<D, STEP, PITCH>(own, rows, lane, part, s_m[warp], s_l[warp], sums, ml);
         if constexpr (SOLO) __syncwarp();
         else __syncthreads();
-        const int seq = work.seq, item = work.item, t0 = work.t0, t1 = work.t1, rt = item / a.c.heads, h = item - rt * a.c.heads, rows = min(ROWS, a.nq * a.g - rt * ROWS);
-        const bool whole = t0 == 0 && t1 == work.tiles;
+        const bool all = i0 == 0 && i1 == work.tiles, whole = all && work.t1 == i1;  // the item lies in this worker; this is the end of it
         if (SOLO ? lane == 0 : tid == 0) {
             int2 *at = a.where + (long long)seq * per + item;
-            if (whole) *at = make_int2(-1, -1);
-            else if (t0 == 0) at->x = work.id;
-            else if (t1 == work.tiles) at->y = work.id;
+            if (all) *at = make_int2(-1, -1);
+            else if (i0 == 0) at->x = work.id;
+            else if (i1 == work.tiles) at->y = work.id;
         }
-        const int slot_out = 2 * work.id + (t0 == 0 ? 1 : 0);
-        float *sums = a.part + (size_t)slot_out * ROWS * D, *ml = a.ml + (size_t)slot_out * ROWS * 2;
         constexpr int NW = SOLO ? 1 : AT_WARPS;
         for (int row = own; row < rows; row += STEP) {
             float top = -INFINITY, wt[NW], sum = 0.0f;
@@ -759,7 +792,7 @@ __global__ void __launch_bounds__(AT_THREADS, at_resident(D, G, RN)) kv4_attend_
         }
         asm volatile("fence.proxy.async.shared::cta;" ::: "memory");  // the next copies may overwrite what was read and written here
         __syncwarp();
-        if (lane == 0) work.u += t1 - t0;
+        if (lane == 0) work.u += work.t1 - work.t0;
         if constexpr (SOLO) __syncwarp();
         else __syncthreads();
     }

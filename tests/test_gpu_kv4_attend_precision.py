@@ -1,4 +1,4 @@
-"""scap_kv4_attend where rows and tokens differ much in size: bounds that follow the products of a row, not its largest value."""
+"""scap_kv4_attend where rows and tokens differ much in size, and where a sum is long: bounds that follow the products of a row, not its largest value."""
 import math
 
 import pytest
@@ -126,3 +126,44 @@ def test_values_of_any_size(up):
     c.scap.scap_kv4_append(c.cache, *c.kv, starts(lens))
     out, lse = attend(c, q, D ** -0.5)
     tight(c, q, out, lse, lens, 1, D ** -0.5)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("B,heads,g,nq", [(120, 8, 1, 1), (1, 8, 1, 1), (40, 1, 4, 4), (60, 8, 1, 2)])  # a warp for an item; one item over the device; sixteen rows; a CTA for an item
+@pytest.mark.parametrize("scale,hole", [(0.0, 0), (0.125, 0), (0.125, 1800)])
+def test_a_long_mean(B, heads, g, nq, scale, hole):
+    """Means of up to 400000 values, 1 / 630 of their size, as many as 4000 tiles of them in one warp; where there is a hole the first pages are missing.  The
+    sequences share their pages."""
+    import paper_2412_07174_b200 as scap
+    D, page, n, dev = 64, 128, 400000, "cuda"
+    width = -(-n // page)
+    gen = torch.Generator(device=dev).manual_seed(5)
+    k, v = (torch.empty(n, heads, D, dtype=HF, device=dev).normal_(generator=gen) for _ in range(2))
+    pool = torch.zeros(width, scap.scap_kv4_page_bytes(page, heads, D, 64), dtype=torch.uint8, device=dev)
+    row = torch.randperm(width, generator=gen, device=dev).to(torch.int32)
+    lens = torch.full((B,), n, dtype=torch.int32, device=dev)
+    one = scap.ScapKv4(pool, page, heads, D, 64, row[None].contiguous(), lens[:1])
+    scap.scap_kv4_append(one, k, v, torch.tensor([0, n], dtype=torch.int32, device=dev))
+    row[:hole] = -1
+    cache = scap.ScapKv4(pool, page, heads, D, 64, row.expand(B, width).contiguous(), lens)
+    q = queries(B, nq, g * heads, D, HF)
+    out = torch.empty_like(q)
+    lse = torch.empty(B, nq, g * heads, device=dev)
+    ws = torch.full((scap.scap_kv4_attend_workspace(B, nq, g * heads, heads, D),), 255, dtype=torch.uint8, device=dev)
+    scap.scap_kv4_attend(cache, q, out, scale, ws, lse=lse)
+    torch.cuda.synchronize()
+    scap.scap_device_status()
+    k64, v64 = side64(k, 64)[0], side64(v, 64)[0]
+    for b in {0, B - 1}:
+        for i in range(nq):
+            seen = slice(hole * page, n - nq + i + 1)
+            s = scale * torch.einsum("hgd,nhd->hgn", q[b, i].view(heads, g, D).double(), k64[seen])
+            want_l = torch.logsumexp(s, -1)
+            want = torch.einsum("hgn,nhd->hgd", torch.exp(s - want_l[..., None]), v64[seen])
+            # The product of a weight with the scale of its value is off by at most 2^-11 of it, differently from token to token: in the mean of independent
+            # values 2^-11 of its size at most (as a root of mean squares); the rounding of the result likewise.
+            off = (out[b, i].double().view(heads, g, D) - want).square().mean().sqrt() / want.square().mean().sqrt()
+            assert float(off) <= 2.0 ** -10, (b, i, float(off))
+            # a score is off by at most 2 scale sum |q| |k| (D / 8 + 16) 2^-23 (codes and zero points apart, 15 scales each), a weight by 2^-17
+            es = scale * 2 * q[b, i].double().abs().sum(-1).max() * k64.abs().max() * 2 * (D / 8 + 16) * 2.0 ** -23 + 2.0 ** -17
+            assert bool(((lse[b, i].double().view(heads, g) - want_l).abs() <= es).all())
