@@ -216,6 +216,8 @@ scap_status scap_dense_fc(const void *x, const void *W, const float *b, float *y
  *           y itself (with the same stride); x may not overlap y
  *   act     u: none; relu: max(u, 0); silu: u / (1 + e^-u); gelu: u/2 (1 + erf(u / sqrt 2)); gelu_tanh: u/2 (1 + tanh(sqrt(2/pi) (u +
  *           0.044715 u^3)))
+ * An accumulator of the tensor cores, which truncate as they add, takes 512 channels where y is fp32 or K above 16384 (fp16 results) or 131072 (bf16 ones); their
+ * sums are added up in fp32, rounded to nearest.  Below that what the truncation takes off is under an eighth of half a step of y.
  * A NaN or an infinity in x makes its row non-finite before act, one in W its column; a NaN stays one.  Rows and columns beyond M and N are left as they were.
  * Workspace: scap_fc_act_workspace(M, K, N, ldx) bytes.                                                                         */
 typedef enum { SCAP_ACT_NONE = 0, SCAP_ACT_RELU = 1, SCAP_ACT_SILU = 2, SCAP_ACT_GELU = 3, SCAP_ACT_GELU_TANH = 4 } scap_act;

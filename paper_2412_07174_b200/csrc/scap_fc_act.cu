@@ -39,10 +39,13 @@ constexpr int FA_BK = 128;                   // channels per stage: eight MMAs p
 constexpr int FA_TN = 128;                   // output channels per CTA
 constexpr int FA_ABYTES = FA_TN * FA_BK * 2; // 32 KB of W per stage
 // The tensor core truncates where it adds to an accumulator, always towards zero, so a sum is off by about 2^-25 of itself per addition: 3e-6
-// at K = 2560, nothing beside a rounding to 16 bits but much beside one to fp32.  For an fp32 result an accumulator takes 512 channels (32
+// at K = 2560, nothing beside a rounding to 16 bits but much beside one to fp32, and 2e-4 at K = 2^18.  For an fp32 result, and where a sum over all channels would be
+// off by more than an eighth of half a step of the 16-bit result (fa_long), an accumulator takes 512 channels (32
 // additions) and the epilogue warps add those sums up in registers, rounding to nearest, while the next 512 are under way.
 constexpr int FA_CHUNK = 4;
-constexpr int FA_MAX_BN_F32 = 192;           // rows per tile then: the sums of half of them are a thread's registers
+constexpr int FA_MAX_BN_CHUNKED = 192;       // rows per tile then: the sums of half of them are a thread's registers
+// K / 16 additions of 2^-25: an eighth of 2^-12 for fp16, of 2^-9 for bf16.
+static bool fa_long(int K, bool bf16) { return K > (bf16 ? 131072 : 16384); }
 constexpr int FA_MAX_STAGES = 12;
 constexpr int FA_SMEM = 226 * 1024;          // of the 227 KB that a CTA may have; the barriers are inside
 
@@ -213,7 +216,7 @@ __device__ __forceinline__ void fa_tile(const FaArgs &a, int t, int &tn, int &tm
     tm = g * a.groups + in - tn * rows;
 }
 
-template <bool BF16, int CG, bool F32>
+template <bool BF16, int CG, bool F32, bool CHUNKED>
 __global__ void __launch_bounds__(FA_THREADS, 1) fc_act_kernel(const FaArgs a, const __grid_constant__ CUtensorMap wmap,
                                                                 const __grid_constant__ CUtensorMap xmap) {
     extern __shared__ unsigned char fa_raw[];
@@ -230,7 +233,7 @@ __global__ void __launch_bounds__(FA_THREADS, 1) fc_act_kernel(const FaArgs a, c
     const int tiles = a.tiles_n * a.tiles_m;
     const int nkb_all = (a.K + FA_BK - 1) / FA_BK;
     const int kb0 = (int)((long long)nkb_all * srank / S), nkb = (int)((long long)nkb_all * (srank + 1) / S) - kb0;
-    const int chunk = F32 ? FA_CHUNK : nkb;  // stages that are added up in one accumulator
+    const int chunk = CHUNKED ? FA_CHUNK : nkb;  // stages that are added up in one accumulator
     volatile int *abort_flag = &sh->abort_flag;
 
     if (tid == 0) {
@@ -456,8 +459,8 @@ __global__ void __launch_bounds__(FA_THREADS, 1) fc_act_kernel(const FaArgs a, c
                     }
                 }
             };
-            if constexpr (F32) {
-                constexpr int NC = FA_MAX_BN_F32 / 32;
+            if constexpr (CHUNKED) {
+                constexpr int NC = FA_MAX_BN_CHUNKED / 32;
                 float sum[NC][16];
 #pragma unroll
                 for (int i = 0; i < NC; ++i)
@@ -628,7 +631,7 @@ static int fa_clusters(int S) {
     }
     int n = sm_count() / S;
     static SmemOptIn opt_in;
-    auto kern = fc_act_kernel<true, 1, false>;
+    auto kern = fc_act_kernel<true, 1, false, false>;
     if (ensure_dynamic_smem(kern, FA_SMEM, opt_in) == cudaSuccess) {
         cudaLaunchConfig_t cfg = {};
         cfg.gridDim = dim3(1, S);
@@ -655,16 +658,16 @@ static int fa_clusters(int S) {
 // bytes per cycle and SM, from L2), W at the rate of the memory, the epilogue of the last wave (18 cycles a row; more with a function to compute or
 // fp32 rows), and what a pair or the sum over ranks costs.  A sum reads
 // its peers four at a time, and clusters of 5 and 7 were never the best.  Over 70 drawn shapes with every form measured the choice is 4% off the best.
-static FaPlan fa_plan(int M, int K, int N, bool f32, int act) {
+static FaPlan fa_plan(int M, int K, int N, bool chunked, int act) {
     const int nkb = (K + FA_BK - 1) / FA_BK;
     FaPlan best = {1, 16, 1, 0};
     const double floor = 0.45 * K * (double)N * 2 / 1000.0;  // W at the rate of the memory, in cycles
-    const double row = (f32 ? 25.0 : 18.0) + (act > SCAP_ACT_RELU ? 10.0 : 0.0);
+    const double row = (chunked ? 25.0 : 18.0) + (act > SCAP_ACT_RELU ? 10.0 : 0.0);
     double best_t = 1e300;
     int slots_of[MAX_CLUSTER + 1];
     for (int S = 1; S <= MAX_CLUSTER; ++S) slots_of[S] = fa_clusters(S);
     for (int cg = 1; cg <= 2; ++cg)
-        for (int BN = 16 * cg; BN <= (f32 ? FA_MAX_BN_F32 : 256); BN += 16 * cg) {
+        for (int BN = 16 * cg; BN <= (chunked ? FA_MAX_BN_CHUNKED : 256); BN += 16 * cg) {
             if (BN >= M + 16 * cg) break;
             const long long tiles = (long long)((N + FA_TN * cg - 1) / (FA_TN * cg)) * ((M + BN - 1) / BN);
             const int most = cg == 1 ? MAX_CLUSTER : 1;
@@ -697,10 +700,10 @@ static bool fa_map(CUtensorMap *map, const void *p, long long inner, long long o
               CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
-template <bool BF16, int CG, bool F32>
+template <bool BF16, int CG, bool F32, bool CHUNKED>
 static cudaError_t fa_launch_y(const FaArgs &a, const CUtensorMap &wmap, const CUtensorMap &xmap, cudaStream_t st) {
     static SmemOptIn opt_in;
-    auto kern = fc_act_kernel<BF16, CG, F32>;
+    auto kern = fc_act_kernel<BF16, CG, F32, CHUNKED>;
     cudaError_t e = ensure_dynamic_smem(kern, FA_SMEM, opt_in);
     if (e != cudaSuccess) return e;
     const int tiles = a.tiles_n * a.tiles_m;
@@ -728,7 +731,8 @@ static cudaError_t fa_launch_y(const FaArgs &a, const CUtensorMap &wmap, const C
 
 template <bool BF16, int CG>
 static cudaError_t fa_launch(const FaArgs &a, bool f32, const CUtensorMap &wmap, const CUtensorMap &xmap, cudaStream_t st) {
-    return f32 ? fa_launch_y<BF16, CG, true>(a, wmap, xmap, st) : fa_launch_y<BF16, CG, false>(a, wmap, xmap, st);
+    if (f32) return fa_launch_y<BF16, CG, true, true>(a, wmap, xmap, st);
+    return fa_long(a.K, BF16) ? fa_launch_y<BF16, CG, false, true>(a, wmap, xmap, st) : fa_launch_y<BF16, CG, false, false>(a, wmap, xmap, st);
 }
 
 }  // namespace scap
@@ -755,7 +759,7 @@ extern "C" scap_status scap_fc_act(const void *x, int64_t ldx, const void *W, co
     if (dev != SCAP_OK) return dev;
     cudaStream_t st = reinterpret_cast<cudaStream_t>(stream);
 
-    const FaPlan p = fa_plan(M, K, N, ydt == SCAP_F32, act);
+    const FaPlan p = fa_plan(M, K, N, ydt == SCAP_F32 || fa_long(K, dt == SCAP_BF16), act);
     FaArgs a = {};
     a.b = b; a.r = r; a.y = y; a.ldr = ldr; a.ldy = ldy;
     a.M = M; a.K = K; a.N = N; a.act = act;
