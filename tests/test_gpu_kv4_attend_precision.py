@@ -1,4 +1,5 @@
 """scap_kv4_attend where rows and tokens differ much in size, and where a sum is long: bounds that follow the products of a row, not its largest value."""
+import functools
 import math
 
 import pytest
@@ -128,6 +129,14 @@ def test_values_of_any_size(up):
     tight(c, q, out, lse, lens, 1, D ** -0.5)
 
 
+@functools.lru_cache(2)
+def long_values(n, heads, D):
+    """Keys and values of one sequence, and what a cache holds of them in 64 bits."""
+    gen = torch.Generator(device="cuda").manual_seed(5)
+    k, v = (torch.empty(n, heads, D, dtype=HF, device="cuda").normal_(generator=gen) for _ in range(2))
+    return k, v, side64(k, 64)[0], side64(v, 64)[0]
+
+
 @pytest.mark.gpu
 @pytest.mark.parametrize("B,heads,g,nq", [(120, 8, 1, 1), (1, 8, 1, 1), (40, 1, 4, 4), (60, 8, 1, 2)])  # a warp for an item; one item over the device; sixteen rows; a CTA for an item
 @pytest.mark.parametrize("scale,hole", [(0.0, 0), (0.125, 0), (0.125, 1800)])
@@ -137,8 +146,8 @@ def test_a_long_mean(B, heads, g, nq, scale, hole):
     import paper_2412_07174_b200 as scap
     D, page, n, dev = 64, 128, 400000, "cuda"
     width = -(-n // page)
-    gen = torch.Generator(device=dev).manual_seed(5)
-    k, v = (torch.empty(n, heads, D, dtype=HF, device=dev).normal_(generator=gen) for _ in range(2))
+    gen = torch.Generator(device=dev).manual_seed(6)
+    k, v, k64, v64 = long_values(n, heads, D)
     pool = torch.zeros(width, scap.scap_kv4_page_bytes(page, heads, D, 64), dtype=torch.uint8, device=dev)
     row = torch.randperm(width, generator=gen, device=dev).to(torch.int32)
     lens = torch.full((B,), n, dtype=torch.int32, device=dev)
@@ -153,7 +162,6 @@ def test_a_long_mean(B, heads, g, nq, scale, hole):
     scap.scap_kv4_attend(cache, q, out, scale, ws, lse=lse)
     torch.cuda.synchronize()
     scap.scap_device_status()
-    k64, v64 = side64(k, 64)[0], side64(v, 64)[0]
     for b in {0, B - 1}:
         for i in range(nq):
             seen = slice(hole * page, n - nq + i + 1)
@@ -167,3 +175,68 @@ def test_a_long_mean(B, heads, g, nq, scale, hole):
             # a score is off by at most 2 scale sum |q| |k| (D / 8 + 16) 2^-23 (codes and zero points apart, 15 scales each), a weight by 2^-17
             es = scale * 2 * q[b, i].double().abs().sum(-1).max() * k64.abs().max() * 2 * (D / 8 + 16) * 2.0 ** -23 + 2.0 ** -17
             assert bool(((lse[b, i].double().view(heads, g) - want_l).abs() <= es).all())
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("B,heads,n,nq,g", [(1, 32, 215000, 1, 2), (2, 16, 180000, 2, 8), (110, 8, 4200, 1, 2), (2, 2, 9000, 4, 4)])
+def test_no_tile_is_lost(B, heads, n, nq, g):
+    """The values of every page lie around a mean of its own, the keys too: a tile that is left out, read twice or taken for another shows in the root of mean
+    squares of all outputs, whatever the bounds of one of them."""
+    import paper_2412_07174_b200 as scap
+    D, page, dev = 64, 128, "cuda"
+    width = -(-n // page)
+    gen = torch.Generator(device=dev).manual_seed(n)
+    lens = torch.randint(n - 200, n + 1, (B,), generator=gen, device=dev).to(torch.int32)
+    table = torch.randperm(B * width, generator=gen, device=dev).to(torch.int32).view(B, width)
+    pool = torch.zeros(B * width, scap.scap_kv4_page_bytes(page, heads, D, 64), dtype=torch.uint8, device=dev)
+    cache = scap.ScapKv4(pool, page, heads, D, 64, table, lens)
+    at = starts(lens.tolist())
+    total = int(at[-1])
+    mean = torch.empty(2, total // 32 + 1, heads, D, dtype=BF, device=dev).normal_(generator=gen).repeat_interleave(32, 1)[:, :total]
+    k, v = ((m + torch.empty_like(m).normal_(generator=gen)).contiguous() for m in mean)
+    scap.scap_kv4_append(cache, k, v, at)
+    q = queries(B, nq, g * heads, D, BF)
+    out, lse = torch.empty_like(q), torch.empty(B, nq, g * heads, device=dev)
+    ws = torch.empty(scap.scap_kv4_attend_workspace(B, nq, g * heads, heads, D), dtype=torch.uint8, device=dev)
+    scap.scap_kv4_attend(cache, q, out, 0.125, ws, lse=lse)
+    torch.cuda.synchronize()
+    scap.scap_device_status()
+    for b in {0, B // 2, B - 1}:
+        rows, some = slice(int(at[b]), int(at[b + 1])), sorted({0, heads // 2, heads - 1})
+        k64, v64 = side64(k[rows][:, some], 64)[0], side64(v[rows][:, some], 64)[0]
+        for i in range(nq):
+            m = len(k64) - nq + i + 1
+            p = torch.softmax(0.125 * torch.einsum("hgd,nhd->hgn", q[b, i].view(heads, g, D)[some].double(), k64[:m]), -1)
+            want = torch.einsum("hgn,nhd->hgd", p, v64[:m])
+            off = (out[b, i].view(heads, g, D)[some].double() - want).square().mean().sqrt() / want.square().mean().sqrt()
+            # The rounding of a weight times its scale (2^-11 of it) and of the result (2^-8): 2^-7 of the outputs together.  One tile of 6700, with a 6700th of the weight,
+            # holds a value 1 / 82 of the outputs' size or more: of the tiles of a warp beyond the first 32 there are a tenth.
+            assert float(off) <= 2.0 ** -7, (b, i, float(off))
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("lens,heads,nq", [([200000], 8, 1), ([20000] * 20, 8, 1), ([2000] * 200, 8, 1)])
+def test_waits_that_run_out_are_reported(lens, heads, nq):
+    """One try of 4 us at most per wait, beside first copies that take longer (three tiles of 4352 bytes for each of 2368 warps, 31 MB: 4.7 us at the rate of the
+    memory): scap_device_status says so."""
+    import paper_2412_07174_b200 as scap
+    c = filled(lens, heads, 128, 128, seed=1)
+    q = queries(len(lens), nq, heads, 128, BF)
+    out = torch.empty_like(q)
+    ws = torch.empty(scap.scap_kv4_attend_workspace(len(lens), nq, heads, heads, 128), dtype=torch.uint8, device="cuda")
+    scap.scap_kv4_attend(c.cache, q, out, 0.1, ws)
+    want = out.clone()
+    flush = torch.zeros(1 << 28, dtype=torch.uint8, device="cuda")  # nothing of the cache in L2
+    torch.cuda.synchronize()
+    scap.scap_device_status()
+    scap.scap_tune("tc_spin", 1)
+    try:
+        scap.scap_kv4_attend(c.cache, q, out, 0.1, ws)
+        with pytest.raises(scap.ScapError) as e:
+            scap.scap_device_status()
+        assert e.value.code == 7
+    finally:
+        scap.scap_tune("tc_spin", 0)
+    scap.scap_kv4_attend(c.cache, q, out, 0.1, ws)
+    scap.scap_device_status()  # and is done with it
+    assert torch.equal(out, want) and flush is not None
