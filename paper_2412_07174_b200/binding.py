@@ -453,7 +453,7 @@ def scap_fc_act(x, W, b, y, ws, act: int = SCAP_ACT_NONE, res=None, stream=None)
 
 class ScapKv4(C.Structure):
     """The 4-bit cache of one layer (``scap_kv4``), made of the tensors that hold it.  ``pages`` [n_pages, bytes] uint8 may be a
-    view of wider pages (several layers side by side); ``table`` [n_seqs, pages of a sequence], ``lens`` [n_seqs] and ``refs`` [n_pages] are int32."""
+    view of wider pages (several layers side by side), but the calls that copy pages want the pool itself; ``table`` [n_seqs, pages of a sequence], ``lens`` [n_seqs] and ``refs`` [n_pages] are int32."""
     _fields_ = [("pages", C.c_void_p), ("page_stride", C.c_size_t), ("n_pages", C.c_int), ("page_tokens", C.c_int), ("heads", C.c_int),
                 ("head_dim", C.c_int), ("group", C.c_int), ("table_stride", C.c_int), ("n_seqs", C.c_int), ("table", C.c_void_p),
                 ("lens", C.c_void_p), ("refs", C.c_void_p)]
@@ -475,6 +475,8 @@ class ScapKv4(C.Structure):
         super().__init__(pages.data_ptr(), stride if n_pages > 1 else max(stride, width), n_pages, page_tokens, heads, head_dim, group, row, n_seqs, table.data_ptr(),
                          lens.data_ptr(), None if refs is None else refs.data_ptr())
         self.tensors = (pages, table, lens, refs)  # kept alive with the description
+        at, size = pages.storage_offset(), self.page_stride  # (bytes) whole pages: rows of the matrix that `pages` is, or is a slice of
+        self.whole = width == size or (at % size == 0 and at + n_pages * size <= pages.untyped_storage().nbytes())
         self.address = C.addressof(self)
         self.shape = (n_seqs, heads, head_dim)
 
@@ -550,13 +552,20 @@ def _numbers(name: str, *tensors) -> int:
     return n
 
 
+def _whole(cache) -> None:
+    if not cache.whole:
+        raise ValueError("pages move whole, all page_stride bytes: the cache must be described by the pool, not by a layer inside its pages")
+
+
 def scap_kv4_copy(cache, src, dst, stream=None) -> None:
     """Copies page src[i] to page dst[i]."""
+    _whole(cache)
     _invoke("scap_kv4_copy", cache.address, src, dst, _numbers("src and dst", src, dst), _stream(stream))
 
 
 def scap_kv4_fork(cache, src, dst, fail, ws, stream=None) -> None:
     """Row dst[i] becomes a copy of row src[i]: full pages shared, the last one copied.  fail [1] int32 or None: requests not carried out."""
+    _whole(cache)
     p, n = _ws(ws)
     _invoke("scap_kv4_fork", cache.address, src, dst, _numbers("src and dst", src, dst), fail, p, n, _stream(stream))
 
@@ -576,5 +585,6 @@ def scap_kv4_reserve(cache, add, fail, ws, stream=None) -> None:
 
 def scap_kv4_compact(cache, used, ws, stream=None) -> None:
     """Moves the used pages to the front of the pool; used [1] int32 or None: how many there are."""
+    _whole(cache)
     p, n = _ws(ws)
     _invoke("scap_kv4_compact", cache.address, used, p, n, _stream(stream))
