@@ -552,6 +552,13 @@ def _numbers(name: str, *tensors) -> int:
     return n
 
 
+def _count(t, name: str):
+    """Where a count goes: an int32 tensor of one element or more, an address or None."""
+    if isinstance(t, torch.Tensor) and (t.dtype is not torch.int32 or t.numel() < 1):
+        raise ValueError("%s must be int32 [1]" % name)
+    return t
+
+
 def _whole(cache) -> None:
     if not cache.whole:
         raise ValueError("pages move whole, all page_stride bytes: the cache must be described by the pool, not by a layer inside its pages")
@@ -567,7 +574,7 @@ def scap_kv4_fork(cache, src, dst, fail, ws, stream=None) -> None:
     """Row dst[i] becomes a copy of row src[i]: full pages shared, the last one copied.  fail [1] int32 or None: requests not carried out."""
     _whole(cache)
     p, n = _ws(ws)
-    _invoke("scap_kv4_fork", cache.address, src, dst, _numbers("src and dst", src, dst), fail, p, n, _stream(stream))
+    _invoke("scap_kv4_fork", cache.address, src, dst, _numbers("src and dst", src, dst), _count(fail, "fail"), p, n, _stream(stream))
 
 
 def scap_kv4_free(cache, rows, stream=None) -> None:
@@ -580,11 +587,11 @@ def scap_kv4_reserve(cache, add, fail, ws, stream=None) -> None:
     if _numbers("add", add) != cache.shape[0]:
         raise ValueError("add must be int32 [n_seqs]")
     p, n = _ws(ws)
-    _invoke("scap_kv4_reserve", cache.address, add, fail, p, n, _stream(stream))
+    _invoke("scap_kv4_reserve", cache.address, add, _count(fail, "fail"), p, n, _stream(stream))
 
 
 def scap_kv4_compact(cache, used, ws, stream=None) -> None:
     """Moves the used pages to the front of the pool; used [1] int32 or None: how many there are."""
     _whole(cache)
     p, n = _ws(ws)
-    _invoke("scap_kv4_compact", cache.address, used, p, n, _stream(stream))
+    _invoke("scap_kv4_compact", cache.address, _count(used, "used"), p, n, _stream(stream))

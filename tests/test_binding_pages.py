@@ -42,3 +42,17 @@ def test_pages_move_whole(seen):  # noqa: F811
     binding.scap_kv4_free(c, i32(2), stream=0)
     binding.scap_kv4_reserve(c, i32(3), None, torch.zeros(64, dtype=torch.uint8), stream=0)
     assert len(seen) == 2
+
+
+def test_counts_are_int32(seen):  # noqa: F811
+    c, i, ws = cache(torch.zeros(8, binding.scap_kv4_page_bytes(32, 2, 64, 32), dtype=torch.uint8)), i32(2), torch.zeros(64, dtype=torch.uint8)
+    calls = (lambda t: binding.scap_kv4_fork(c, i, i, t, ws, stream=0), lambda t: binding.scap_kv4_reserve(c, i32(3), t, ws, stream=0), lambda t: binding.scap_kv4_compact(c, t, ws, stream=0))
+    for f in calls:
+        for bad in (torch.zeros(1), torch.zeros(1, dtype=torch.int64), torch.zeros(1, dtype=torch.int16), i32(0)):
+            with pytest.raises(ValueError):
+                f(bad)
+    assert not seen
+    for f in calls:
+        for good in (None, i32(1), i32(()), i32(4), 0x10000):
+            f(good)
+    assert len(seen) == 15
