@@ -17,7 +17,7 @@
  *   y[B,N]      fp32
  *
  * General rules for every entry point
- *   - All data pointers are DEVICE pointers unless the parameter name ends in _host.
+ *   - All data pointers are DEVICE pointers, of the current device, unless the parameter name ends in _host.
  *   - The caller owns every buffer; the library allocates no device memory and keeps no state
  *     between calls except the process-wide tuning set by scap_tune().
  *   - Calls enqueue work on `stream` and return without synchronising; they perform no host
@@ -379,7 +379,8 @@ scap_status scap_moe_ffn(const void *h, const float *logits, const scap_expert *
  * A key / value cache in 4 bits, in pages
  *
  * What a decoding program needs beside the pruned projections: keys and values of the tokens so far, in the library's 4-bit
- * convention (codes 0..15, value s (q - zero)).  A group of `group` channels of one token and key head, values x, is stored as
+ * convention (codes 0..15, value s (q - zero)).  The pruned FCs return fp32 while keys, values and queries here have 16 bits, as the activations
+ * of every call: the program rounds the results of one to the inputs of the other, by a copy on the same stream.  A group of `group` channels of one token and key head, values x, is stored as
  *   lo = min(0, min x), hi = max(0, max x);  s = (hi - lo) / 15, rounded to 20 significant bits;  zero = round(-lo / s);
  *   q = min(15, max(0, round(x / s) + zero))                                              (ties to even; s = 0: all zeros)
  * decided exactly as in real numbers.  A group with an infinity or a NaN reads back as NaN.
@@ -450,7 +451,8 @@ scap_status scap_kv4_attend(const scap_kv4 *cache, const void *q, int64_t ldq, v
  *   free     the pages of the rows are let go (refs - 1), the rows are empty after it; a row that is named twice is freed once
  *   reserve  room for add[b] more tokens of every sequence b (add[n_seqs] int32): lens[b] += add[b], and free pages for them.  All of a
  *            sequence's pages or none: one that would have to take more than are left after those before it (carried out or not) stays
- *            as it is, and so does one whose row of the table is too short
+ *            as it is, and so does one whose row of the table is too short.  Its length says so: an append of its new tokens would write
+ *            over its last ones, so they are left out of row_start
  *   compact  the used pages move to the front of the pool: with U of them, the used ones at U and behind go, in order, into the free
  *            ones before U; table and refs follow.  used_out[1] (int32, may be NULL) receives U.  Only that many pages are copied      */
 size_t scap_kv4_pages_workspace(int n_pages, int n);
