@@ -470,6 +470,8 @@ class ScapKv4(C.Structure):
             raise ValueError("lens must be contiguous int32 [%d]" % n_seqs)
         if refs is not None and (refs.dtype is not torch.int32 or refs.shape != (n_pages,) or not refs.is_contiguous()):
             raise ValueError("refs must be contiguous int32 [%d]" % n_pages)
+        if any(t is not None and t.device != pages.device for t in (table, lens, refs)):
+            raise ValueError("pages, table, lens and refs must be on one device")
         if heads and width < scap_kv4_page_bytes(page_tokens, heads, head_dim, group):
             raise ValueError("a page needs %d bytes, has %d" % (scap_kv4_page_bytes(page_tokens, heads, head_dim, group), width))
         super().__init__(pages.data_ptr(), stride if n_pages > 1 else max(stride, width), n_pages, page_tokens, heads, head_dim, group, row, n_seqs, table.data_ptr(),

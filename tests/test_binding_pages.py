@@ -56,3 +56,13 @@ def test_counts_are_int32(seen):  # noqa: F811
         for good in (None, i32(1), i32(()), i32(4), 0x10000):
             f(good)
     assert len(seen) == 15
+
+
+def test_a_cache_lies_on_one_device():
+    pages = torch.zeros(8, binding.scap_kv4_page_bytes(32, 2, 64, 32), dtype=torch.uint8)
+    good = dict(pages=pages, table=i32(3, 4), lens=i32(3), refs=i32(8))
+    make = lambda pages, table, lens, refs: binding.ScapKv4(pages, 32, 2, 64, 32, table, lens, refs=refs)  # noqa: E731
+    make(**good)
+    for name in good:
+        with pytest.raises(ValueError):
+            make(**{**good, name: good[name].to("meta")})  # a device that is not the others'
