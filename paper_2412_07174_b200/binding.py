@@ -420,6 +420,22 @@ def scap_moe_ffn(h, logits, experts, top_k: int, y, ws, expert_out=None, weight_
                               _ptr(weight_out), p, n, _stream(stream)), "scap_moe_ffn")
 
 
+_getDevice, _getCurrentRawStream = getattr(torch._C, "_cuda_getDevice", None), getattr(torch._C, "_cuda_getCurrentRawStream", None)
+
+
+def _stream_on(device: int, stream, *tensors) -> int:
+    """The stream of a call whose tensors have to be on one device, the current one (device: the number of that, -1 for none): memory of another one, or of
+    the host, is out of a kernel's reach."""
+    for t in tensors:
+        if t is not None and t.get_device() != device:
+            raise ValueError("all tensors must be on one device")
+    if device < 0:
+        return _stream(stream)
+    if device != _getDevice():
+        raise ValueError("the tensors are on device %d, which is not the current one" % device)
+    return _getCurrentRawStream(device) if stream is None else _stream(stream)
+
+
 def _rows(t, rows: int, cols: int, name: str) -> int:
     """Row stride of a matrix [rows, cols] whose rows are contiguous, in elements."""
     ld, one = t.stride()
@@ -447,8 +463,9 @@ def scap_fc_act(x, W, b, y, ws, act: int = SCAP_ACT_NONE, res=None, stream=None)
         if res.dtype is not y.dtype or res.shape != (M, N):
             raise ValueError("res must have the shape and dtype of y")
         ldr = _rows(res, M, N, "res")
+    stream = _stream_on(x.get_device(), stream, W, b, y, ws, res)
     p, n = _ws(ws)
-    _invoke("scap_fc_act", x, _rows(x, M, K, "x"), W, b, int(act), res, ldr, y, _rows(y, M, N, "y"), M, K, N, dt, ydt, p, n, _stream(stream))
+    _invoke("scap_fc_act", x, _rows(x, M, K, "x"), W, b, int(act), res, ldr, y, _rows(y, M, N, "y"), M, K, N, dt, ydt, p, n, stream)
 
 
 class ScapKv4(C.Structure):
@@ -480,6 +497,7 @@ class ScapKv4(C.Structure):
         at, size = pages.storage_offset(), self.page_stride  # (bytes) whole pages: rows of the matrix that `pages` is, or is a slice of
         self.whole = width == size or (at % size == 0 and at + n_pages * size <= pages.untyped_storage().nbytes())
         self.address = C.addressof(self)
+        self.device = pages.get_device()
         self.shape = (n_seqs, heads, head_dim)
 
 
@@ -502,7 +520,8 @@ def _kv4_rows(name: str, cache, k, v, row_start, stream) -> None:
         raise ValueError("k and v must be [rows, %d, %d] of one dtype" % (heads, D))
     if row_start is not None and (row_start.dtype is not torch.int32 or row_start.numel() != n_seqs + 1 or not row_start.is_contiguous()):
         raise ValueError("row_start must be int32 [n_seqs + 1]")
-    _invoke(name, cache.address, k, _tokens(k, rows, heads, D, "k"), v, _tokens(v, rows, heads, D, "v"), row_start, rows, dtype_of(k), _stream(stream))
+    stream = _stream_on(cache.device, stream, k, v, row_start)
+    _invoke(name, cache.address, k, _tokens(k, rows, heads, D, "k"), v, _tokens(v, rows, heads, D, "v"), row_start, rows, dtype_of(k), stream)
 
 
 def scap_kv4_append(cache, k, v, row_start=None, stream=None) -> None:
@@ -536,9 +555,10 @@ def scap_kv4_attend(cache, q, out, scale: float, ws, window: int = 0, lse=None, 
         raise ValueError("q and out must be [%d, nq, q_heads, %d] of one dtype" % (n_seqs, D))
     if lse is not None and (lse.dtype is not torch.float32 or lse.shape != (B, nq, heads) or not lse.is_contiguous()):
         raise ValueError("lse must be contiguous float32 [n_seqs, nq, q_heads]")
+    stream = _stream_on(cache.device, stream, q, out, lse, ws)
     p, n = _ws(ws)
     _invoke_real("scap_kv4_attend", float(scale), 8, cache.address, q, _queries(q, B, nq, heads, D, "q"), out, _queries(out, B, nq, heads, D, "out"), lse, nq, heads, int(window),
-                 dtype_of(q), p, n, _stream(stream))
+                 dtype_of(q), p, n, stream)
 
 
 def scap_kv4_pages_workspace(n_pages: int, n: int) -> int:
@@ -554,10 +574,10 @@ def _numbers(name: str, *tensors) -> int:
     return n
 
 
-def _count(t, name: str):
+def _count(t, name: str, device: int):
     """Where a count goes: an int32 tensor of one element or more, an address or None."""
-    if isinstance(t, torch.Tensor) and (t.dtype is not torch.int32 or t.numel() < 1):
-        raise ValueError("%s must be int32 [1]" % name)
+    if isinstance(t, torch.Tensor) and (t.dtype is not torch.int32 or t.numel() < 1 or t.get_device() != device):
+        raise ValueError("%s must be int32 [1] on the device of the cache" % name)
     return t
 
 
@@ -569,31 +589,36 @@ def _whole(cache) -> None:
 def scap_kv4_copy(cache, src, dst, stream=None) -> None:
     """Copies page src[i] to page dst[i]."""
     _whole(cache)
-    _invoke("scap_kv4_copy", cache.address, src, dst, _numbers("src and dst", src, dst), _stream(stream))
+    stream = _stream_on(cache.device, stream, src, dst)
+    _invoke("scap_kv4_copy", cache.address, src, dst, _numbers("src and dst", src, dst), stream)
 
 
 def scap_kv4_fork(cache, src, dst, fail, ws, stream=None) -> None:
     """Row dst[i] becomes a copy of row src[i]: full pages shared, the last one copied.  fail [1] int32 or None: requests not carried out."""
     _whole(cache)
+    stream = _stream_on(cache.device, stream, src, dst, ws)
     p, n = _ws(ws)
-    _invoke("scap_kv4_fork", cache.address, src, dst, _numbers("src and dst", src, dst), _count(fail, "fail"), p, n, _stream(stream))
+    _invoke("scap_kv4_fork", cache.address, src, dst, _numbers("src and dst", src, dst), _count(fail, "fail", cache.device), p, n, stream)
 
 
 def scap_kv4_free(cache, rows, stream=None) -> None:
     """Lets go the pages of the rows; the rows are empty after it."""
-    _invoke("scap_kv4_free", cache.address, rows, _numbers("rows", rows), _stream(stream))
+    stream = _stream_on(cache.device, stream, rows)
+    _invoke("scap_kv4_free", cache.address, rows, _numbers("rows", rows), stream)
 
 
 def scap_kv4_reserve(cache, add, fail, ws, stream=None) -> None:
     """lens[b] += add[b], with free pages for the new tokens.  fail [1] int32 or None: sequences that did not get them."""
     if _numbers("add", add) != cache.shape[0]:
         raise ValueError("add must be int32 [n_seqs]")
+    stream = _stream_on(cache.device, stream, add, ws)
     p, n = _ws(ws)
-    _invoke("scap_kv4_reserve", cache.address, add, _count(fail, "fail"), p, n, _stream(stream))
+    _invoke("scap_kv4_reserve", cache.address, add, _count(fail, "fail", cache.device), p, n, stream)
 
 
 def scap_kv4_compact(cache, used, ws, stream=None) -> None:
     """Moves the used pages to the front of the pool; used [1] int32 or None: how many there are."""
     _whole(cache)
+    stream = _stream_on(cache.device, stream, ws)
     p, n = _ws(ws)
-    _invoke("scap_kv4_compact", cache.address, _count(used, "used"), p, n, _stream(stream))
+    _invoke("scap_kv4_compact", cache.address, _count(used, "used", cache.device), p, n, stream)

@@ -66,3 +66,50 @@ def test_a_cache_lies_on_one_device():
     for name in good:
         with pytest.raises(ValueError):
             make(**{**good, name: good[name].to("meta")})  # a device that is not the others'
+
+
+class Elsewhere(torch.Tensor):
+    def get_device(self):
+        return 3
+
+
+def other(t):
+    return t.as_subclass(Elsewhere)
+
+
+def test_tensors_lie_on_the_device_of_the_cache(seen):  # noqa: F811
+    """Memory of another device, or of the host, would be read and written by a kernel that cannot reach it."""
+    c, ws, i = cache(torch.zeros(8, binding.scap_kv4_page_bytes(32, 2, 64, 32), dtype=torch.uint8)), torch.zeros(64, dtype=torch.uint8), i32(2)
+    k, q = torch.zeros(5, 2, 64, dtype=torch.float16), torch.zeros(3, 1, 4, 64, dtype=torch.float16)
+    x, W, y, b = torch.zeros(5, 16, dtype=torch.float16), torch.zeros(16, 8, dtype=torch.float16), torch.zeros(5, 8), torch.zeros(8)
+    calls = [
+        (lambda k, v, st: binding.scap_kv4_append(c, k, v, st, stream=0), [k, k, i32(4)]),
+        (lambda k, v, st: binding.scap_kv4_read(c, k, v, st, stream=0), [k, k, i32(4)]),
+        (lambda q, o, lse, ws: binding.scap_kv4_attend(c, q, o, 0.5, ws, lse=lse, stream=0), [q, q, torch.zeros(3, 1, 4), ws]),
+        (lambda x, W, b, y, ws, r: binding.scap_fc_act(x, W, b, y, ws, res=r, stream=0), [x, W, b, y, ws, y]),
+        (lambda a, b: binding.scap_kv4_copy(c, a, b, stream=0), [i, i]),
+        (lambda a, b, f, ws: binding.scap_kv4_fork(c, a, b, f, ws, stream=0), [i, i, i32(1), ws]),
+        (lambda a: binding.scap_kv4_free(c, a, stream=0), [i]),
+        (lambda a, f, ws: binding.scap_kv4_reserve(c, a, f, ws, stream=0), [i32(3), i32(1), ws]),
+        (lambda f, ws: binding.scap_kv4_compact(c, f, ws, stream=0), [i32(1), ws]),
+    ]
+    for f, args in calls:
+        f(*args)
+        assert seen.pop() and not seen
+        for n in range(len(args)):
+            with pytest.raises(ValueError):
+                f(*[other(a) if m == n else a for m, a in enumerate(args)])
+    assert not seen
+
+
+def test_the_device_is_the_current_one(monkeypatch):
+    """A launch goes to the current device, so memory of another one is refused."""
+    class On0:
+        def get_device(self):
+            return 0
+    monkeypatch.setattr(binding, "_getDevice", lambda: 1)
+    with pytest.raises(ValueError):
+        binding._stream_on(0, 5, On0())
+    monkeypatch.setattr(binding, "_getDevice", lambda: 0)
+    monkeypatch.setattr(binding, "_getCurrentRawStream", lambda device: 70 + device)
+    assert binding._stream_on(0, 5, On0(), None) == 5 and binding._stream_on(0, None, On0()) == 70
