@@ -620,11 +620,14 @@ static int fa_stages(int cg, int BN) {
 // Clusters of S CTAs that the device holds at once, as the runtime reports it.  A CTA takes a whole SM, and the S of a cluster come from one group
 // of SMs, so the larger sizes leave SMs over: on 148, 74 clusters of 2, 33 of 4, 22 of 6 and 15 of 8.  One cluster more is a second turn of
 // them all: 18 of 8 took 18.7 us where 9 of them with twice the rows take 10.2 (28 rows, 8736 x 1048).
-static int fa_clusters(int S) {
-    static std::atomic<int> cached_by_dev[64][MAX_CLUSTER + 1];
-    if (S == 1) return sm_count();
+// The current device, -1 where there is none; asked for once per call (once per size it was 0.3 us of the host's time).
+static int fa_device() {
     int dev = 0;
     if (cudaGetDevice(&dev) != cudaSuccess) { cudaGetLastError(); dev = -1; }
+    return dev;
+}
+static int fa_clusters(int S, int dev) {
+    static std::atomic<int> cached_by_dev[64][MAX_CLUSTER + 1];
     if (dev >= 0 && dev < 64) {
         const int hit = cached_by_dev[dev][S].load(std::memory_order_relaxed);
         if (hit) return hit;
@@ -632,7 +635,7 @@ static int fa_clusters(int S) {
     int n = sm_count() / S;
     static SmemOptIn opt_in;
     auto kern = fc_act_kernel<true, 1, false, false>;
-    if (ensure_dynamic_smem(kern, FA_SMEM, opt_in) == cudaSuccess) {
+    if (S > 1 && ensure_dynamic_smem(kern, FA_SMEM, opt_in) == cudaSuccess) {
         cudaLaunchConfig_t cfg = {};
         cfg.gridDim = dim3(1, S);
         cfg.blockDim = dim3(FA_THREADS);
@@ -647,7 +650,7 @@ static int fa_clusters(int S) {
         int found = 0;
         if (cudaOccupancyMaxActiveClusters(&found, kern, &cfg) == cudaSuccess && found > 0) n = found;
         else cudaGetLastError();
-    } else {
+    } else if (S > 1) {
         cudaGetLastError();
     }
     if (dev >= 0 && dev < 64) cached_by_dev[dev][S].store(n, std::memory_order_relaxed);
@@ -658,14 +661,14 @@ static int fa_clusters(int S) {
 // bytes per cycle and SM, from L2), W at the rate of the memory, the epilogue of the last wave (18 cycles a row; more with a function to compute or
 // fp32 rows), and what a pair or the sum over ranks costs.  A sum reads
 // its peers four at a time, and clusters of 5 and 7 were never the best.  Over 70 drawn shapes with every form measured the choice is 4% off the best.
-static FaPlan fa_plan(int M, int K, int N, bool chunked, int act) {
+static FaPlan fa_plan(int M, int K, int N, bool chunked, int act, int dev) {
     const int nkb = (K + FA_BK - 1) / FA_BK;
     FaPlan best = {1, 16, 1, 0};
     const double floor = 0.45 * K * (double)N * 2 / 1000.0;  // W at the rate of the memory, in cycles
     const double row = (chunked ? 25.0 : 18.0) + (act > SCAP_ACT_RELU ? 10.0 : 0.0);
     double best_t = 1e300;
     int slots_of[MAX_CLUSTER + 1];
-    for (int S = 1; S <= MAX_CLUSTER; ++S) slots_of[S] = fa_clusters(S);
+    for (int S = 1; S <= MAX_CLUSTER; ++S) slots_of[S] = fa_clusters(S, dev);
     for (int cg = 1; cg <= 2; ++cg)
         for (int BN = 16 * cg; BN <= (chunked ? FA_MAX_BN_CHUNKED : 256); BN += 16 * cg) {
             if (BN >= M + 16 * cg) break;
@@ -701,7 +704,7 @@ static bool fa_map(CUtensorMap *map, const void *p, long long inner, long long o
 }
 
 template <bool BF16, int CG, bool F32, bool CHUNKED>
-static cudaError_t fa_launch_y(const FaArgs &a, const CUtensorMap &wmap, const CUtensorMap &xmap, cudaStream_t st) {
+static cudaError_t fa_launch_y(const FaArgs &a, int slots, const CUtensorMap &wmap, const CUtensorMap &xmap, cudaStream_t st) {
     static SmemOptIn opt_in;
     auto kern = fc_act_kernel<BF16, CG, F32, CHUNKED>;
     cudaError_t e = ensure_dynamic_smem(kern, FA_SMEM, opt_in);
@@ -709,10 +712,9 @@ static cudaError_t fa_launch_y(const FaArgs &a, const CUtensorMap &wmap, const C
     const int tiles = a.tiles_n * a.tiles_m;
     cudaLaunchConfig_t cfg = {};
     if (CG == 2) {
-        const int pairs = fa_clusters(2);
-        cfg.gridDim = dim3(2 * (tiles < pairs ? tiles : pairs));
+        cfg.gridDim = dim3(2 * (tiles < slots ? tiles : slots));
     } else {
-        cfg.gridDim = a.S > 1 ? dim3(tiles, a.S) : dim3(tiles < sm_count() ? tiles : sm_count());
+        cfg.gridDim = a.S > 1 ? dim3(tiles, a.S) : dim3(tiles < slots ? tiles : slots);
     }
     cfg.blockDim = dim3(FA_THREADS);
     cfg.dynamicSmemBytes = FA_SMEM;
@@ -730,9 +732,9 @@ static cudaError_t fa_launch_y(const FaArgs &a, const CUtensorMap &wmap, const C
 }
 
 template <bool BF16, int CG>
-static cudaError_t fa_launch(const FaArgs &a, bool f32, const CUtensorMap &wmap, const CUtensorMap &xmap, cudaStream_t st) {
-    if (f32) return fa_launch_y<BF16, CG, true, true>(a, wmap, xmap, st);
-    return fa_long(a.K, BF16) ? fa_launch_y<BF16, CG, false, true>(a, wmap, xmap, st) : fa_launch_y<BF16, CG, false, false>(a, wmap, xmap, st);
+static cudaError_t fa_launch(const FaArgs &a, int slots, bool f32, const CUtensorMap &wmap, const CUtensorMap &xmap, cudaStream_t st) {
+    if (f32) return fa_launch_y<BF16, CG, true, true>(a, slots, wmap, xmap, st);
+    return fa_long(a.K, BF16) ? fa_launch_y<BF16, CG, false, true>(a, slots, wmap, xmap, st) : fa_launch_y<BF16, CG, false, false>(a, slots, wmap, xmap, st);
 }
 
 }  // namespace scap
@@ -759,7 +761,9 @@ extern "C" scap_status scap_fc_act(const void *x, int64_t ldx, const void *W, co
     if (dev != SCAP_OK) return dev;
     cudaStream_t st = reinterpret_cast<cudaStream_t>(stream);
 
-    const FaPlan p = fa_plan(M, K, N, ydt == SCAP_F32 || fa_long(K, dt == SCAP_BF16), act);
+    const int device = fa_device();
+    const FaPlan p = fa_plan(M, K, N, ydt == SCAP_F32 || fa_long(K, dt == SCAP_BF16), act, device);
+    const int slots = fa_clusters(p.cg == 2 ? 2 : 1, device);  // tiles that run at once, where S is 1
     FaArgs a = {};
     a.b = b; a.r = r; a.y = y; a.ldr = ldr; a.ldy = ldy;
     a.M = M; a.K = K; a.N = N; a.act = act;
@@ -789,7 +793,7 @@ extern "C" scap_status scap_fc_act(const void *x, int64_t ldx, const void *W, co
     }
     const bool f32 = ydt == SCAP_F32;
     cudaError_t e;
-    if (bf16) e = p.cg == 2 ? fa_launch<true, 2>(a, f32, wmap, xmap, st) : fa_launch<true, 1>(a, f32, wmap, xmap, st);
-    else e = p.cg == 2 ? fa_launch<false, 2>(a, f32, wmap, xmap, st) : fa_launch<false, 1>(a, f32, wmap, xmap, st);
+    if (bf16) e = p.cg == 2 ? fa_launch<true, 2>(a, slots, f32, wmap, xmap, st) : fa_launch<true, 1>(a, slots, f32, wmap, xmap, st);
+    else e = p.cg == 2 ? fa_launch<false, 2>(a, slots, f32, wmap, xmap, st) : fa_launch<false, 1>(a, slots, f32, wmap, xmap, st);
     return cuda_status(e);
 }
