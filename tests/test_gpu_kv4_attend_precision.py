@@ -130,11 +130,11 @@ def test_values_of_any_size(up):
 
 
 @functools.lru_cache(2)
-def long_values(n, heads, D):
+def long_values(n, heads, D, group):
     """Keys and values of one sequence, and what a cache holds of them in 64 bits."""
     gen = torch.Generator(device="cuda").manual_seed(5)
     k, v = (torch.empty(n, heads, D, dtype=HF, device="cuda").normal_(generator=gen) for _ in range(2))
-    return k, v, side64(k, 64)[0], side64(v, 64)[0]
+    return k, v, side64(k, group)[0], side64(v, group)[0]
 
 
 @pytest.mark.gpu
@@ -143,18 +143,28 @@ def long_values(n, heads, D):
 def test_a_long_mean(B, heads, g, nq, scale, hole):
     """Means of up to 400000 values, 1 / 630 of their size, as many as 4000 tiles of them in one warp; where there is a hole the first pages are missing.  The
     sequences share their pages."""
+    long_mean(B, heads, g, nq, scale, hole, 64, 64, 400000)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("D,group,B,g,nq,n", [(128, 32, 120, 2, 1, 60000), (256, 64, 80, 1, 2, 40000), (128, 128, 30, 4, 4, 100000), (256, 128, 20, 16, 1, 70000)])
+def test_a_long_mean_of_other_shapes(D, group, B, g, nq, n):
+    long_mean(B, 8, g, nq, 0.05, 0, D, group, n)
+
+
+def long_mean(B, heads, g, nq, scale, hole, D, group, n):
     import paper_2412_07174_b200 as scap
-    D, page, n, dev = 64, 128, 400000, "cuda"
+    page, dev = 128, "cuda"
     width = -(-n // page)
     gen = torch.Generator(device=dev).manual_seed(6)
-    k, v, k64, v64 = long_values(n, heads, D)
-    pool = torch.zeros(width, scap.scap_kv4_page_bytes(page, heads, D, 64), dtype=torch.uint8, device=dev)
+    k, v, k64, v64 = long_values(n, heads, D, group)
+    pool = torch.zeros(width, scap.scap_kv4_page_bytes(page, heads, D, group), dtype=torch.uint8, device=dev)
     row = torch.randperm(width, generator=gen, device=dev).to(torch.int32)
     lens = torch.full((B,), n, dtype=torch.int32, device=dev)
-    one = scap.ScapKv4(pool, page, heads, D, 64, row[None].contiguous(), lens[:1])
+    one = scap.ScapKv4(pool, page, heads, D, group, row[None].contiguous(), lens[:1])
     scap.scap_kv4_append(one, k, v, torch.tensor([0, n], dtype=torch.int32, device=dev))
     row[:hole] = -1
-    cache = scap.ScapKv4(pool, page, heads, D, 64, row.expand(B, width).contiguous(), lens)
+    cache = scap.ScapKv4(pool, page, heads, D, group, row.expand(B, width).contiguous(), lens)
     q = queries(B, nq, g * heads, D, HF)
     out = torch.empty_like(q)
     lse = torch.empty(B, nq, g * heads, device=dev)
@@ -240,3 +250,22 @@ def test_waits_that_run_out_are_reported(lens, heads, nq):
     scap.scap_kv4_attend(c.cache, q, out, 0.1, ws)
     scap.scap_device_status()  # and is done with it
     assert torch.equal(out, want) and flush is not None
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("every", [700, 20])  # in one tile, in all of them
+def test_a_group_that_is_not_finite_stays_in_its_channels(every):
+    """Values of one group of channels that are NaN make those channels NaN; the other groups of the same tokens count, in size too."""
+    lens, D, group = [40, 300, 2500], 128, 32
+    c, q = spiked(lens, D, group, 0.5, 0.2, 2.0 ** 12)
+    k, v = c.kv
+    v[7::every, 0, 40] = float("nan")
+    c.scap.scap_kv4_append(c.cache, k, v, starts(lens))
+    out, lse = attend(c, q, D ** -0.5)
+    assert bool(out[..., 32:64].isnan().all()) if every == 20 else bool(out[0, ..., 32:64].isnan().all())
+    v[7::every, 0, 32:64] = 0.0
+    c.scap.scap_kv4_append(c.cache, k, v, starts(lens))
+    zero, lse0 = attend(c, q, D ** -0.5)
+    tight(c, q, zero, lse0, lens, 1, D ** -0.5)
+    assert bool(torch.isfinite(out[..., :32]).all()) and bool(torch.isfinite(out[..., 64:]).all())
+    tight(c, q, torch.cat((out[..., :32], zero[..., 32:64], out[..., 64:]), -1), lse, lens, 1, D ** -0.5)
