@@ -91,14 +91,17 @@ __device__ __forceinline__ int at_tiles_of(const AtArgs &a, int len, int &first)
 
 __device__ __forceinline__ long long at_cut(long long units, int i, int workers) { return units * i / workers; }
 // CTAs that share the units, and workers in them: the CTA, or (SOLO) each of its warps.  Where there is much to do there are twice as many CTAs as
-// the device holds: the SMs favour the older ones of their CTAs, and the younger ones of a second wave take over from those (83 units
-// per resident CTA: 75 -> 71 us; 55 units: 42 -> 52).
-constexpr int AT_TWO_WAVES = 64;
+// the device holds: the SMs favour the older ones of their CTAs, and the younger ones of a second wave take over from those.  It helps where CTAs end items
+// of their own (us with one wave and two, 128 channels, 80 units per resident CTA; 70 sequences: 85 and 80, 32: 74 and 72, 16: 68 and 67) and costs the time of the
+// more and shorter parts where few items are cut into many (8: 59 and 65, one: 58 and 67), so it takes half as many items as there are resident CTAs.  With
+// less to do it varies (20 to 60 units, 48 and 70 sequences: from 12 better to 9 worse).
+constexpr int AT_TWO_WAVES = 64;  // units per resident CTA
+__host__ __device__ constexpr bool at_two_waves(long long units, long long items, int resident) { return units >= (long long)AT_TWO_WAVES * resident && 2 * items >= resident; }
 template <bool SOLO>
 __device__ __forceinline__ int at_workers(const AtArgs &a, long long units, long long items, int &ctas) {
     constexpr int PER = SOLO ? AT_WARPS : 1;
     const long long n = max((units + AT_MIN_UNITS - 1) / AT_MIN_UNITS, items);
-    const int most = units >= (long long)AT_TWO_WAVES * a.resident ? a.waves * a.resident : a.resident;
+    const int most = at_two_waves(units, items, a.resident) ? a.waves * a.resident : a.resident;
     const int workers = n < (long long)PER * most ? (int)n : PER * most;
     ctas = min(most, workers);  // (SOLO: worker w is warp w / ctas of CTA w % ctas, so that few of them lie in different CTAs)
     return workers;
@@ -986,7 +989,7 @@ extern "C" scap_status scap_kv4_attend(const scap_kv4 *cache, const void *q, int
     a.tile_cap = (int)(cap < (1ll << 30) ? cap : (1ll << 30));
     const long long items = (long long)cache->n_seqs * cache->heads * a.row_tiles, units = (cap < seen ? cap : seen) * items;
     const long long few = (units + AT_MIN_UNITS - 1) / AT_MIN_UNITS > items ? (units + AT_MIN_UNITS - 1) / AT_MIN_UNITS : items;
-    const int most = units >= (long long)AT_TWO_WAVES * a.resident ? a.waves * a.resident : a.resident;
+    const int most = at_two_waves(units, items, a.resident) ? a.waves * a.resident : a.resident;  // (both at least what the kernel counts)
     const int grid = few < most ? (int)few : most;
     a.ml = a.part + 2 * p.workers() * 8 * p.rn * cache->head_dim;
     a.where = reinterpret_cast<int2 *>(a.ml + 2 * p.workers() * 8 * p.rn * 2);
