@@ -565,60 +565,61 @@ def scap_kv4_pages_workspace(n_pages: int, n: int) -> int:
     return lib().scap_kv4_pages_workspace(int(n_pages), int(n))
 
 
-def _numbers(name: str, *tensors) -> int:
+def _numbers(name: str, device: int, *tensors) -> int:
     """Length that the int32 tensors share."""
     n = tensors[0].numel()
     for t in tensors:
-        if t.dtype is not torch.int32 or t.numel() != n or not t.is_contiguous():
-            raise ValueError("%s must be contiguous int32 tensors of one length" % name)
+        if t.dtype is not torch.int32 or t.numel() != n or not t.is_contiguous() or t.get_device() != device:
+            raise ValueError("%s must be contiguous int32 tensors of one length on the device of the cache" % name)
     return n
 
 
 def _count(t, name: str, device: int):
     """Where a count goes: an int32 tensor of one element or more, an address or None."""
-    if isinstance(t, torch.Tensor) and (t.dtype is not torch.int32 or t.numel() < 1 or t.get_device() != device):
+    if t is not None and type(t) is not int and (t.dtype is not torch.int32 or t.get_device() != device or t.numel() < 1):
         raise ValueError("%s must be int32 [1] on the device of the cache" % name)
     return t
 
 
-def _whole(cache) -> None:
-    if not cache.whole:
-        raise ValueError("pages move whole, all page_stride bytes: the cache must be described by the pool, not by a layer inside its pages")
+_WHOLE = "pages move whole, all page_stride bytes: the cache must be described by the pool, not by a layer inside its pages"
 
 
 def scap_kv4_copy(cache, src, dst, stream=None) -> None:
     """Copies page src[i] to page dst[i]."""
-    _whole(cache)
-    stream = _stream_on(cache.device, stream, src, dst)
-    _invoke("scap_kv4_copy", cache.address, src, dst, _numbers("src and dst", src, dst), stream)
+    if not cache.whole:
+        raise ValueError(_WHOLE)
+    device = cache.device
+    _invoke("scap_kv4_copy", cache.address, src, dst, _numbers("src and dst", device, src, dst), _stream_on(device, stream))
 
 
 def scap_kv4_fork(cache, src, dst, fail, ws, stream=None) -> None:
     """Row dst[i] becomes a copy of row src[i]: full pages shared, the last one copied.  fail [1] int32 or None: requests not carried out."""
-    _whole(cache)
-    stream = _stream_on(cache.device, stream, src, dst, ws)
+    if not cache.whole:
+        raise ValueError(_WHOLE)
+    device = cache.device
     p, n = _ws(ws)
-    _invoke("scap_kv4_fork", cache.address, src, dst, _numbers("src and dst", src, dst), _count(fail, "fail", cache.device), p, n, stream)
+    _invoke("scap_kv4_fork", cache.address, src, dst, _numbers("src and dst", device, src, dst), _count(fail, "fail", device), p, n, _stream_on(device, stream, ws))
 
 
 def scap_kv4_free(cache, rows, stream=None) -> None:
     """Lets go the pages of the rows; the rows are empty after it."""
-    stream = _stream_on(cache.device, stream, rows)
-    _invoke("scap_kv4_free", cache.address, rows, _numbers("rows", rows), stream)
+    device = cache.device
+    _invoke("scap_kv4_free", cache.address, rows, _numbers("rows", device, rows), _stream_on(device, stream))
 
 
 def scap_kv4_reserve(cache, add, fail, ws, stream=None) -> None:
     """lens[b] += add[b], with free pages for the new tokens.  fail [1] int32 or None: sequences that did not get them."""
-    if _numbers("add", add) != cache.shape[0]:
+    device = cache.device
+    if _numbers("add", device, add) != cache.shape[0]:
         raise ValueError("add must be int32 [n_seqs]")
-    stream = _stream_on(cache.device, stream, add, ws)
     p, n = _ws(ws)
-    _invoke("scap_kv4_reserve", cache.address, add, _count(fail, "fail", cache.device), p, n, stream)
+    _invoke("scap_kv4_reserve", cache.address, add, _count(fail, "fail", device), p, n, _stream_on(device, stream, ws))
 
 
 def scap_kv4_compact(cache, used, ws, stream=None) -> None:
     """Moves the used pages to the front of the pool; used [1] int32 or None: how many there are."""
-    _whole(cache)
-    stream = _stream_on(cache.device, stream, ws)
+    if not cache.whole:
+        raise ValueError(_WHOLE)
+    device = cache.device
     p, n = _ws(ws)
-    _invoke("scap_kv4_compact", cache.address, _count(used, "used", cache.device), p, n, stream)
+    _invoke("scap_kv4_compact", cache.address, _count(used, "used", device), p, n, _stream_on(device, stream, ws))
