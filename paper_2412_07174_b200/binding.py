@@ -487,17 +487,19 @@ class ScapKv4(C.Structure):
             raise ValueError("lens must be contiguous int32 [%d]" % n_seqs)
         if refs is not None and (refs.dtype is not torch.int32 or refs.shape != (n_pages,) or not refs.is_contiguous()):
             raise ValueError("refs must be contiguous int32 [%d]" % n_pages)
-        if any(t is not None and t.device != pages.device for t in (table, lens, refs)):
+        device = pages.get_device()
+        if table.get_device() != device or lens.get_device() != device or (refs is not None and refs.get_device() != device):
             raise ValueError("pages, table, lens and refs must be on one device")
         if heads and width < scap_kv4_page_bytes(page_tokens, heads, head_dim, group):
             raise ValueError("a page needs %d bytes, has %d" % (scap_kv4_page_bytes(page_tokens, heads, head_dim, group), width))
         super().__init__(pages.data_ptr(), stride if n_pages > 1 else max(stride, width), n_pages, page_tokens, heads, head_dim, group, row, n_seqs, table.data_ptr(),
                          lens.data_ptr(), None if refs is None else refs.data_ptr())
         self.tensors = (pages, table, lens, refs)  # kept alive with the description
-        at, size = pages.storage_offset(), self.page_stride  # (bytes) whole pages: rows of the matrix that `pages` is, or is a slice of
-        self.whole = width == size or (at % size == 0 and at + n_pages * size <= pages.untyped_storage().nbytes())
+        # whole pages (bytes): rows of the matrix that `pages` is, or is a slice of
+        self.whole = width == self.page_stride or (pages.storage_offset() % self.page_stride == 0 and
+                                         pages.storage_offset() + n_pages * self.page_stride <= pages.untyped_storage().nbytes())
         self.address = C.addressof(self)
-        self.device = pages.get_device()
+        self.device = device
         self.shape = (n_seqs, heads, head_dim)
 
 

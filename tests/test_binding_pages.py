@@ -65,7 +65,7 @@ def test_a_cache_lies_on_one_device():
     make(**good)
     for name in good:
         with pytest.raises(ValueError):
-            make(**{**good, name: good[name].to("meta")})  # a device that is not the others'
+            make(**{**good, name: other(good[name])})
 
 
 class Elsewhere(torch.Tensor):
