@@ -215,7 +215,7 @@ scap_status scap_dense_fc(const void *x, const void *W, const float *b, float *y
  *   r[M,N]  residual, NULL for none; y[M,N]; both of dtype ydt (dt or SCAP_F32), rows ldr / ldy >= N elements apart.  r may be
  *           y itself (with the same stride); x may not overlap y
  *   act     u: none; relu: max(u, 0); silu: u / (1 + e^-u); gelu: u/2 (1 + erf(u / sqrt 2)); gelu_tanh: u/2 (1 + tanh(sqrt(2/pi) (u +
- *           0.044715 u^3)))
+ *           0.044715 u^3))); off by at most (4 z + 16) 2^-24 of itself, z being |u|, u^2 / 2 and 1.6 (|u| + 0.045 |u|^3)
  * An accumulator of the tensor cores, which truncate as they add, takes 512 channels where y is fp32 or K above 16384 (fp16 results) or 131072 (bf16 ones); their
  * sums are added up in fp32, rounded to nearest.  Below that what the truncation takes off is under an eighth of half a step of y.
  * A NaN or an infinity in x makes its row non-finite before act, one in W its column; a NaN stays one.  Rows and columns beyond M and N are left as they were.

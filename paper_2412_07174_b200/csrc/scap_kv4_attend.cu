@@ -10,10 +10,11 @@
 // (With the rows as the M rows of the MMA a head with eight or fewer of them pays for sixteen: twice the MMAs, accumulators and
 // exponentials; 131001 tokens, 8 key heads, 8 rows: 57 us against 45 at that time.)
 //
-// What bounds it: the instructions.  The bytes of the cache are D/2 + 4 groups per token, head and side; per tile of 32 tokens (D = 128,
-// RN = 1, one group) a warp issues 36 MMAs, 160 mask and shift instructions - five for eight codes, and the pipe that runs them takes two cycles
-// each - and about 150 others.  48 sequences of together 196608 tokens, 8 key heads, groups of 64: 67 us at 228 MB = 3.4 TB/s, issue slots
-// 56 % busy, the mask pipe 47 %, tensor pipe 22 %, DRAM 43 %; 131001 tokens of one sequence, groups of 128: 38 us at 143 MB = 3.7 TB/s.  With
+// What bounds it: latency inside a warp, with four warps per scheduler to cover it; no unit is saturated.  The bytes of the cache are D/2 + 4 groups per token, head
+// and side; per tile of 32 tokens (D = 128, RN = 1, one group) a warp issues about 565 instructions, 36 of them MMAs and 160 masks and shifts - five for eight codes, and the
+// pipe that runs them takes two cycles each.  48 sequences of together 196608 tokens, 8 key heads, groups of 64: 69 us at 228 MB = 3.3 TB/s, issue slots
+// 57 % busy with 1.1 of 3.6 warps ready, the mask pipe 46 %, tensor pipe 21 %, DRAM 42 %; of 6.3 cycles between two instructions of a warp 1.7 go to results of fixed latency,
+// 1.0 to other warps, 0.8 to the mask pipe, 0.4 to memory.  131001 tokens of one sequence, groups of 128: 39 us at 143 MB = 3.7 TB/s.  With
 // the copies alone, no arithmetic, these took 48 and 33 us: 4 to 6 us until the first tiles of all warps have come, then 5.7 TB/s.
 //
 // Work is cut into equal parts, whatever the lengths: a unit is one tile of 32 tokens of one (sequence, 8 RN rows, head), all units are
