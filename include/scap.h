@@ -429,9 +429,10 @@ scap_status scap_kv4_read(const scap_kv4 *cache, void *k, int64_t ldk, void *v, 
  * q_heads a multiple of cache->heads up to 1024, query head h reads key head h / (q_heads / heads).  lse[n_seqs, nq, q_heads] fp32 or
  * NULL: log of the sum of the exp(...), for joining with attention over tokens that are not in the cache.  A row that sees nothing (an
  * empty sequence, or nq > lens[b]) gives 0 and -inf.  A NaN or an infinity in a query, or in a key or value that it sees, makes
- * its row non-finite (a value: the channels of its group in that row), no other one.  Scores, sums and accumulators are fp32; a weight times the scale of its value is rounded to
- * fp16 once (11 bits): off by 2^-11 of itself at most down to 2^-20 of the largest such product of the row, and by 2^-31 of that one below; scales
- * under 2^-56 count as 2^-56 in this.  Queries are exact down to 2^-21 of the largest channel of their row, and off by at most 2^-32 of it below.
+ * its row non-finite (a value: the channels of its group in that row), no other one.  Scores and sums are fp32, as the tensor core keeps them: of 16
+ * products that it adds at a time each loses at most 2^-16 of the largest product of a weight and a scale, or of a channel of the query
+ * and the scale of a key.  A weight times the scale of its value is rounded to fp16 once (11 bits): off by 2^-11 of itself at most down to
+ * 2^-20 of the largest such product of the row, and by 2^-31 of that one below; scales under 2^-56 count as 2^-56 in this.  Queries are exact down to 2^-21 of the largest channel of their row, and off by at most 2^-32 of it below.
  * A row does not depend, to the bit, on what the others hold.
  * Bitwise reproducible on one device.  Workspace: scap_kv4_attend_workspace() bytes.                                             */
 size_t scap_kv4_attend_workspace(int n_seqs, int nq, int q_heads, int heads, int head_dim);

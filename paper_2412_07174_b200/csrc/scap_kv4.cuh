@@ -14,8 +14,8 @@
 //      D/32 consecutive words of token g.
 //   V  word ((nt / 4) 32 + 4 g + t) 4 + nt % 4 holds the eight tokens 8 j + 2 t + o of channel 8 nt + g, in nibble j + 4 o (j = 0..3,
 //      o = 0, 1): lane (g, t) reads four consecutive words, for four blocks of eight channels.
-// In both, the nibbles i and i + 4 of a word are the two halves of one operand register: (w >> 8 h) & 0x000f000f and & 0x00f000f0
-// are pairs of fp16 subnormals, code 2^-24 and code 2^-20, which the tensor core multiplies exactly.  No code is converted.
+// In both, the nibbles i and i + 4 of a word are the two halves of one operand register: w << 2 and w >> 6 under the masks 0x003c003c and 0x03c003c0
+// are pairs of fp16 subnormals, code 2^-22 and code 2^-18, which the tensor core multiplies exactly.  No code is converted.
 #pragma once
 
 #include "scap_common.cuh"

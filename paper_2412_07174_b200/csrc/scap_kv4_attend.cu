@@ -11,10 +11,10 @@
 // exponentials; 131001 tokens, 8 key heads, 8 rows: 57 us against 45 at that time.)
 //
 // What bounds it: latency inside a warp, with four warps per scheduler to cover it; no unit is saturated.  The bytes of the cache are D/2 + 4 groups per token, head
-// and side; per tile of 32 tokens (D = 128, RN = 1, one group) a warp issues about 565 instructions, 36 of them MMAs and 160 masks and shifts - five for eight codes, and the
-// pipe that runs them takes two cycles each.  48 sequences of together 196608 tokens, 8 key heads, groups of 64: 69 us at 228 MB = 3.3 TB/s, issue slots
-// 57 % busy with 1.1 of 3.6 warps ready, the mask pipe 46 %, tensor pipe 21 %, DRAM 42 %; of 6.3 cycles between two instructions of a warp 1.7 go to results of fixed latency,
-// 1.0 to other warps, 0.8 to the mask pipe, 0.4 to memory.  131001 tokens of one sequence, groups of 128: 39 us at 143 MB = 3.7 TB/s.  With
+// and side; per tile of 32 tokens (D = 128, RN = 1, one group) a warp issues about 600 instructions, 36 of them MMAs and 192 masks and shifts - six for eight codes, and the
+// pipe that runs them takes two cycles each.  48 sequences of together 196608 tokens, 8 key heads, groups of 64: 73 us at 228 MB = 3.1 TB/s, issue slots
+// 57 % busy with 1.1 of 3.6 warps ready, the mask pipe 45 %, tensor pipe 20 %, DRAM 40 %; of 6.3 cycles between two instructions of a warp 1.5 go to results of fixed latency,
+// 1.0 to other warps, 0.7 to the mask pipe, 0.6 to memory.  131001 tokens of one sequence, groups of 128: 40 us at 143 MB = 3.6 TB/s.  With
 // the copies alone, no arithmetic, these took 48 and 33 us: 4 to 6 us until the first tiles of all warps have come, then 5.7 TB/s.
 //
 // Work is cut into equal parts, whatever the lengths: a unit is one tile of 32 tokens of one (sequence, 8 RN rows, head), all units are
@@ -247,6 +247,12 @@ __device__ __forceinline__ float at_pow2(int e) { return __int_as_float((e + 127
 
 // Adds the sums of the stretches before to those that a warp has put into shared memory, for the rows own, own + STEP, ... that this warp puts out (and put
 // where parts go, a channel the same lane).  Out of line: in line it costs the loop over tiles registers (four new tokens of 32 key heads: 80 -> 82 us).
+// The codes of a word as pairs of subnormal numbers.  Of the products that it adds at a time the tensor core drops what lies below 2^-24 of the largest exponent, and a subnormal
+// number counts with 2^-14 there, so codes lie as high as one shift for each half of a word puts them: 2^-22 and 2^-18.  (At 2^-24 and 2^-20, without the first shift,
+// sums lose four times as much: 15 others added with a token of nine tenths of the weight were off by 2^-13 of its scale together; 72.6 -> 75.9 us for 48 sequences of 196608 tokens.)
+constexpr uint32_t AT_LOW = 0x003c003cu, AT_HIGH = 0x03c003c0u;
+__device__ __forceinline__ uint32_t at_place(uint32_t w, int second) { return second ? w >> 6 : w << 2; }
+
 template <int D, int STEP, int PITCH>
 __device__ __noinline__ void at_fold(int own, int rows, int lane, float *part, float *s_m, float *s_l, const float *sums, const float *ml) {
     __syncwarp();
@@ -383,7 +389,7 @@ __global__ void __launch_bounds__(AT_THREADS, at_resident(D, G, RN)) kv4_attend_
         // row does not depend on those it is taken with); channels 32 j + 8 qt + i, the
         // even and odd nibbles of a code word in the two k halves of an MMA, the odd ones 16 times smaller as their codes are larger: a channel is exact
         // down to 2^-21 of the largest of its row, and off by 2^-32 of that below.
-        // zq: minus the sum of a group, in two fp16 parts, against the zero points (times 2^6, as zero 2^-18 is the subnormal used)
+        // zq: minus the sum of a group, in two fp16 parts, against the zero points (times 2^4, as zero 2^-18 is the subnormal used and code 2^-22 the other)
         uint32_t qb[QS ? 1 : 2 * W][2], zq[QS ? 1 : G];
         if (!QS || warp < RN) {  // (in shared memory: warp rn for its eight rows)
             const int rn = QS ? warp : 0, row = 8 * rn + qg;
@@ -426,11 +432,11 @@ __global__ void __launch_bounds__(AT_THREADS, at_resident(D, G, RN)) kv4_attend_
             for (int n = 0; n < G; ++n) {
                 sum[n] += __shfl_xor_sync(0xffffffffu, sum[n], 1);
                 sum[n] += __shfl_xor_sync(0xffffffffu, sum[n], 2);
-                const float x = -sum[n] * 0.015625f, x_hi = __half2float(__float2half_rn(x));
+                const float x = -sum[n] * 0.0625f, x_hi = __half2float(__float2half_rn(x));
                 if constexpr (QS) s_zq[rn][n][lane] = at_pack(x_hi, x - x_hi);
                 else zq[n] = at_pack(x_hi, x - x_hi);
             }
-            const float back = a.scale * at_pow2((24 - e) / 2) * at_pow2(24 - e - (24 - e) / 2);
+            const float back = a.scale * at_pow2((22 - e) / 2) * at_pow2(22 - e - (22 - e) / 2);
             if (qt == 0) s_f[warp][qg] = back;
             __syncwarp();
         }
@@ -537,8 +543,8 @@ __global__ void __launch_bounds__(AT_THREADS, at_resident(D, G, RN)) kv4_attend_
                         for (int hi8 = 0; hi8 < 2; ++hi8)
 #pragma unroll
                             for (int mt = 0; mt < MB; ++mt) {
-                                const uint32_t x = w[2 * mt][k] >> (8 * hi8), y = w[2 * mt + 1][k] >> (8 * hi8);
-                                const uint32_t a0 = x & 0x000f000fu, a1 = y & 0x000f000fu, a2 = x & 0x00f000f0u, a3 = y & 0x00f000f0u;
+                                const uint32_t x = at_place(w[2 * mt][k], hi8), y = at_place(w[2 * mt + 1][k], hi8);
+                                const uint32_t a0 = x & AT_LOW, a1 = y & AT_LOW, a2 = x & AT_HIGH, a3 = y & AT_HIGH;
 #pragma unroll
                                 for (int rn = 0; rn < RN; ++rn) at_mma(acc[mt][rn][k * G / W], a0, a1, a2, a3, q[rn][hi8][0], q[rn][hi8][1]);
                             }
@@ -690,7 +696,7 @@ __global__ void __launch_bounds__(AT_THREADS, at_resident(D, G, RN)) kv4_attend_
                     *reinterpret_cast<uint4 *>(w1) = *reinterpret_cast<const uint4 *>(tile + kv_v_words(D, G) + (n * KV_TILE + 8 * qt + 4) * 4);
 #pragma unroll
                     for (int ks = 0; ks < 2; ++ks) {
-                        const uint32_t z0 = __byte_perm(w0[2 * ks], w1[2 * ks], 0x5410) & 0x000f000fu, z1 = (__byte_perm(w0[2 * ks + 1], w1[2 * ks + 1], 0x5410) & 0x000f000fu) << 4;
+                        const uint32_t z0 = (__byte_perm(w0[2 * ks], w1[2 * ks], 0x5410) & 0x000f000fu) << 2, z1 = (__byte_perm(w0[2 * ks + 1], w1[2 * ks + 1], 0x5410) & 0x000f000fu) << 6;
 #pragma unroll
                         for (int rn = 0; rn < RN; ++rn) at_mma(z[rn][n], z0, z0, z1, z1, pb[n][rn][2 * ks], pb[n][rn][2 * ks + 1]);
                     }
@@ -702,8 +708,8 @@ __global__ void __launch_bounds__(AT_THREADS, at_resident(D, G, RN)) kv4_attend_
                         for (int ks = 0; ks < 2; ++ks)
 #pragma unroll
                             for (int half = 0; half < 2; ++half) {
-                                const uint32_t x = w[2 * half] >> (8 * ks), y = w[2 * half + 1] >> (8 * ks);
-                                const uint32_t a0 = x & 0x000f000fu, a1 = y & 0x000f000fu, a2 = x & 0x00f000f0u, a3 = y & 0x00f000f0u;
+                                const uint32_t x = at_place(w[2 * half], ks), y = at_place(w[2 * half + 1], ks);
+                                const uint32_t a0 = x & AT_LOW, a1 = y & AT_LOW, a2 = x & AT_HIGH, a3 = y & AT_HIGH;
 #pragma unroll
                                 for (int rn = 0; rn < RN; ++rn) at_mma(o[rn][2 * b4 + half], a0, a1, a2, a3, pb[n][rn][2 * ks], pb[n][rn][2 * ks + 1]);
                             }
@@ -724,7 +730,7 @@ __global__ void __launch_bounds__(AT_THREADS, at_resident(D, G, RN)) kv4_attend_
         }
 
         // ---- join of the four warps: each puts its sums where its ring was (all of its copies have landed)
-        constexpr float BACK = 0x1p24f / AT_DOWN;  // codes are held times 2^-24
+        constexpr float BACK = 0x1p22f / AT_DOWN;  // codes are held times 2^-22
         float *part = reinterpret_cast<float *>(ring);
 #pragma unroll
         for (int rn = 0; rn < RN; ++rn)

@@ -64,12 +64,19 @@ def tight(c, q, out, lse, lens, nq, scale, run=512):
                 want = p @ v64[idx, h]
                 # A score: as in `check`, D / 8 + 16 additions and multiplications in fp32.  s - m is rounded once and below 2^8: 2^-17 of the weight.
                 es = scale * 2 * (qq.abs() @ kmag[idx, h].T) * (D / 8 + 16) * 2.0 ** -23 + 2.0 ** -17
+                # Of 16 products that it adds at a time the tensor core drops from each what lies below 2^-24 of the largest one's exponent (the largest itself has no
+                # such bits).  A code is held as a subnormal number, 2^-8 of what its exponent stands for, so that is 2^-16 of the largest product of a weight and a
+                # scale, from codes or from zero points, which are subtracted.
+                block = (p[..., None] * vmag[idx, h] / 15).amax(-1)
+                block = torch.nn.functional.pad(block, (0, -block.shape[-1] % 16)).unflatten(-1, (-1, 16)).amax(-1)
+                others = (len(s[0]) - 16 * torch.arange(block.shape[-1], device="cuda")).clamp(max=16) - 1
+                drop = (block * others).sum(-1, keepdim=True) * 2.0 ** -16
                 # A weight times the scale of its value is rounded to fp16: 2^-11 of it, or half a step of the subnormal numbers, 2^-25, where the largest
                 # product of the row is 2^10 or more, 16 times more in half of the blocks: 2^-31 of the largest (a value is up to 15 scales).
                 err = (p * (2.0 ** -11 + 2 * es)) @ v64[idx, h].abs() + (p * 2 * es).sum(-1, keepdim=True) * want.abs()
                 err = err + (p[..., None] * vmag[idx, h]).amax((-2, -1))[:, None] * len(s[0]) * 2.0 ** -31
                 # code and zero-point parts are added up apart, two additions per tile
-                err = err + 2 * (p @ vmag[idx, h]) * (min(len(s[0]) / 16, run) + 32) * 2.0 ** -23
+                err = err + 2 * (p @ vmag[idx, h]) * min(len(s[0]) / 16 + 2, run) * 2.0 ** -23 + drop
                 err = err + want.abs() * torch.finfo(out.dtype).eps / 2 * 1.001 + (2.0 ** -25 if out.dtype is HF else 2.0 ** -134)
                 assert bool(((o - want).abs() <= err).all()), (b, i, h, float(((o - want).abs() / err).max()))
                 el = es.amax(-1) + 2.0 ** -22 * (want_l.abs() + math.log(n) + 4)
@@ -269,3 +276,28 @@ def test_a_group_that_is_not_finite_stays_in_its_channels(every):
     tight(c, q, zero, lse0, lens, 1, D ** -0.5)
     assert bool(torch.isfinite(out[..., :32]).all()) and bool(torch.isfinite(out[..., 64:]).all())
     tight(c, q, torch.cat((out[..., :32], zero[..., 32:64], out[..., 64:]), -1), lse, lens, 1, D ** -0.5)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("D,group", [(64, 32), (64, 64), (128, 128), (256, 64)])
+@pytest.mark.parametrize("where", [0, 5, 7])
+def test_small_values_beside_a_large_one(D, group, where):
+    """A token with nine tenths of the weight and a large scale, whose value is zero in most channels: what the tokens that are added with it have there."""
+    lens = [8, 18, 33, 64]
+    c = Cache(lens, heads=1, D=D, group=group, dt=HF)
+    gen = torch.Generator(device="cuda").manual_seed(D + where)
+    rand = lambda *s: torch.randn(*s, generator=gen, device="cuda", dtype=torch.float64)  # noqa: E731
+    base = rand(D)
+    k = 0.1 * rand(sum(lens), 1, D)
+    v = (1 + 0.3 * torch.rand(sum(lens), 1, 1, generator=gen, device="cuda", dtype=torch.float64)) * torch.where(torch.arange(D, device="cuda") % 2 == 0, -1.0, 1.0)
+    at = 0
+    for n in lens:
+        k[at + where, 0] = base * (math.log(9 * n) / float(base @ base) * D ** 0.5)
+        v[at + where] = 0.0
+        v[at + where, 0, ::group], v[at + where, 0, 1::group] = 320.0, -280.0
+        at += n
+    c.kv = (k.to(HF), v.to(HF))
+    c.scap.scap_kv4_append(c.cache, *c.kv, starts(lens))
+    q = (base + 0.02 * rand(len(lens), 1, 4, D)).to(HF)
+    out, lse = attend(c, q, D ** -0.5)
+    tight(c, q, out, lse, lens, 1, D ** -0.5)
